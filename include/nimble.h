@@ -59,7 +59,8 @@ typedef enum nimble_epilogue {
   NIMBLE_EPI_BIAS_GELU_ERF = 2  /* y = gelu(x.w^T + b), gelu(v)=v/2 (1+erf(v/sqrt 2)) */
 } nimble_epilogue;
 
-typedef enum nimble_dtype { NIMBLE_BF16 = 0, NIMBLE_F32 = 1 } nimble_dtype;
+/* (2 is the VM's 64-bit integer) */
+typedef enum nimble_dtype { NIMBLE_BF16 = 0, NIMBLE_F32 = 1, NIMBLE_I8 = 3 } nimble_dtype;
 
 /* The kernel family the dispatch function chooses from.  Every tiled variant
  * exists in two copies: one compiled for residue r = 0 (no bounds code at
@@ -350,6 +351,63 @@ size_t nimble_lstm_loop_workspace_bytes(int64_t B, int64_t Ix, int64_t H);
 int nimble_lstm_loop_dyn(const void* x, const void* pre, const void* w, const void* bias, const void* h0,
                          const void* c0, void* h_seq, void* c_out, int64_t T, int64_t B, int64_t Ix, int64_t H,
                          void* workspace, size_t workspace_bytes, uint32_t max_polls, void* stream);
+
+/* ---- 8-bit products, and products whose rows belong to groups -----------------------------
+ * dense in 8-bit integers: rows are codes of -127..127 with an f32 scale each (a token of x, an output channel of w).
+ * Grouped dense: x [R,K] holds the rows of E groups (experts) one after the other, w [E,N,K] a weight for each; where the
+ * groups begin is known on the device only.  No call here needs a workspace or waits, and any number may run at once.
+ *
+ * Shape function of nimble_quantize_rows_dyn: x (M,K) -> q (M, cols), scale (M).  cols = K rounded up to whole 128 bytes, the
+ * width at which the products' loads are whole lines, where `cols` is 0; else `cols`, which must not be less than K. */
+int nimble_quantize_rows_shape(const int64_t* x_shape, int x_rank, int64_t cols, int64_t* q_shape, int64_t* scale_shape);
+
+/* scale[m] = max_k |x[m,k]| / 127 (f32), q[m,k] = 127 x[m,k] / max_k |x[m,k]| rounded to the nearest integer, ties to even (the
+ * exactly rounded code).  Codes at K .. cols-1 are 0: the product of two rows is the same over cols as over K.  A row of zeros has
+ * scale 0; a row with an infinity or a NaN has codes 0 and scale NaN, so that every result made of it is NaN.
+ * x [rows, K] of x_dtype (NIMBLE_BF16 or NIMBLE_F32), q [rows, cols] int8, scale [rows] f32. */
+int nimble_quantize_rows_dyn(const void* x, int x_dtype, void* q, void* scale, int64_t rows, int64_t K, int64_t cols, void* stream);
+
+/* Shape function of dense in 8 bits: x (M,K), x_scale (M), w (N,K), w_scale (N) -> (M,N). */
+int nimble_dense_i8_shape(const int64_t* x_shape, int x_rank, const int64_t* x_scale_shape, int x_scale_rank, const int64_t* w_shape,
+                          int w_rank, const int64_t* w_scale_shape, int w_scale_rank, int64_t* out_shape);
+
+/* y[m,n] = epi( x_scale[m] w_scale[n] sum_k x[m,k] w[n,k] + bias[n] ): x [M,K], w [N,K] int8 (any value, -128 too), the scales f32,
+ * bias [N] bf16 (NULL for NIMBLE_EPI_NONE), y [M,N] of out_dtype.  Sums in 32-bit integers, so exact: K is at most 131071
+ * (NIMBLE_ERR_ARG).  Scales, bias and epilogue in f32.  K need not be a multiple of anything; rows of whole 16 bytes are the fast ones. */
+int nimble_dense_i8_dyn(const void* x, const void* x_scale, const void* w, const void* w_scale, const void* bias, void* y, int64_t M,
+                        int64_t N, int64_t K, int epilogue, int out_dtype, void* stream);
+
+/* Shape function of grouped dense: x (R,K), w (E,N,K), offsets (E+1) -> (R,N). */
+int nimble_grouped_dense_shape(const int64_t* x_shape, int x_rank, const int64_t* w_shape, int w_rank, const int64_t* offsets_shape,
+                               int offsets_rank, int64_t* out_shape);
+
+/* y[r,:] = epi( x[r,:] . w[e]^T + bias[e] ) for the rows r in [offsets[e], offsets[e+1]) of each group e.  Rows of no group (ahead
+ * of offsets[0], from offsets[E] on) are left as they were; a group may be empty.
+ * x [R,K] bf16, w [E,N,K] bf16, bias [E,N] bf16 (NULL for NIMBLE_EPI_NONE), offsets [E+1] int64 ON THE DEVICE, 8-byte
+ * aligned, not falling and within 0..R, y [R,N] of out_dtype.  The host never sees the offsets: offsets that do not keep to this give
+ * rows of unspecified content, but no access outside the tensors.  1 <= E <= 1024 (NIMBLE_ERR_ARG; E = 0: nothing to do). */
+int nimble_grouped_dense_dyn(const void* x, const void* w, const void* bias, const void* offsets, void* y, int64_t R, int64_t E,
+                             int64_t N, int64_t K, int epilogue, int out_dtype, void* stream);
+
+/* The same in 8 bits: x [R,K] int8 with x_scale [R], w [E,N,K] int8 with w_scale [E,N]; otherwise as nimble_dense_i8_dyn. */
+int nimble_grouped_dense_i8_dyn(const void* x, const void* x_scale, const void* w, const void* w_scale, const void* bias,
+                                const void* offsets, void* y, int64_t R, int64_t E, int64_t N, int64_t K, int epilogue, int out_dtype,
+                                void* stream);
+
+/* What the dispatch function decides for a call of these products (host only): in_dtype NIMBLE_BF16 or NIMBLE_I8, E = -1 for
+ * nimble_dense_i8_dyn.  It knows R, E, N and K, not how the rows fall on the groups: the grid is for the most tiles there can be. */
+typedef enum nimble_product_kernel {
+  NIMBLE_PRODUCT_DIRECT = 0, /* any alignment: operands straight into the matrix instruction's registers */
+  NIMBLE_PRODUCT_COUNT = 1
+} nimble_product_kernel;
+typedef struct nimble_product_plan {
+  int32_t kernel;     /* nimble_product_kernel                                    */
+  int32_t bm, bn;     /* rows and columns of a tile                               */
+  int32_t k_waves;    /* waves of a workgroup among which K is divided            */
+  int64_t tiles;      /* the most tiles there can be                              */
+  uint32_t grid, block;
+} nimble_product_plan;
+int nimble_product_plan_of(int64_t R, int64_t E, int64_t N, int64_t K, int in_dtype, int out_dtype, nimble_product_plan* plan);
 
 #ifdef __cplusplus
 }

@@ -13,7 +13,7 @@ _LIB_PATH = os.environ.get("NIMBLE_LIBRARY") or os.path.join(_PKG, "libnimble_hi
 _HEADERS = [os.path.join(os.path.dirname(_PKG), "include", h) for h in ("nimble.h", "nimble_probe.h", "nimble_vm.h")]
 
 EPI_NONE, EPI_BIAS, EPI_BIAS_GELU_ERF = 0, 1, 2
-BF16, F32 = 0, 1
+BF16, F32, I8 = 0, 1, 3
 VAR_AUTO = -1
 
 _STATUS = {0: "OK", -1: "ERR_NULL", -2: "ERR_RANK", -3: "ERR_SHAPE", -4: "ERR_DTYPE", -5: "ERR_ALIGN",
@@ -38,6 +38,22 @@ class _CPlan(ctypes.Structure):
                 ("grid", ctypes.c_uint32 * 3), ("block", ctypes.c_uint32),
                 ("workspace_bytes", ctypes.c_uint64), ("split_rows", ctypes.c_int64),
                 ("residue_variant", ctypes.c_int32), ("residue_split_k", ctypes.c_int32)]
+
+
+class _CProductPlan(ctypes.Structure):
+    _fields_ = [("kernel", ctypes.c_int32), ("bm", ctypes.c_int32), ("bn", ctypes.c_int32), ("k_waves", ctypes.c_int32),
+                ("tiles", ctypes.c_int64), ("grid", ctypes.c_uint32), ("block", ctypes.c_uint32)]
+
+
+@dataclass
+class ProductPlan:
+    kernel: int
+    bm: int
+    bn: int
+    k_waves: int
+    tiles: int
+    grid: int
+    block: int
 
 
 @dataclass
@@ -129,6 +145,14 @@ def load():
                                            ctypes.c_uint32, ctypes.c_uint32, vp]
     lib.nimble_probe_mfma_bf16.argtypes = [vp, vp, i32, i32, ctypes.POINTER(ctypes.c_double), vp]
     lib.nimble_probe_hbm_read.argtypes = [vp, ctypes.c_size_t, vp, vp]
+    lib.nimble_quantize_rows_shape.argtypes = [ip, i32, i64, ip, ip]
+    lib.nimble_quantize_rows_dyn.argtypes = [vp, i32, vp, vp, i64, i64, i64, vp]
+    lib.nimble_dense_i8_shape.argtypes = [ip, i32, ip, i32, ip, i32, ip, i32, ip]
+    lib.nimble_dense_i8_dyn.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, i64, i32, i32, vp]
+    lib.nimble_grouped_dense_shape.argtypes = [ip, i32, ip, i32, ip, i32, ip]
+    lib.nimble_grouped_dense_dyn.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, i64, i32, i32, vp]
+    lib.nimble_grouped_dense_i8_dyn.argtypes = [vp, vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, i32, i32, vp]
+    lib.nimble_product_plan_of.argtypes = [i64, i64, i64, i64, i32, i32, ctypes.POINTER(_CProductPlan)]
     _lib = lib
     return lib
 
@@ -335,6 +359,36 @@ def lstm_plan(B: int, Ix: int, H: int) -> Plan:
     return _plan(c)
 
 
+def quantize_rows_shape(x_shape: Sequence[int], cols: int = 0) -> Tuple[Tuple[int, int], Tuple[int]]:
+    """Shapes of the codes and of the scales; cols = 0: K rounded up to whole 128 bytes."""
+    q, s = (ctypes.c_int64 * 2)(-1, -1), (ctypes.c_int64 * 1)(-1)
+    _check(load().nimble_quantize_rows_shape(_arr(x_shape), len(x_shape), cols, q, s))
+    return (int(q[0]), int(q[1])), (int(s[0]),)
+
+
+def dense_i8_shape(x_shape, x_scale_shape, w_shape, w_scale_shape) -> Tuple[int, int]:
+    out = (ctypes.c_int64 * 2)(-1, -1)
+    _check(load().nimble_dense_i8_shape(_arr(x_shape), len(x_shape), _arr(x_scale_shape), len(x_scale_shape), _arr(w_shape),
+                                        len(w_shape), _arr(w_scale_shape), len(w_scale_shape), out))
+    return int(out[0]), int(out[1])
+
+
+def grouped_dense_shape(x_shape, w_shape, offsets_shape) -> Tuple[int, int]:
+    out = (ctypes.c_int64 * 2)(-1, -1)
+    _check(load().nimble_grouped_dense_shape(_arr(x_shape), len(x_shape), _arr(w_shape), len(w_shape), _arr(offsets_shape),
+                                             len(offsets_shape), out))
+    return int(out[0]), int(out[1])
+
+
+def product_plan(R: int, E: Optional[int], N: int, K: int, in_dtype: int = I8, out_dtype: int = BF16) -> ProductPlan:
+    """The dispatch decision of dense_i8 (E = None) or of a grouped product."""
+    c = _CProductPlan()
+    if E is not None and E < 0:
+        raise NimbleError(-8, "negative extent")
+    _check(load().nimble_product_plan_of(R, -1 if E is None else E, N, K, in_dtype, out_dtype, ctypes.byref(c)))
+    return ProductPlan(c.kernel, c.bm, c.bn, c.k_waves, c.tiles, c.grid, c.block)
+
+
 # ---------------------------------------------------------------- device side
 # Pointers are integers (tensor.data_ptr()); `stream` is a hipStream_t handle as
 # an integer (torch.cuda.current_stream().cuda_stream), 0 for the default one.
@@ -411,3 +465,22 @@ def nimble_probe_lstm_loop(x: int, pre: int, w: int, bias: int, h0: int, c0: int
     """The token loop with workgroups of even (bit 0 of apart) and odd number (bit 1) storing as if their row group did not share an XCD."""
     _check(load().nimble_probe_lstm_loop(x, pre, w, bias, h0, c0, h_seq, c_out, T, B, Ix, H, workspace, workspace_bytes, max_polls,
                                          apart, stream))
+
+
+def nimble_quantize_rows_dyn(x: int, x_dtype: int, q: int, scale: int, rows: int, K: int, cols: int, stream: int = 0) -> None:
+    _check(load().nimble_quantize_rows_dyn(x, x_dtype, q, scale, rows, K, cols, stream))
+
+
+def nimble_dense_i8_dyn(x: int, x_scale: int, w: int, w_scale: int, bias: int, y: int, M: int, N: int, K: int, epilogue: int,
+                        out_dtype: int = BF16, stream: int = 0) -> None:
+    _check(load().nimble_dense_i8_dyn(x, x_scale, w, w_scale, bias, y, M, N, K, epilogue, out_dtype, stream))
+
+
+def nimble_grouped_dense_dyn(x: int, w: int, bias: int, offsets: int, y: int, R: int, E: int, N: int, K: int, epilogue: int,
+                             out_dtype: int = BF16, stream: int = 0) -> None:
+    _check(load().nimble_grouped_dense_dyn(x, w, bias, offsets, y, R, E, N, K, epilogue, out_dtype, stream))
+
+
+def nimble_grouped_dense_i8_dyn(x: int, x_scale: int, w: int, w_scale: int, bias: int, offsets: int, y: int, R: int, E: int, N: int,
+                                K: int, epilogue: int, out_dtype: int = BF16, stream: int = 0) -> None:
+    _check(load().nimble_grouped_dense_i8_dyn(x, x_scale, w, w_scale, bias, offsets, y, R, E, N, K, epilogue, out_dtype, stream))

@@ -9,18 +9,14 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libnimble_hip.so")
 HOST_CALLS = os.path.join(PKG, "_host_calls.so")
-SOURCES = ["nimble_host.cpp", "nimble_vm.cpp", "nimble_kernels.hip"]  # the .h files under csrc/ hold the kernels
+SOURCES = ["nimble_host.cpp", "grouped_host.cpp", "nimble_vm.cpp", "nimble_kernels.hip", "grouped_kernels.hip"]  # the .h files under csrc/ hold the kernels
 
 
-def hipcc_command(out: str = LIB):
-    return [
-        "hipcc", "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
-        "-I" + os.path.join(ROOT, "include"), "-I" + CSRC,
-        # keep the compiler from forming packed-fp32 instructions
-        "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-        *[os.path.join(CSRC, s) for s in SOURCES],
-        "-o", out,
-    ]
+FLAGS = [
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-I" + os.path.join(ROOT, "include"), "-I" + CSRC,
+    # keep the compiler from forming packed-fp32 instructions
+    "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+]
 
 
 def host_calls_command(out: str = HOST_CALLS):
@@ -47,11 +43,22 @@ def build_host_calls() -> str:
 
 
 def build_library(verbose: bool = False) -> str:
+    import tempfile
+    from concurrent.futures import ThreadPoolExecutor
+
+    def run(command):
+        return subprocess.run(command, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+
     build_host_calls()
-    proc = subprocess.run(hipcc_command(), stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    with tempfile.TemporaryDirectory() as tmp:
+        objects = [os.path.join(tmp, s + ".o") for s in SOURCES]
+        with ThreadPoolExecutor(len(SOURCES)) as pool:   # side by side: nimble_kernels.hip alone is most of the time
+            done = list(pool.map(run, [["hipcc", *FLAGS, "-c", os.path.join(CSRC, s), "-o", o] for s, o in zip(SOURCES, objects)]))
+        if all(p.returncode == 0 for p in done):
+            done.append(run(["hipcc", "--offload-arch=gfx950", "-fPIC", "-shared", *objects, "-o", LIB]))
     noise = "is not a recognized feature for this target"
-    log = "\n".join(l for l in proc.stdout.splitlines() if noise not in l)
-    if proc.returncode != 0:
+    log = "\n".join(l for p in done for l in p.stdout.splitlines() if noise not in l)
+    if any(p.returncode != 0 for p in done):
         raise RuntimeError("hipcc failed:\n" + log)
     if verbose and log.strip():
         print(log)
@@ -61,19 +68,17 @@ def build_library(verbose: bool = False) -> str:
 def device_assembly() -> str:
     """The gfx950 assembly of the kernels, as text (same flags as the library)."""
     import tempfile
+    text = ""
     with tempfile.TemporaryDirectory() as tmp:
-        out = os.path.join(tmp, "kernels.s")
-        cmd = [
-            "hipcc", "--offload-arch=gfx950", "-O3", "-std=c++17", "--cuda-device-only", "-S",
-            "-I" + os.path.join(ROOT, "include"), "-I" + CSRC,
-            "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-            os.path.join(CSRC, "nimble_kernels.hip"), "-o", out,
-        ]
-        proc = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
-        if proc.returncode != 0:
-            raise RuntimeError("hipcc -S failed:\n" + proc.stdout[-4000:])
-        with open(out) as f:
-            return f.read()
+        for source in (s for s in SOURCES if s.endswith(".hip")):
+            out = os.path.join(tmp, "kernels.s")
+            cmd = ["hipcc", *FLAGS, "--cuda-device-only", "-S", os.path.join(CSRC, source), "-o", out]
+            proc = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+            if proc.returncode != 0:
+                raise RuntimeError("hipcc -S failed:\n" + proc.stdout[-4000:])
+            with open(out) as f:
+                text += f.read()
+    return text
 
 
 def _agprs(text: str) -> set:

@@ -1,0 +1,238 @@
+// Products whose rows fall into groups with a weight each, at offsets that only the device knows: the map from workgroups to
+// tiles, the epilogue, and the kernel for operands of any alignment.
+#ifndef NIMBLE_GROUPED_KERNEL_H_
+#define NIMBLE_GROUPED_KERNEL_H_
+#include <type_traits>
+
+#include "device_common.h"
+#include "grouped_internal.h"
+
+namespace nimble {
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+// The matrix instruction of an element type.  Either takes 16 bytes of one row per lane (row lane & 15, piece lane >> 4), 64 bytes
+// of K per instruction, and leaves four consecutive n of one m in a lane: the kernels differ in nothing else.
+struct OfBf16 {
+  typedef f32x4 Acc;
+  static constexpr bool kInt8 = false;
+  static __device__ __forceinline__ Acc mfma(uint4 w, uint4 x, Acc c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(w), as_bf16x8(x), c, 0, 0, 0);
+  }
+};
+struct OfInt8 {
+  typedef i32x4 Acc;
+  static constexpr bool kInt8 = true;
+  static __device__ __forceinline__ Acc mfma(uint4 w, uint4 x, Acc c) {
+    return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, w), __builtin_bit_cast(i32x4, x), c, 0, 0, 0);
+  }
+};
+
+// Where the tiles of a launch are.  With groups, tile rows are counted group after group, a group of m rows has ceil(m / BM) of
+// them; `ends[e]` is their number up to and with group e, `starts[e]` the group's first row.  Offsets are brought into [0, rows], and one
+// that falls to the largest before it: whatever they hold, groups do not overlap, no access leaves the operands, and
+// there are no more tiles than the host allowed for.
+struct GroupMap {
+  int ends[kMostGroups];
+  int starts[kMostGroups + 1];
+};
+// Filled by the first wave; the caller's barrier publishes it.
+template <int BM>
+__device__ __forceinline__ void map_groups(const ProductArgs& g, GroupMap& map) {
+  if (threadIdx.x >= 64) return;
+  const int lane = (int)threadIdx.x;
+  int tiles = 0, furthest = 0;
+  for (int base = 0; base < g.groups; base += 64) {
+    const int e = base + lane;
+    int first = 0, end = 0;
+    if (e < g.groups) {
+      first = (int)min(max(g.offsets[e], 0ll), g.rows);
+      end = (int)min(max(g.offsets[e + 1], 0ll), g.rows);
+    }
+    first = max(first, furthest);
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int up = __shfl_up(first, o, 64);
+      if (lane >= o) first = max(first, up);
+    }
+    end = e < g.groups ? max(end, first) : first;
+    furthest = max(furthest, __shfl(end, 63, 64));
+    int n = (int)(((long long)end - first + BM - 1) / BM);
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int up = __shfl_up(n, o, 64);
+      if (lane >= o) n += up;
+    }
+    n += tiles;
+    if (e < g.groups) {
+      map.ends[e] = n;
+      map.starts[e] = first;
+      if (e == g.groups - 1) map.starts[g.groups] = end;
+    }
+    tiles = __shfl(n, 63, 64);
+  }
+}
+// The group of tile row t (t < ends[groups - 1]): as many groups end at or before it.  The same in all lanes.
+__device__ __forceinline__ int group_of_tile_row(const GroupMap& map, int groups, int t) {
+  int e = 0;
+  for (int base = 0; base < groups; base += 64) {
+    const int i = base + (int)(threadIdx.x & 63);
+    e += __popcll(__ballot(i < groups && map.ends[i] <= t));
+  }
+  return e;
+}
+
+struct ProductTile {
+  long long row0;  // first row of the tile
+  int rows;        // of its group from there on, at most BM of them are the tile's
+  int group, n0;
+};
+
+// The 16 bytes at byte `at` of a row; past the end of the row zero.  Any alignment.
+__device__ __forceinline__ uint4 load16(const unsigned char* row, int at, int row_bytes) {
+  uint4 v = make_uint4(0, 0, 0, 0);
+  const int left = row_bytes - at;
+  if (left >= 16) {
+    __builtin_memcpy(&v, row + at, 16);
+  } else if (left > 0 && row_bytes >= 16) {  // the row's last 16 bytes, moved down
+    __builtin_memcpy(&v, row + row_bytes - 16, 16);
+    const uint64_t lo = ((uint64_t)v.y << 32) | v.x, hi = ((uint64_t)v.w << 32) | v.z;
+    const int sh = 8 * (16 - left);  // 8 .. 120 bits
+    const uint64_t rlo = sh < 64 ? (lo >> sh) | (hi << (64 - sh)) : hi >> (sh - 64);
+    const uint64_t rhi = sh < 64 ? hi >> sh : 0;
+    v = make_uint4((uint32_t)rlo, (uint32_t)(rlo >> 32), (uint32_t)rhi, (uint32_t)(rhi >> 32));
+  } else if (left > 0) {
+    uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int b = 0; b < 15; ++b)
+      if (b < left) w[b >> 2] |= (uint32_t)row[at + b] << (8 * (b & 3));
+    v = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  return v;
+}
+
+// Four consecutive outputs of a row from their sums.  8-bit products: the row's and the column's scale are
+// multiplied first and the product with the (exact) sum is rounded once more; either way three roundings of 2^-24 in all.
+template <typename T>
+__device__ __forceinline__ void store4(const ProductArgs& g, const float (&sum)[4], int group, long long row, int n) {
+  const float xs = T::kInt8 ? g.x_scale[row] : 1.0f;
+  const int n4 = g.N - n;
+  float v[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const long long c = (long long)group * g.N + (e < n4 ? n + e : n);
+    const float b = g.epilogue != NIMBLE_EPI_NONE ? bf2f(g.bias[c]) : 0.0f;
+    const float s = T::kInt8 ? sum[e] * (xs * g.w_scale[c]) : sum[e];
+    v[e] = s + b;
+  }
+  if (g.epilogue == NIMBLE_EPI_BIAS_GELU_ERF) epilogue_of<true>(v);
+  const long long at = row * g.N + n;
+  if (g.out_f32) {
+    float* y = (float*)g.y + at;
+    if (n4 >= 4) {
+      __builtin_memcpy(y, v, 16);
+    } else {
+      for (int e = 0; e < n4; ++e) y[e] = v[e];
+    }
+  } else {
+    u16* y = (u16*)g.y + at;
+    if (n4 >= 4) {
+      const uint2 pk = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+      __builtin_memcpy(y, &pk, 8);
+    } else {
+      for (int e = 0; e < n4; ++e) y[e] = f2bf(v[e]);
+    }
+  }
+}
+
+// The tile at tile row t and tile column tn; false where there is none (fewer tile rows than the host had to allow for).
+template <int BM, int BN, bool GROUPED>
+__device__ __forceinline__ bool find_tile(const ProductArgs& g, const GroupMap* map, int t, int tn, ProductTile& tile) {
+  tile.n0 = tn * BN;
+  tile.group = 0;
+  tile.row0 = (long long)t * BM;
+  long long end = g.rows;
+  if (GROUPED) {
+    if (t >= map->ends[g.groups - 1]) return false;
+    tile.group = group_of_tile_row(*map, g.groups, t);
+    tile.row0 = map->starts[tile.group] + (long long)(t - (tile.group ? map->ends[tile.group - 1] : 0)) * BM;
+    end = map->starts[tile.group + 1];
+  }
+  tile.rows = (int)min(end - tile.row0, (long long)BM);
+  return true;
+}
+
+// ---------------------------------------------------------------------------
+// Any alignment: TM x TN blocks of 16 x 16 per workgroup, KW waves that take pieces of 64 bytes of K in turn, operands from
+// memory straight into the registers that the matrix instruction reads; the waves' sums meet in LDS.
+// ---------------------------------------------------------------------------
+template <typename T, bool GROUPED, int TM, int TN, int KW>
+__global__ void __launch_bounds__(KW * 64) product_direct_kernel(ProductArgs g, unsigned tiles, unsigned tiles_n) {
+  constexpr int BM = 16 * TM, BN = 16 * TN;
+  typedef typename T::Acc Acc;
+  __shared__ typename std::conditional<GROUPED, GroupMap, int>::type map_[1];
+  const GroupMap* map = (const GroupMap*)map_;
+  __shared__ __attribute__((aligned(16))) Acc sums[KW][TM * TN * 64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int fr_row = lane & 15, fr_at = (lane >> 4) * 16;
+  if (GROUPED) {
+    map_groups<BM>(g, (GroupMap&)map_[0]);
+    __syncthreads();
+  }
+  for (unsigned b = blockIdx.x; b < tiles; b += gridDim.x) {
+    ProductTile tile;
+    const unsigned t = b / tiles_n;
+    if (!find_tile<BM, BN, GROUPED>(g, map, (int)t, (int)(b - t * tiles_n), tile)) return;
+    const unsigned char *xp[TM], *wp[TN];
+#pragma unroll
+    for (int j = 0; j < TM; ++j) xp[j] = g.x + (tile.row0 + min(16 * j + fr_row, tile.rows - 1)) * g.row_bytes;
+#pragma unroll
+    for (int i = 0; i < TN; ++i) wp[i] = g.w + ((long long)tile.group * g.N + min(tile.n0 + 16 * i + fr_row, g.N - 1)) * g.row_bytes;
+    Acc acc[TN][TM];
+#pragma unroll
+    for (int i = 0; i < TN; ++i)
+#pragma unroll
+      for (int j = 0; j < TM; ++j) acc[i][j] = Acc{0, 0, 0, 0};
+    uint4 x[TM], w[TN];
+    int at = wave * 64;
+    for (; at + 64 <= g.row_bytes; at += KW * 64) {
+#pragma unroll
+      for (int i = 0; i < TN; ++i) __builtin_memcpy(&w[i], wp[i] + at + fr_at, 16);
+#pragma unroll
+      for (int j = 0; j < TM; ++j) __builtin_memcpy(&x[j], xp[j] + at + fr_at, 16);
+#pragma unroll
+      for (int i = 0; i < TN; ++i)
+#pragma unroll
+        for (int j = 0; j < TM; ++j) acc[i][j] = T::mfma(w[i], x[j], acc[i][j]);
+    }
+    if (at < g.row_bytes) {
+#pragma unroll
+      for (int i = 0; i < TN; ++i) w[i] = load16(wp[i], at + fr_at, g.row_bytes);
+#pragma unroll
+      for (int j = 0; j < TM; ++j) x[j] = load16(xp[j], at + fr_at, g.row_bytes);
+#pragma unroll
+      for (int i = 0; i < TN; ++i)
+#pragma unroll
+        for (int j = 0; j < TM; ++j) acc[i][j] = T::mfma(w[i], x[j], acc[i][j]);
+    }
+    if (b != blockIdx.x) __syncthreads();  // the tile before has been read
+#pragma unroll
+    for (int i = 0; i < TN; ++i)
+#pragma unroll
+      for (int j = 0; j < TM; ++j) sums[wave][(i * TM + j) * 64 + lane] = acc[i][j];
+    __syncthreads();
+    for (int o = threadIdx.x; o < TM * TN * 64; o += KW * 64) {
+      Acc s = sums[0][o];
+#pragma unroll
+      for (int k = 1; k < KW; ++k) s += sums[k][o];
+      const int l = o & 63, block = o >> 6, i = block / TM, j = block % TM;
+      const int r = 16 * j + (l & 15), n = tile.n0 + 16 * i + 4 * (l >> 4);
+      if (r >= tile.rows || n >= g.N) continue;
+      const float v[4] = {(float)s[0], (float)s[1], (float)s[2], (float)s[3]};
+      store4<T>(g, v, tile.group, tile.row0 + r, n);
+    }
+  }
+}
+
+}  // namespace nimble
+#endif

@@ -865,7 +865,7 @@ size_t nimble_lstm_loop_workspace_bytes(int64_t B, int64_t Ix, int64_t H) {
 int64_t nimble_storage_bytes(const int64_t* shape, int rank, int dtype) {
   clear_error();
   if (rank < 0 || (rank > 0 && !shape)) return fail(NIMBLE_ERR_NULL, "null shape pointer");
-  const size_t es = dtype_size(dtype);
+  const size_t es = dtype == NIMBLE_I8 ? 1 : dtype_size(dtype);
   if (es == 0) return fail(NIMBLE_ERR_DTYPE, "unknown dtype %d", dtype);
   int64_t n = 1;
   for (int i = 0; i < rank; ++i) {

@@ -37,7 +37,7 @@ try:
 except ImportError as e:
     _host_calls = _StepsOnly(e)
 
-_TORCH_DTYPE = {nb.BF16: torch.bfloat16, nb.F32: torch.float32}
+_TORCH_DTYPE = {nb.BF16: torch.bfloat16, nb.F32: torch.float32, nb.I8: torch.int8}
 
 
 try:  # raw handle of torch's current stream without building a Stream object (several us cheaper)
@@ -237,6 +237,99 @@ def fused_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, alpha: fl
     if not _bound:
         _bind_host_calls(q.device)
     return o
+
+
+def _together(**tensors):
+    """The device that all of these tensors are on, made the current one for the call: the library launches on the stream of
+    the current device."""
+    device = None
+    for what, t in tensors.items():
+        if t is None:
+            continue
+        if not t.is_cuda or (device is not None and t.device != device):
+            raise nb.NimbleError(-8, f"{what} is on {t.device}" + (f", the operands before it on {device}" if device is not None else
+                                                                   ", not on a GPU"))
+        device = t.device
+    return torch.cuda.device(device)
+
+
+def _output(out: Optional[torch.Tensor], shape, dtype: int, device, what: str) -> torch.Tensor:
+    if dtype not in (nb.BF16, nb.F32):
+        raise nb.NimbleError(-4, f"{what}: unknown output dtype {dtype}")
+    if out is None:
+        return _alloc(shape, dtype, device)
+    if tuple(out.shape) != tuple(shape):
+        raise nb.NimbleError(-3, f"{what}: out is {tuple(out.shape)}, the shape function gives {tuple(shape)}")
+    return out
+
+
+def _bias(bias: Optional[torch.Tensor], shape, epilogue: int, what: str) -> int:
+    if epilogue == nb.EPI_NONE:
+        return 0
+    if bias is None:
+        raise nb.NimbleError(-1, f"{what}: this epilogue needs a bias")
+    if tuple(bias.shape) != tuple(shape):
+        raise nb.NimbleError(-3, f"{what}: bias is {tuple(bias.shape)}, {tuple(shape)} needed")
+    return _ptr(bias, _BF, "bias")
+
+
+def quantize_rows(x: torch.Tensor, cols: int = 0) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Rows of x [M, K] (bf16 or f32) as 8-bit codes q [M, cols] and a scale each (f32 [M]): x is about q * scale.  Codes past K are
+    0; cols = 0 rounds K up to whole 128 bytes.  Serves tokens and, row by row of w [N, K], output channels alike; a stack of
+    experts' weights w [E, N, K] is quantised as w.view(E * N, K) and its results viewed back."""
+    q_shape, s_shape = nb.quantize_rows_shape(tuple(x.shape), cols)
+    if x.dtype not in (_BF, _F32):
+        raise nb.NimbleError(-4, f"quantize_rows: x is {x.dtype}")
+    with _together(x=x):
+        px = _ptr(x, x.dtype, "x")
+        q, scale = _alloc(q_shape, nb.I8, x.device), _alloc(s_shape, nb.F32, x.device)
+        nb.nimble_quantize_rows_dyn(px, nb.BF16 if x.dtype is _BF else nb.F32, q.data_ptr(), scale.data_ptr(), x.shape[0], x.shape[1],
+                                    q_shape[1], _stream())
+    return q, scale
+
+
+def dense_i8(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, bias: Optional[torch.Tensor] = None,
+             epilogue: int = nb.EPI_BIAS, out_dtype: int = nb.BF16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """dense in 8-bit integers: y = epi(x_scale[m] w_scale[n] x.w^T + bias), x [M, K] and w [N, K] int8 with their scales (the results of
+    quantize_rows), sums exact in 32 bits."""
+    M, N = nb.dense_i8_shape(tuple(x.shape), tuple(x_scale.shape), tuple(w.shape), tuple(w_scale.shape))
+    with _together(x=x, x_scale=x_scale, w=w, w_scale=w_scale, bias=bias, out=out):
+        y = _output(out, (M, N), out_dtype, x.device, "dense_i8")
+        nb.nimble_dense_i8_dyn(_ptr(x, torch.int8, "x"), _ptr(x_scale, _F32, "x_scale"), _ptr(w, torch.int8, "w"),
+                               _ptr(w_scale, _F32, "w_scale"), _bias(bias, (N,), epilogue, "dense_i8"),
+                               _ptr(y, _TORCH_DTYPE[out_dtype], "y"), M, N, x.shape[1], epilogue, out_dtype, _stream())
+    return y
+
+
+def grouped_dense(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor], offsets: torch.Tensor, epilogue: int = nb.EPI_BIAS,
+                  out_dtype: int = nb.BF16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """dense for rows that belong to E groups (experts) with a weight each: rows offsets[e] .. offsets[e+1]-1 of x [R, K] times
+    w[e] of [E, N, K], bias [E, N].  offsets [E+1] is int64 on the GPU and is not waited for.  Rows of no group are left as they
+    were in `out` (unspecified in a new output)."""
+    R, N = nb.grouped_dense_shape(tuple(x.shape), tuple(w.shape), tuple(offsets.shape))
+    with _together(x=x, w=w, bias=bias, offsets=offsets, out=out):
+        y = _output(out, (R, N), out_dtype, x.device, "grouped_dense")
+        nb.nimble_grouped_dense_dyn(_ptr(x, _BF, "x"), _ptr(w, _BF, "w"), _bias(bias, w.shape[:2], epilogue, "grouped_dense"),
+                                    _ptr(offsets, torch.int64, "offsets"), _ptr(y, _TORCH_DTYPE[out_dtype], "y"), R, w.shape[0], N,
+                                    x.shape[1], epilogue, out_dtype, _stream())
+    return y
+
+
+def grouped_dense_i8(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, bias: Optional[torch.Tensor],
+                     offsets: torch.Tensor, epilogue: int = nb.EPI_BIAS, out_dtype: int = nb.BF16,
+                     out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """grouped_dense in 8-bit integers: x [R, K] int8 with x_scale [R], w [E, N, K] int8 with w_scale [E, N]."""
+    R, N = nb.grouped_dense_shape(tuple(x.shape), tuple(w.shape), tuple(offsets.shape))
+    if tuple(x_scale.shape) != (R,) or tuple(w_scale.shape) != tuple(w.shape[:2]):
+        raise nb.NimbleError(-3, f"grouped_dense_i8: scales of {tuple(x_scale.shape)} and {tuple(w_scale.shape)} for x {tuple(x.shape)} "
+                                 f"and w {tuple(w.shape)}")
+    with _together(x=x, x_scale=x_scale, w=w, w_scale=w_scale, bias=bias, offsets=offsets, out=out):
+        y = _output(out, (R, N), out_dtype, x.device, "grouped_dense_i8")
+        nb.nimble_grouped_dense_i8_dyn(_ptr(x, torch.int8, "x"), _ptr(x_scale, _F32, "x_scale"), _ptr(w, torch.int8, "w"),
+                                       _ptr(w_scale, _F32, "w_scale"), _bias(bias, w.shape[:2], epilogue, "grouped_dense_i8"),
+                                       _ptr(offsets, torch.int64, "offsets"), _ptr(y, _TORCH_DTYPE[out_dtype], "y"), R, w.shape[0], N,
+                                       x.shape[1], epilogue, out_dtype, _stream())
+    return y
 
 
 def lstm_step(x: torch.Tensor, h: torch.Tensor, w: torch.Tensor, bias: torch.Tensor, c: torch.Tensor,
