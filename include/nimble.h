@@ -398,7 +398,9 @@ int nimble_grouped_dense_i8_dyn(const void* x, const void* x_scale, const void* 
  * nimble_dense_i8_dyn.  It knows R, E, N and K, not how the rows fall on the groups: the grid is for the most tiles there can be. */
 typedef enum nimble_product_kernel {
   NIMBLE_PRODUCT_DIRECT = 0, /* any alignment: operands straight into the matrix instruction's registers */
-  NIMBLE_PRODUCT_COUNT = 1
+  NIMBLE_PRODUCT_TILES = 1,  /* large tiles by four waves, rows of whole 16 bytes                        */
+  NIMBLE_PRODUCT_STREAM = 2, /* small tiles, K divided among a workgroup's waves, rows of whole 16 bytes */
+  NIMBLE_PRODUCT_COUNT = 3
 } nimble_product_kernel;
 typedef struct nimble_product_plan {
   int32_t kernel;     /* nimble_product_kernel                                    */

@@ -1,23 +1,48 @@
 // Shape functions and the dispatch function of the 8-bit and the grouped products.  Integer arithmetic only; no HIP call.
 #include "grouped_internal.h"
 
+#include <cstdlib>
+#include <cstdio>
+
 namespace nimble {
 
 static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 int plan_product(const ProductShape& s, nimble_product_plan* p) {
   nimble_product_plan out{};
-  out.kernel = NIMBLE_PRODUCT_DIRECT;
-  out.bm = s.rows <= 16 * (s.grouped ? s.groups : 1) ? 16 : 64;
-  out.bn = out.bm == 16 ? 16 : 64;
-  out.k_waves = out.bm == 16 ? 8 : 4;
-  out.block = 64u * (unsigned)out.k_waves;
+  const int64_t rb = s.row_bytes(), ks = ceil_div(rb, 128);
+  const bool tiles_ok = rb % 16 == 0 && rb <= kMostTileRowBytes && s.N <= kMostTileColumns && s.N % 8 == 0 && (rb % 128 == 0 ? ks >= 3 : ks >= 4);
+  const int64_t most_groups = s.grouped ? s.groups : 1;
+  static const char* fs = getenv("PRODUCT");  // k,bm
+  int fk = -1, fb = 0;
+  if (fs) sscanf(fs, "%d,%d", &fk, &fb);
+  int64_t most = kMostWorkgroups;
+  const bool stream_ok = rb % 16 == 0 && rb > 0 && rb <= kMostTileRowBytes;
+  if (fk == 1 ? tiles_ok : fk < 0 && tiles_ok && s.rows >= 256 * most_groups) {
+    out.kernel = NIMBLE_PRODUCT_TILES;
+    out.bm = 128;
+    out.bn = 256;
+    out.k_waves = 1;
+    out.block = 256;
+    most = 256;
+  } else if (stream_ok && fk != 0) {
+    out.kernel = NIMBLE_PRODUCT_STREAM;
+    out.bm = out.bn = fb ? fb : s.rows <= 16 * most_groups ? 16 : s.rows <= 64 * most_groups ? 32 : 64;
+    out.k_waves = 4;
+    out.block = 256;
+  } else {
+    out.kernel = NIMBLE_PRODUCT_DIRECT;
+    out.bm = fb ? fb : s.rows <= 16 * most_groups ? 16 : 64;
+    out.bn = out.bm;
+    out.k_waves = out.bm == 16 ? 8 : 4;
+    out.block = 64u * (unsigned)out.k_waves;
+  }
   // a group adds at most one tile row that is not full, and only if it has a row
   const int64_t tile_rows = s.grouped ? s.rows / out.bm + (s.groups < s.rows ? s.groups : s.rows) : ceil_div(s.rows, out.bm);
   const int64_t tiles_n = ceil_div(s.N, out.bn);
   if (tile_rows > 0x7fffffffll / (tiles_n > 0 ? tiles_n : 1)) return fail(NIMBLE_ERR_ARG, "more than 2^31 tiles");
   out.tiles = tile_rows * tiles_n;
-  out.grid = (uint32_t)(out.tiles < kMostWorkgroups ? out.tiles : kMostWorkgroups);
+  out.grid = (uint32_t)(out.tiles < most ? out.tiles : most);
   *p = out;
   return NIMBLE_OK;
 }

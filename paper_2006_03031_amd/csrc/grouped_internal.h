@@ -21,12 +21,15 @@ struct ProductArgs {
 };
 
 // Groups whose first rows and tile counts a workgroup keeps in LDS.
-constexpr int kMostGroups = 1024;
+constexpr int kMostGroups = 1024, kFewGroups = 512;  // (the latter where two workgroups share a compute unit)
 // A launch is of fewer than 2^32 threads; workgroups go round where there is more to do.
 constexpr int64_t kMostWorkgroups = 1 << 21;
 // 8-bit codes are down to -128: K * 128 * 128 stays below 2^31.
 constexpr int64_t kMostK8 = 131071;
 constexpr int64_t kMostK16 = 1ll << 22;
+
+// Offsets inside a tile of 256 rows stay below 2^31.
+constexpr int64_t kMostTileRowBytes = 1ll << 22, kMostTileColumns = 1ll << 20;
 
 struct ProductShape {
   int64_t rows, groups, N, K;

@@ -28,17 +28,37 @@ struct OfInt8 {
   }
 };
 
+typedef int rsrc_t __attribute__((ext_vector_type(4)));
+// The first `bytes` (below 2^31) from p on.
+__device__ __forceinline__ rsrc_t descriptor(const void* p, uint32_t bytes) {
+  const uint64_t a = (uint64_t)p;
+  return rsrc_t{__builtin_amdgcn_readfirstlane((int)(uint32_t)a), __builtin_amdgcn_readfirstlane((int)(uint32_t)(a >> 32)),
+                __builtin_amdgcn_readfirstlane((int)bytes), 0x00027000};
+}
+// 16 bytes per lane from the descriptor's byte voff + soff to LDS; past its end zeros.
+__device__ __forceinline__ void dma16_buffer(uint32_t voff, rsrc_t rsrc, uint32_t soff, uint32_t lds_addr) {
+  asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds" ::"v"(voff), "s"(rsrc), "s"(soff),
+               "s"(lds_addr)
+               : "memory", "m0");
+}
+__device__ __forceinline__ void dma4_buffer(uint32_t voff, rsrc_t rsrc, uint32_t lds_addr) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds" ::"v"(voff), "s"(rsrc), "s"(lds_addr)
+               : "memory", "m0");
+}
+
 // Where the tiles of a launch are.  With groups, tile rows are counted group after group, a group of m rows has ceil(m / BM) of
 // them; `ends[e]` is their number up to and with group e, `starts[e]` the group's first row.  Offsets are brought into [0, rows], and one
 // that falls to the largest before it: whatever they hold, groups do not overlap, no access leaves the operands, and
 // there are no more tiles than the host allowed for.
+// (MOST = 0: no groups.)
+template <int MOST>
 struct GroupMap {
-  int ends[kMostGroups];
-  int starts[kMostGroups + 1];
+  int ends[MOST + 1];
+  int starts[MOST + 1];
 };
 // Filled by the first wave; the caller's barrier publishes it.
-template <int BM>
-__device__ __forceinline__ void map_groups(const ProductArgs& g, GroupMap& map) {
+template <int BM, int MOST>
+__device__ __forceinline__ void map_groups(const ProductArgs& g, GroupMap<MOST>& map) {
   if (threadIdx.x >= 64) return;
   const int lane = (int)threadIdx.x;
   int tiles = 0, furthest = 0;
@@ -73,7 +93,8 @@ __device__ __forceinline__ void map_groups(const ProductArgs& g, GroupMap& map) 
   }
 }
 // The group of tile row t (t < ends[groups - 1]): as many groups end at or before it.  The same in all lanes.
-__device__ __forceinline__ int group_of_tile_row(const GroupMap& map, int groups, int t) {
+template <int MOST>
+__device__ __forceinline__ int group_of_tile_row(const GroupMap<MOST>& map, int groups, int t) {
   int e = 0;
   for (int base = 0; base < groups; base += 64) {
     const int i = base + (int)(threadIdx.x & 63);
@@ -83,8 +104,8 @@ __device__ __forceinline__ int group_of_tile_row(const GroupMap& map, int groups
 }
 
 struct ProductTile {
-  long long row0;  // first row of the tile
-  int rows;        // of its group from there on, at most BM of them are the tile's
+  int row0;  // first row of the tile
+  int rows;  // how many, at most BM
   int group, n0;
 };
 
@@ -111,20 +132,9 @@ __device__ __forceinline__ uint4 load16(const unsigned char* row, int at, int ro
   return v;
 }
 
-// Four consecutive outputs of a row from their sums.  8-bit products: the row's and the column's scale are
-// multiplied first and the product with the (exact) sum is rounded once more; either way three roundings of 2^-24 in all.
-template <typename T>
-__device__ __forceinline__ void store4(const ProductArgs& g, const float (&sum)[4], int group, long long row, int n) {
-  const float xs = T::kInt8 ? g.x_scale[row] : 1.0f;
+// Four consecutive outputs of a row from n on, as many as there are; `v` is scaled and has its bias.
+__device__ __forceinline__ void store4(const ProductArgs& g, float (&v)[4], long long row, int n) {
   const int n4 = g.N - n;
-  float v[4];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const long long c = (long long)group * g.N + (e < n4 ? n + e : n);
-    const float b = g.epilogue != NIMBLE_EPI_NONE ? bf2f(g.bias[c]) : 0.0f;
-    const float s = T::kInt8 ? sum[e] * (xs * g.w_scale[c]) : sum[e];
-    v[e] = s + b;
-  }
   if (g.epilogue == NIMBLE_EPI_BIAS_GELU_ERF) epilogue_of<true>(v);
   const long long at = row * g.N + n;
   if (g.out_f32) {
@@ -132,7 +142,9 @@ __device__ __forceinline__ void store4(const ProductArgs& g, const float (&sum)[
     if (n4 >= 4) {
       __builtin_memcpy(y, v, 16);
     } else {
-      for (int e = 0; e < n4; ++e) y[e] = v[e];
+#pragma unroll
+      for (int e = 0; e < 3; ++e)
+        if (e < n4) y[e] = v[e];
     }
   } else {
     u16* y = (u16*)g.y + at;
@@ -140,25 +152,27 @@ __device__ __forceinline__ void store4(const ProductArgs& g, const float (&sum)[
       const uint2 pk = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
       __builtin_memcpy(y, &pk, 8);
     } else {
-      for (int e = 0; e < n4; ++e) y[e] = f2bf(v[e]);
+#pragma unroll
+      for (int e = 0; e < 3; ++e)
+        if (e < n4) y[e] = f2bf(v[e]);
     }
   }
 }
 
 // The tile at tile row t and tile column tn; false where there is none (fewer tile rows than the host had to allow for).
-template <int BM, int BN, bool GROUPED>
-__device__ __forceinline__ bool find_tile(const ProductArgs& g, const GroupMap* map, int t, int tn, ProductTile& tile) {
+template <int BM, int BN, int MOST>
+__device__ __forceinline__ bool find_tile(const ProductArgs& g, const GroupMap<MOST>& map, int t, int tn, ProductTile& tile) {
+  int first = t * BM, end = (int)g.rows;
   tile.n0 = tn * BN;
   tile.group = 0;
-  tile.row0 = (long long)t * BM;
-  long long end = g.rows;
-  if (GROUPED) {
-    if (t >= map->ends[g.groups - 1]) return false;
-    tile.group = group_of_tile_row(*map, g.groups, t);
-    tile.row0 = map->starts[tile.group] + (long long)(t - (tile.group ? map->ends[tile.group - 1] : 0)) * BM;
-    end = map->starts[tile.group + 1];
+  if (MOST > 0) {
+    if (t >= map.ends[g.groups - 1]) return false;
+    tile.group = group_of_tile_row(map, g.groups, t);
+    first = map.starts[tile.group] + (t - (tile.group ? map.ends[tile.group - 1] : 0)) * BM;
+    end = map.starts[tile.group + 1];
   }
-  tile.rows = (int)min(end - tile.row0, (long long)BM);
+  tile.row0 = __builtin_amdgcn_readfirstlane(first);
+  tile.rows = __builtin_amdgcn_readfirstlane(min(end - first, BM));
   return true;
 }
 
@@ -166,26 +180,25 @@ __device__ __forceinline__ bool find_tile(const ProductArgs& g, const GroupMap* 
 // Any alignment: TM x TN blocks of 16 x 16 per workgroup, KW waves that take pieces of 64 bytes of K in turn, operands from
 // memory straight into the registers that the matrix instruction reads; the waves' sums meet in LDS.
 // ---------------------------------------------------------------------------
-template <typename T, bool GROUPED, int TM, int TN, int KW>
+template <typename T, int GROUPS, int TM, int TN, int KW>
 __global__ void __launch_bounds__(KW * 64) product_direct_kernel(ProductArgs g, unsigned tiles, unsigned tiles_n) {
   constexpr int BM = 16 * TM, BN = 16 * TN;
   typedef typename T::Acc Acc;
-  __shared__ typename std::conditional<GROUPED, GroupMap, int>::type map_[1];
-  const GroupMap* map = (const GroupMap*)map_;
+  __shared__ GroupMap<GROUPS> map;
   __shared__ __attribute__((aligned(16))) Acc sums[KW][TM * TN * 64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int fr_row = lane & 15, fr_at = (lane >> 4) * 16;
-  if (GROUPED) {
-    map_groups<BM>(g, (GroupMap&)map_[0]);
+  if (GROUPS) {
+    map_groups<BM>(g, map);
     __syncthreads();
   }
   for (unsigned b = blockIdx.x; b < tiles; b += gridDim.x) {
     ProductTile tile;
     const unsigned t = b / tiles_n;
-    if (!find_tile<BM, BN, GROUPED>(g, map, (int)t, (int)(b - t * tiles_n), tile)) return;
+    if (!find_tile<BM, BN>(g, map, (int)t, (int)(b - t * tiles_n), tile)) return;
     const unsigned char *xp[TM], *wp[TN];
 #pragma unroll
-    for (int j = 0; j < TM; ++j) xp[j] = g.x + (tile.row0 + min(16 * j + fr_row, tile.rows - 1)) * g.row_bytes;
+    for (int j = 0; j < TM; ++j) xp[j] = g.x + ((long long)tile.row0 + min(16 * j + fr_row, tile.rows - 1)) * g.row_bytes;
 #pragma unroll
     for (int i = 0; i < TN; ++i) wp[i] = g.w + ((long long)tile.group * g.N + min(tile.n0 + 16 * i + fr_row, g.N - 1)) * g.row_bytes;
     Acc acc[TN][TM];
@@ -228,8 +241,16 @@ __global__ void __launch_bounds__(KW * 64) product_direct_kernel(ProductArgs g, 
       const int l = o & 63, block = o >> 6, i = block / TM, j = block % TM;
       const int r = 16 * j + (l & 15), n = tile.n0 + 16 * i + 4 * (l >> 4);
       if (r >= tile.rows || n >= g.N) continue;
-      const float v[4] = {(float)s[0], (float)s[1], (float)s[2], (float)s[3]};
-      store4<T>(g, v, tile.group, tile.row0 + r, n);
+      const long long row = (long long)tile.row0 + r;
+      const float xs = T::kInt8 ? g.x_scale[row] : 1.0f;
+      float v[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const long long c = (long long)tile.group * g.N + min(n + e, g.N - 1);
+        const float bias = g.epilogue != NIMBLE_EPI_NONE ? bf2f(g.bias[c]) : 0.0f;
+        v[e] = T::kInt8 ? fmaf((float)s[e], xs * g.w_scale[c], bias) : (float)s[e] + bias;
+      }
+      store4(g, v, row, n);
     }
   }
 }

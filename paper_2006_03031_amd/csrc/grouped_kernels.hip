@@ -1,7 +1,9 @@
 // Device entry points and launchers of the 8-bit and the grouped products.
-//   quantize_kernel.h   quantize_rows_kernel<F32,WAVES,NV>: rows to 8-bit codes and a scale each.
-//   grouped_kernel.h    the map from workgroups to the tiles of groups that only the device knows, the epilogue, and
-//       product_direct_kernel<T,GROUPED,TM,TN,KW>: operands of any alignment.
+//   quantize_kernel.h        quantize_rows_kernel: rows to 8-bit codes and a scale each.
+//   grouped_kernel.h         the map from workgroups to the tiles of groups that only the device knows, loads through buffer descriptors,
+//       and product_direct_kernel: operands of any alignment.
+//   product_stream_kernel.h  product_stream_kernel: small tiles, K divided among a workgroup's waves.
+//   product_tile_kernel.h    product_tile_kernel: large tiles by four waves, a tile's end computed during the next one.
 #include <hip/hip_runtime.h>
 
 #include "grouped_internal.h"
@@ -16,15 +18,9 @@ static int check_hip(hipError_t e, const char* what) {
 }
 static bool misaligned(const void* p, unsigned to = 16) { return ((uintptr_t)p & (to - 1)) != 0; }
 
-template <typename T, bool GROUPED>
-static int launch_product(const ProductArgs& g, const nimble_product_plan& p, hipStream_t stream) {
-  const unsigned tiles = (unsigned)p.tiles, tiles_n = (unsigned)((g.N + p.bn - 1) / p.bn);
-  if (p.bm == 16)
-    hipLaunchKernelGGL((product_direct_kernel<T, GROUPED, 1, 1, 8>), dim3(p.grid), dim3(p.block), 0, stream, g, tiles, tiles_n);
-  else
-    hipLaunchKernelGGL((product_direct_kernel<T, GROUPED, 4, 4, 4>), dim3(p.grid), dim3(p.block), 0, stream, g, tiles, tiles_n);
-  return check_hip(hipGetLastError(), "product kernel launch");
-}
+// (product_launch.h; built in product_bf16_grouped.hip, product_i8_grouped.hip and product_i8.hip)
+template <typename T, int GROUPS>
+int launch_product(const ProductArgs& g, const nimble_product_plan& p, hipStream_t stream);
 
 // What the three products have in common behind their checks of types and extents.
 static int run_product(ProductArgs g, int64_t R, int64_t E, int64_t N, int64_t K, bool grouped, bool int8, hipStream_t stream) {
@@ -45,8 +41,8 @@ static int run_product(ProductArgs g, int64_t R, int64_t E, int64_t N, int64_t K
   g.N = (int)N;
   g.row_bytes = (int)(int8 ? K : 2 * K);
   if (g.epilogue == NIMBLE_EPI_NONE) g.bias = nullptr;
-  if (!int8) return launch_product<OfBf16, true>(g, p, stream);
-  return grouped ? launch_product<OfInt8, true>(g, p, stream) : launch_product<OfInt8, false>(g, p, stream);
+  if (!int8) return launch_product<OfBf16, kMostGroups>(g, p, stream);
+  return grouped ? launch_product<OfInt8, kMostGroups>(g, p, stream) : launch_product<OfInt8, 0>(g, p, stream);
 }
 
 }  // namespace nimble

@@ -1,0 +1,49 @@
+// The launcher of a product's kernels; each file that includes this builds those of one type.
+#ifndef NIMBLE_PRODUCT_LAUNCH_H_
+#define NIMBLE_PRODUCT_LAUNCH_H_
+#include <hip/hip_runtime.h>
+
+#include "grouped_kernel.h"
+#include "product_stream_kernel.h"
+#include "product_tile_kernel.h"
+
+namespace nimble {
+
+static int launched(const char* what) {
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? NIMBLE_OK : fail(NIMBLE_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
+}
+
+template <typename T, int GROUPS>
+int launch_product(const ProductArgs& g, const nimble_product_plan& p, hipStream_t stream) {
+  const unsigned tiles = (unsigned)p.tiles, tiles_n = (unsigned)((g.N + p.bn - 1) / p.bn);
+  const dim3 grid(p.grid), block(p.block);
+  if (p.kernel == NIMBLE_PRODUCT_TILES) {
+    const int tiles_m = (int)(p.tiles / tiles_n), group_m = 8;
+    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, g, tiles_m, (int)tiles_n, group_m); };
+    const bool gelu = g.epilogue == NIMBLE_EPI_BIAS_GELU_ERF;
+    if (g.out_f32) {
+      if (gelu) launch(product_tile_kernel<T, GROUPS, true, true, 128, 256, 3>);
+      else launch(product_tile_kernel<T, GROUPS, true, false, 128, 256, 3>);
+    } else {
+      if (gelu) launch(product_tile_kernel<T, GROUPS, false, true, 128, 256, 3>);
+      else launch(product_tile_kernel<T, GROUPS, false, false, 128, 256, 3>);
+    }
+    return launched("product tile kernel launch");
+  }
+  if (p.kernel == NIMBLE_PRODUCT_STREAM) {
+    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, g, tiles, tiles_n); };
+    if (p.bm == 16) launch(product_stream_kernel<T, GROUPS, 1, 1, 4, 4>);
+    else if (p.bm == 32) launch(product_stream_kernel<T, GROUPS, 2, 2, 4, 3>);
+    else launch(product_stream_kernel<T, GROUPS, 4, 4, 4, 2>);
+    return launched("product stream kernel launch");
+  }
+  if (p.bm == 16)
+    hipLaunchKernelGGL((product_direct_kernel<T, GROUPS, 1, 1, 8>), grid, block, 0, stream, g, tiles, tiles_n);
+  else
+    hipLaunchKernelGGL((product_direct_kernel<T, GROUPS, 4, 4, 4>), grid, block, 0, stream, g, tiles, tiles_n);
+  return launched("product kernel launch");
+}
+
+}  // namespace nimble
+#endif

@@ -1,0 +1,448 @@
+// The 8-bit and the grouped products in large tiles by four waves.
+#ifndef NIMBLE_PRODUCT_TILE_KERNEL_H_
+#define NIMBLE_PRODUCT_TILE_KERNEL_H_
+#include "grouped_kernel.h"
+
+namespace nimble {
+
+// ---------------------------------------------------------------------------
+// Tiles of BM x BN by four waves in two rows and two columns, one wave per SIMD, one tile after the other: a ring of S stages
+// of 128 bytes of K in LDS, each stage multiplied in four quarters, the fragments that the next quarter needs read and the
+// stage S ahead loaded in between its MFMAs (the schedule of gemm_quarter_kernel.h).  A stage of 128 bytes takes the matrix cores the
+// same time in either type: 64 k of bf16, 128 k of int8.
+//   The end of a tile is computed during the next one.  With K = 1024 a tile is 8 (int8) or 16 stages, and scales, bias, GELU and stores
+// of its outputs took as long again, the matrix cores idle and all workgroups storing at once.  So a tile's sums are moved aside by the
+// first products of the next (which start from zero), and one to three blocks of 16 x 32 outputs are finished in each of the stages
+// behind, a step of eight instructions between two MFMAs, which leave three issue slots in four free.
+//   Columns go to the matrix instruction's rows such that a lane holds eight neighbouring ones of bf16 (four of f32): 16 bytes, 64
+// contiguous ones with its three neighbours, stored from registers as they are.  The swizzle of the weights' rows in LDS
+// follows (see b_swizzle).
+//   Loads go through buffer descriptors that end with the tile's last row (of its group, of the weight): rows past it, which
+// belong to another group or to nobody, come back as zeros, and so does, by an offset past every descriptor, what lies behind
+// the end of K in the last stage.  Stores past the last row or column are dropped in the same way.  So every tile runs the same code
+// whatever its number of rows.
+//   Tiles are told from the offsets of the groups (GroupMap), which the workgroup reads once.  The loads past a tile's last
+// stage are the next tile's first ones.
+// ---------------------------------------------------------------------------
+#define NIMBLE_INLINE __attribute__((always_inline))
+template <int N>
+using Int = std::integral_constant<int, N>;
+// f(Int<FROM>{}), f(Int<FROM + 1>{}), ... up to TO: indexes that are constants for the compiler from the start, since
+// the sums have to stay in registers that they name.
+template <int FROM, int TO, typename F>
+__device__ __forceinline__ void each(F&& f) {
+  if constexpr (FROM < TO) {
+    f(Int<FROM>{});
+    each<FROM + 1, TO>(f);
+  }
+}
+
+// 16 bytes per lane to the descriptor's byte voff + soff, through the L2 (see store_through); past its end nothing.
+__device__ __forceinline__ void store16_buffer(uint4 v, uint32_t voff, rsrc_t rsrc, uint32_t soff) {
+  asm volatile("buffer_store_dwordx4 %0, %1, %2, %3 offen sc1\n\ts_nop 1" ::"v"(__builtin_bit_cast(i32x4, v)), "v"(voff),
+               "s"(rsrc), "s"(soff)
+               : "memory");
+}
+
+// The matrix instruction as a volatile statement (see mfma_acc): C is the sum or, for a tile's first, zero; with a load
+// behind it; with the wait states that let the sums be read (`last`).
+#define NIMBLE_PRODUCT_MFMA(T, INSN)                                                                                          \
+  template <bool ZERO>                                                                                                        \
+  __device__ __forceinline__ void mfma_in_place(T::Acc& acc, const uint4& a, const uint4& b) {                                \
+    if (ZERO)                                                                                                                 \
+      asm volatile(INSN " %0, %1, %2, 0" : "+a"(acc) : "v"(__builtin_bit_cast(i32x4, a)), "v"(__builtin_bit_cast(i32x4, b))); \
+    else                                                                                                                      \
+      asm volatile(INSN " %0, %1, %2, %0" : "+a"(acc) : "v"(__builtin_bit_cast(i32x4, a)), "v"(__builtin_bit_cast(i32x4, b))); \
+  }                                                                                                                           \
+  __device__ __forceinline__ void mfma_in_place_last(T::Acc& acc, const uint4& a, const uint4& b, int last) {                 \
+    asm volatile(INSN                                                                                                         \
+                 " %0, %1, %2, %0\n\t"                                                                                        \
+                 "s_cmp_eq_u32 %3, 0\n\t"                                                                                     \
+                 "s_cbranch_scc1 .Lnimble_product_done_%=\n\t"                                                                \
+                 "s_nop 15\n\t"                                                                                               \
+                 "s_nop 15\n"                                                                                                 \
+                 ".Lnimble_product_done_%=:"                                                                                  \
+                 : "+a"(acc)                                                                                                  \
+                 : "v"(__builtin_bit_cast(i32x4, a)), "v"(__builtin_bit_cast(i32x4, b)),                                      \
+                   "s"(__builtin_amdgcn_readfirstlane(last))                                                                  \
+                 : "scc");                                                                                                    \
+  }                                                                                                                           \
+  template <bool ZERO>                                                                                                        \
+  __device__ __forceinline__ void mfma_in_place_load(T::Acc& acc, const uint4& a, const uint4& b, uint32_t voff, rsrc_t rsrc,  \
+                                                     uint32_t soff, uint32_t lds_base, uint32_t lds_off) {                    \
+    if (ZERO)                                                                                                                 \
+      asm volatile("s_add_u32 m0, %6, %7\n\t" INSN                                                                            \
+                   " %0, %1, %2, 0\n\t"                                                                                       \
+                   "buffer_load_dwordx4 %3, %4, %5 offen lds"                                                                 \
+                   : "+a"(acc)                                                                                                \
+                   : "v"(__builtin_bit_cast(i32x4, a)), "v"(__builtin_bit_cast(i32x4, b)), "v"(voff), "s"(rsrc), "s"(soff),   \
+                     "s"(lds_base), "s"(lds_off)                                                                              \
+                   : "memory", "m0", "scc");                                                                                  \
+    else                                                                                                                      \
+      asm volatile("s_add_u32 m0, %6, %7\n\t" INSN                                                                            \
+                   " %0, %1, %2, %0\n\t"                                                                                      \
+                   "buffer_load_dwordx4 %3, %4, %5 offen lds"                                                                 \
+                   : "+a"(acc)                                                                                                \
+                   : "v"(__builtin_bit_cast(i32x4, a)), "v"(__builtin_bit_cast(i32x4, b)), "v"(voff), "s"(rsrc), "s"(soff),   \
+                     "s"(lds_base), "s"(lds_off)                                                                              \
+                   : "memory", "m0", "scc");                                                                                  \
+  }
+NIMBLE_PRODUCT_MFMA(OfBf16, "v_mfma_f32_16x16x32_bf16")
+NIMBLE_PRODUCT_MFMA(OfInt8, "v_mfma_i32_16x16x64_i8")
+#undef NIMBLE_PRODUCT_MFMA
+
+// (A statement: as an ordinary copy the compiler would let either stand for both, and move 128 registers back in every stage.)
+template <typename Acc>
+__device__ __forceinline__ void copy_sums(int32_t (&to)[4], const Acc& from) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const auto one = from[k];
+    asm volatile("v_accvgpr_mov_b32 %0, %1" : "=a"(to[k]) : "a"(one));
+  }
+}
+
+__device__ __forceinline__ float read_sum(const int32_t& sum) {
+  float v;
+  asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v) : "a"(sum));
+  return v;
+}
+
+// Bias (bf16), column scales and row scales of a tile, in LDS.
+template <int BM, int BN>
+struct TileValues {
+  float w_scale[BN], x_scale[BM];
+  u16 bias[BN];
+};
+template <int BM, int BN, int S>
+constexpr int kProductTileBytes = S * (BM + BN) * 128 + 2 * (int)sizeof(TileValues<BM, BN>);
+
+template <typename T, int GROUPS, bool OUT_F32, bool GELU, int BM, int BN, int S>
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1)))
+    product_tile_kernel(ProductArgs g, int tiles_m, int tiles_n, int group_m) {
+  constexpr int WM = BM / 2, WN = BN / 2;
+  constexpr int TM = WM / 16, TN = WN / 16;
+  constexpr int H0 = (TM + 1) / 2, H1 = TM - H0;  // 16-row tiles in the two halves of a wave's rows
+  constexpr int G = TN / 2;                       // 16-column tiles in either half of its columns
+  static_assert(BM % 32 == 0 && H1 >= 1 && BN % 128 == 0, "whole 16 x 16 tiles in either half of a wave's rows and columns");
+  static_assert(kProductTileBytes<BM, BN, S> + (GROUPS ? (int)sizeof(GroupMap<GROUPS>) : 0) <= 160 * 1024, "LDS");
+  constexpr int SLOT = (BM + BN) * 128;  // bytes
+  constexpr int LDT = TM + TN;           // loads per wave and stage: H0, G, G, H1 of 32 rows each
+  constexpr int FLIGHT = (S - 1) * LDT;  // loads that may be in flight at a barrier
+  static_assert(FLIGHT + G + H1 <= 63, "the wait counter holds 63");
+  constexpr int MFMAS = 2 * TM * TN;     // of a stage
+  constexpr int UNITS = TM * TN / 2;     // blocks of 16 rows and 32 columns
+  constexpr int PARTS = 7;               // stages over which they are finished
+  constexpr int OPS = (T::kInt8 ? 4 : 2) + (GELU ? 7 : 0), STEPS = 2 * OPS + 1;  // of a block, see unit_step
+  constexpr int OS = OUT_F32 ? 4 : 2;
+  typedef TileValues<BM, BN> Values;
+  typedef typename T::Acc Acc;
+  __shared__ __attribute__((aligned(16))) unsigned char smem[kProductTileBytes<BM, BN, S>];
+  __shared__ GroupMap<GROUPS> map;
+  if (GROUPS) {
+    map_groups<BM>(g, map);
+    __syncthreads();
+    tiles_m = __builtin_amdgcn_readfirstlane(map.ends[g.groups - 1]);
+  }
+  const int tiles_total = tiles_m * tiles_n;
+  if ((int)blockIdx.x >= tiles_total) return;
+  auto tile_at = [&](int t, ProductTile& tile) {
+    int tm, tn;
+    tile_of_block(t, tiles_total, tiles_m, tiles_n, group_m, tm, tn);
+    find_tile<BM, BN>(g, map, tm, tn, tile);
+  };
+
+  const int KS = (g.row_bytes + 127) >> 7;
+  const int tid = threadIdx.x;
+  const int lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave >> 1, wn = wave & 1;
+
+  // row of the tile behind row q of half h of A (the halves of both rows of waves), the same for B
+  auto a_row = [](int h, int q) {
+    const int n = 16 * (h ? H1 : H0);
+    return h * 16 * H0 + (q >= n ? WM - n : 0) + q;
+  };
+  auto b_row = [](int h, int q) { return h * 16 * G + (q >= 16 * G ? WN - 16 * G : 0) + q; };
+  // Chunk c of row r lies at c ^ swizzle(r).  A fragment read takes 16 rows and is free of bank conflicts where each value of
+  // the swizzle comes twice: of A, and of B for f32, 16 rows in a row; of B for bf16 rows 8 a + 4 x + b of 32, a, b < 4.
+  auto a_swizzle = [](int r) { return (r >> 1) & 7; };
+  auto b_swizzle = [](int r) { return OUT_F32 ? (r >> 1) & 7 : ((r >> 1) & 1) | ((r >> 2) & 6); };
+  // loads of a stage in the order in which they are needed: H0 of A, G of B, G of B, H1 of A.  Offset of the lane, and
+  // where in a slot the wave's 8 rows go.
+  const int ld_row = tid >> 3;
+  const int ld_a = (tid & 7) ^ a_swizzle(ld_row), ld_b = (tid & 7) ^ b_swizzle(ld_row);  // (the passes are 32 rows apart)
+  uint32_t off[LDT], lds_off[LDT];
+  auto of_a = [](int u) { return u < H0 || u >= H0 + TN; };
+  auto row_of = [&](int u, int q) {
+    const int h = of_a(u) ? u >= H0 : u >= H0 + G, base = of_a(u) ? (h ? u - TN - H0 : u) * 32 : (u - H0 - G * h) * 32;
+    return of_a(u) ? a_row(h, base + q) : b_row(h, base + q);
+  };
+  auto set_off = [&] {
+#pragma unroll
+    for (int u = 0; u < LDT; ++u) off[u] = (uint32_t)(row_of(u, ld_row) * g.row_bytes + (of_a(u) ? ld_a : ld_b) * 16);
+  };
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_addr_of(smem));
+#pragma unroll
+  for (int u = 0; u < LDT; ++u) lds_off[u] = (of_a(u) ? 0 : BM * 128) + row_of(u, wave * 8) * 128;
+  set_off();
+  auto a_desc = [&](const ProductTile& t) {
+    return descriptor(g.x + (long long)t.row0 * g.row_bytes, (uint32_t)t.rows * (uint32_t)g.row_bytes);
+  };
+  auto b_desc = [&](const ProductTile& t) {
+    return descriptor(g.w + ((long long)t.group * g.N + t.n0) * g.row_bytes, (uint32_t)min(BN, g.N - t.n0) * (uint32_t)g.row_bytes);
+  };
+  rsrc_t a_src, b_src;
+  uint32_t at = 0;
+  auto src = [&](int u) NIMBLE_INLINE { return of_a(u) ? a_src : b_src; };
+
+  const int fr_row = lane & 15, fr_q = lane >> 4;
+  // row of B that is row r of the matrix instruction's tile i
+  auto b_tile_row = [](int i, int r) { return OUT_F32 ? 16 * i + r : 32 * (i >> 1) + 8 * (r >> 2) + 4 * (i & 1) + (r & 3); };
+  const int a_phys = fr_q ^ a_swizzle(fr_row), b_phys = fr_q ^ b_swizzle(b_tile_row(0, fr_row));
+  const int a_half = (a_phys ^ 4) - a_phys, b_half = (b_phys ^ 4) - b_phys;
+  const uint4* a_rd = (const uint4*)smem + (wm * WM + fr_row) * 8 + a_phys;
+  const uint4* b_rd = (const uint4*)smem + (BM + wn * WN + b_tile_row(0, fr_row)) * 8 + b_phys;
+  // rows of tile i behind those of tile 0 (the swizzle is the same: whole 16 rows, or 4 of which it does not depend on bit 2)
+  auto b_step = [](int i) { return (OUT_F32 ? 16 * i : 32 * (i >> 1) + 4 * (i & 1)) * 8; };
+
+  Acc acc[TN][TM];          // this tile's sums
+  int32_t done[TN][TM][4];  // the last one's
+  auto put_aside = [&](auto i, auto j) NIMBLE_INLINE { copy_sums<Acc>(done[decltype(i)::value][decltype(j)::value], acc[decltype(i)::value][decltype(j)::value]); };
+
+  Values* const values = (Values*)(smem + S * SLOT);
+  // 4 bytes per lane; past the end of the row or of the tile's rows nothing is needed, and zeros come
+  auto fetch_values = [&](const ProductTile& t, const Values* to) {
+    const long long c0 = (long long)t.group * g.N + t.n0;
+    const int columns = min(BN, g.N - t.n0);
+    if (g.epilogue != NIMBLE_EPI_NONE && wave < BN / 128)
+      dma4_buffer((uint32_t)(wave * 256 + lane * 4), descriptor((const u16*)g.bias + c0, (uint32_t)columns * 2u),
+                  __builtin_amdgcn_readfirstlane(lds_addr_of(to->bias)) + wave * 256);
+    if (T::kInt8) {
+      if (wave < BN / 64)
+        dma4_buffer((uint32_t)(wave * 256 + lane * 4), descriptor(g.w_scale + c0, (uint32_t)columns * 4u),
+                    __builtin_amdgcn_readfirstlane(lds_addr_of(to->w_scale)) + wave * 256);
+      if (wave < BM / 64)
+        dma4_buffer((uint32_t)(wave * 256 + lane * 4), descriptor(g.x_scale + t.row0, (uint32_t)t.rows * 4u),
+                    __builtin_amdgcn_readfirstlane(lds_addr_of(to->x_scale)) + wave * 256);
+    }
+  };
+
+  // ---- the end of a tile, in blocks of two 16-column tiles 2 p, 2 p + 1 of 16 rows j, p first.  A lane's eight values are
+  // columns 8 fr_q .. + 7 of the 32 (bf16), or 4 fr_q .. + 3 of either 16 (f32), of row fr_row.
+  ProductTile from;                     // whose sums are in `done`
+  const Values* from_values = values;
+  rsrc_t out;
+  const uint32_t out_row = (uint32_t)g.N * OS * 16;  // 16 rows
+  const int out_col = OUT_F32 ? 4 * fr_q : 8 * fr_q;  // first column of a lane within its 32
+  const uint32_t out_off = (uint32_t)((wm * WM + fr_row) * g.N + wn * WN + out_col) * OS;
+  float v[8], e[8], t4[4], ws[8], bs[8], xs[TM];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) v[k] = e[k] = 0.0f;
+  auto column = [&](int p, int k) { return wn * WN + 32 * p + out_col + (OUT_F32 ? 16 * (k >> 2) + (k & 3) : k); };
+  auto read_rows = [&] {
+#pragma unroll
+    for (int j = 0; j < TM; ++j) xs[j] = T::kInt8 ? from_values->x_scale[wm * WM + j * 16 + fr_row] : 1.0f;
+  };
+  auto read_columns = [&](int p) NIMBLE_INLINE {
+#pragma unroll
+    for (int k = 0; k < 8; k += 4) {
+      const int c = column(p, k);
+      if (T::kInt8) {
+        const float4 w4 = *(const float4*)(from_values->w_scale + c);
+        ws[k] = w4.x, ws[k + 1] = w4.y, ws[k + 2] = w4.z, ws[k + 3] = w4.w;
+      }
+      const uint2 bb = *(const uint2*)(from_values->bias + c);
+      bs[k] = bf2f((u16)(bb.x & 0xffff)), bs[k + 1] = bf2f((u16)(bb.x >> 16));
+      bs[k + 2] = bf2f((u16)(bb.y & 0xffff)), bs[k + 3] = bf2f((u16)(bb.y >> 16));
+    }
+    if (g.epilogue == NIMBLE_EPI_NONE) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) bs[k] = 0.0f;
+    }
+  };
+  // Step n of a block: an operation on four values of the eight; the last one stores.  What a step leaves goes through an
+  // empty statement, which holds it to its place between the products.
+  auto unit_step = [&](auto unit_tag, auto n_tag) NIMBLE_INLINE {
+    constexpr int p = decltype(unit_tag)::value / TM, j = decltype(unit_tag)::value % TM, n = decltype(n_tag)::value;
+    if constexpr (n == STEPS - 1) {
+      const uint32_t c = (uint32_t)(from.n0 + wn * WN + 32 * p + out_col);
+      if constexpr (OUT_F32) {
+        each<0, 2>([&](auto x_tag) NIMBLE_INLINE {
+          constexpr int x = decltype(x_tag)::value;
+          store16_buffer(__builtin_bit_cast(uint4, make_float4(v[4 * x], v[4 * x + 1], v[4 * x + 2], v[4 * x + 3])),
+                         c + 16 * x < (uint32_t)g.N ? out_off + (32 * p + 16 * x) * OS : 0x80000000u, out, j * out_row);
+        });
+      } else {
+        store16_buffer(make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])),
+                       c < (uint32_t)g.N ? out_off + 32 * p * OS : 0x80000000u, out, j * out_row);
+      }
+    } else {
+      // the operation, those of bf16 and the GELU numbered as if all were there
+      constexpr int o = n / 2, op = T::kInt8 || o == 0 ? o : o + 2;
+      if constexpr (n == 0 && j == 0) read_columns(p);
+#pragma unroll
+      for (int k = n % 2 * 4; k < n % 2 * 4 + 4; ++k) {
+        if constexpr (op == 0) v[k] = read_sum(done[2 * p + (k >> 2)][j][k & 3]);
+        if constexpr (op == 1) v[k] = (float)__float_as_int(v[k]);
+        if constexpr (op == 2) e[k] = xs[j] * ws[k];
+        if constexpr (op == 3) v[k] = T::kInt8 ? fmaf(v[k], e[k], bs[k]) : v[k] + bs[k];
+        // the GELU of epilogue_of: v sigmoid(v (a + b t + c t^2)), t = min(v^2, 81)
+        if constexpr (op == 4) e[k] = v[k] * v[k];
+        if constexpr (op == 5) t4[k & 3] = fminf(e[k], 81.0f), e[k] = fmaf(0.0010142630f, t4[k & 3], -0.10677572f), e[k] = fmaf(e[k], t4[k & 3], -2.3011212f);
+        if constexpr (op == 6) e[k] = e[k] * v[k];
+        if constexpr (op == 7) e[k] = __builtin_amdgcn_exp2f(e[k]);
+        if constexpr (op == 8) e[k] = 1.0f + e[k];
+        if constexpr (op == 9) e[k] = __builtin_amdgcn_rcpf(e[k]);
+        if constexpr (op == 10) v[k] *= e[k];
+        if constexpr (op != 0) asm volatile("" : "+v"(v[k]), "+v"(e[k]));
+      }
+    }
+  };
+  // All blocks at once.
+  auto run_units = [&]() NIMBLE_INLINE {
+    each<0, UNITS>([&](auto u) NIMBLE_INLINE { each<0, STEPS>([&](auto n) NIMBLE_INLINE { unit_step(u, n); }); });
+  };
+  // `t` becomes the tile whose end is to be computed, its values in slot `parity`
+  auto end_of = [&](const ProductTile& t, int parity) {
+    from = t;
+    from_values = values + parity;
+    out = descriptor((unsigned char*)g.y + ((long long)t.row0 * g.N + t.n0) * OS,
+                     (uint32_t)((t.rows - 1) * g.N + min(BN, g.N - t.n0)) * OS);
+    read_rows();
+  };
+
+  // ---- the walk
+  ProductTile tile, next_tile;
+  tile_at(blockIdx.x, tile);
+  a_src = a_desc(tile);
+  b_src = b_desc(tile);
+  fetch_values(tile, values);
+#pragma unroll
+  for (int s = 0; s < S; ++s) {
+#pragma unroll
+    for (int u = 0; u < LDT; ++u) dma16_buffer(off[u], src(u), s * 128, lds0 + s * SLOT + lds_off[u]);
+  }
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(FLIGHT + G + H1) : "memory");
+  __syncthreads();
+
+  uint4 xa0[H0][2], xa1[H1][2], wb0[G][2], wb1[G][2];  // [tile][k half]
+  auto rd_a0 = [&](int s, int x) NIMBLE_INLINE { xa0[x % H0][x / H0] = a_rd[s * (SLOT / 16) + (x % H0) * 128 + (x / H0) * a_half]; };
+  auto rd_a1 = [&](int s, int x) NIMBLE_INLINE { xa1[x % H1][x / H1] = a_rd[s * (SLOT / 16) + (H0 + x % H1) * 128 + (x / H1) * a_half]; };
+  auto rd_b0 = [&](int s, int x) NIMBLE_INLINE { wb0[x % G][x / G] = b_rd[s * (SLOT / 16) + b_step(x % G) + (x / G) * b_half]; };
+  auto rd_b1 = [&](int s, int x) NIMBLE_INLINE { wb1[x % G][x / G] = b_rd[s * (SLOT / 16) + b_step(G + x % G) + (x / G) * b_half]; };
+#pragma unroll
+  for (int x = 0; x < 2 * H0; ++x) rd_a0(0, x);
+#pragma unroll
+  for (int x = 0; x < TN; ++x) rd_b0(0, x);
+
+  // S - 1 whole stages may be in flight (stores in between count as loads: the wait is for a little more then)
+  auto sync = [&] {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(FLIGHT) : "memory");
+    __syncthreads();
+  };
+  // One stage.  FIRST: of a tile, its products start from zero and the sums move over to `done`.  PART < PARTS: with that part
+  // of the last tile's end.
+  auto stage = [&](auto first_tag, auto part_tag, int slot, int next, int last) NIMBLE_INLINE {
+    constexpr bool FIRST = decltype(first_tag)::value;
+    constexpr int PART = decltype(part_tag)::value;
+    constexpr int U0 = PART * UNITS / PARTS, U1 = PART < PARTS ? (PART + 1) * UNITS / PARTS : U0;
+    constexpr int NSTEPS = (U1 - U0) * STEPS;
+    const uint32_t dst = lds0 + slot * SLOT;
+    // TH x G tiles over the stage's 128 bytes, from the stage's product number n0 on; in between `nrd` fragment reads, then the
+    // loads u0 ... u0 + nld - 1
+    auto quarter = [&](auto& x, auto& w, auto th_tag, auto j0_tag, auto i0_tag, auto n0_tag, auto rd, auto nrd_tag, auto u0_tag,
+                       auto nld_tag) NIMBLE_INLINE {
+      constexpr int TH = decltype(th_tag)::value, N = 2 * G * TH, j0 = decltype(j0_tag)::value, i0 = decltype(i0_tag)::value;
+      constexpr int n0 = decltype(n0_tag)::value, nrd = decltype(nrd_tag)::value, u0 = decltype(u0_tag)::value;
+      constexpr int nops = nrd + decltype(nld_tag)::value;
+      each<0, N>([&](auto n_tag) NIMBLE_INLINE {
+        constexpr int n = decltype(n_tag)::value, kh = n / (G * TH), i = n / TH % G, j = i & 1 ? TH - 1 - n % TH : n % TH;
+        constexpr bool zero = FIRST && kh == 0;
+        Acc& sum = acc[i0 + i][j0 + j];
+        if constexpr (zero) put_aside(Int<i0 + i>{}, Int<j0 + j>{});
+        constexpr int m0 = (n * nops + N - 1) / N, m1 = ((n + 1) * nops + N - 1) / N;
+        constexpr int load0 = m0 > nrd ? m0 : nrd;  // loads of this gap: the last one goes behind the MFMA
+        each<m0, (m1 < nrd ? m1 : nrd)>([&](auto m) NIMBLE_INLINE {
+          rd(m);
+          asm volatile("" ::: "memory");
+        });
+        constexpr int u = m1 > load0 && n0 + n != MFMAS - 1 ? u0 + m1 - 1 - nrd : -1;
+        each<load0, (u >= 0 ? m1 - 1 : m1)>([&](auto m) NIMBLE_INLINE {
+          constexpr int l = u0 + decltype(m)::value - nrd;
+          dma16_buffer(off[l], src(l), at, dst + lds_off[l]);
+        });
+        if constexpr (n0 + n == MFMAS - 1)
+          mfma_in_place_last(sum, w[i][kh], x[j][kh], last);
+        else if constexpr (u >= 0)
+          mfma_in_place_load<zero>(sum, w[i][kh], x[j][kh], off[u], src(u), at, dst, lds_off[u]);
+        else
+          mfma_in_place<zero>(sum, w[i][kh], x[j][kh]);
+        if constexpr (NSTEPS > 0)
+          each<(n0 + n) * NSTEPS / MFMAS, (n0 + n + 1) * NSTEPS / MFMAS>([&](auto m) NIMBLE_INLINE {
+            unit_step(Int<U0 + decltype(m)::value / STEPS>{}, Int<decltype(m)::value % STEPS>{});
+          });
+      });
+    };
+    sync();
+    quarter(xa0, wb0, Int<H0>{}, Int<0>{}, Int<0>{}, Int<0>{}, [&](int m) NIMBLE_INLINE { rd_b1(slot, m); }, Int<TN>{}, Int<0>{}, Int<H0>{});
+    quarter(xa0, wb1, Int<H0>{}, Int<0>{}, Int<G>{}, Int<2 * G * H0>{}, [&](int m) NIMBLE_INLINE { rd_a1(slot, m); }, Int<2 * H1>{}, Int<H0>{},
+            Int<G>{});
+    sync();
+    quarter(xa1, wb0, Int<H1>{}, Int<H0>{}, Int<0>{}, Int<4 * G * H0>{}, [&](int m) NIMBLE_INLINE { rd_a0(next, m); }, Int<2 * H0>{},
+            Int<H0 + G>{}, Int<G>{});
+    quarter(xa1, wb1, Int<H1>{}, Int<H0>{}, Int<G>{}, Int<4 * G * H0 + 2 * G * H1>{}, [&](int m) NIMBLE_INLINE { rd_b0(next, m); }, Int<TN>{},
+            Int<H0 + TN>{}, Int<H1>{});
+  };
+  using No = std::false_type;
+  at = S * 128;
+  int slot = 0, parity = 0;
+  bool pending = false;  // `done` holds the sums of the tile before
+  const int left = g.row_bytes - (KS - 1) * 128;  // bytes of the last stage
+  for (int t = blockIdx.x;; t += gridDim.x) {
+    const bool follows = t + (int)gridDim.x < tiles_total;
+    // Stage ks loads stage ks + S of this tile: of its last one the pieces past the end of K are zeros; behind it come the next
+    // tile's first ones (there is none: nothing is read).
+    auto run_stage = [&](int ks, auto first_tag, auto part_tag) NIMBLE_INLINE {
+      if (ks == KS - S - 1 && left < 128) {
+#pragma unroll
+        for (int u = 0; u < LDT; ++u) off[u] = (of_a(u) ? ld_a : ld_b) * 16 < left ? off[u] : 0x80000000u;
+      }
+      if (ks == KS - S) {
+        at = 0;
+        if (left < 128) set_off();
+        a_src = b_src = descriptor(g.x, 0);
+        if (follows) {
+          tile_at(t + (int)gridDim.x, next_tile);
+          a_src = a_desc(next_tile);
+          b_src = b_desc(next_tile);
+        }
+      }
+      const int next = slot + 1 == S ? 0 : slot + 1;
+      stage(first_tag, part_tag, slot, next, ks + 1 >= KS);
+      slot = next;
+      at += 128;
+    };
+    run_stage(0, std::true_type{}, Int<PARTS>{});
+    int ks = 1;
+    if (pending) {
+      each<0, PARTS>([&](auto part) NIMBLE_INLINE { run_stage(1 + decltype(part)::value, No{}, part); });
+      ks = 1 + PARTS;
+    }
+    for (; ks < KS; ++ks) run_stage(ks, No{}, Int<PARTS>{});
+    // (not before this tile's barriers: the values come where those of the tile before were)
+    if (follows) fetch_values(next_tile, values + (parity ^ 1));
+    end_of(tile, parity);
+    pending = follows && KS > PARTS;
+    if (!pending) {
+      each<0, TN>([&](auto i) NIMBLE_INLINE { each<0, TM>([&](auto j) NIMBLE_INLINE { put_aside(i, j); }); });
+      run_units();
+    }
+    if (!follows) break;
+    tile = next_tile;
+    parity ^= 1;
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+}
+
+}  // namespace nimble
+#endif

@@ -101,7 +101,9 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(QuantizeArgs g) {
       if (whole) {
         *(uint2*)(q + at) = make_uint2(code[0], code[1]);
       } else {
-        for (int i = 0; i < 8 && at + i < g.cols; ++i) q[at + i] = (signed char)(code[i >> 2] >> (8 * (i & 3)));
+        #pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (at + i < g.cols) q[at + i] = (signed char)(code[i >> 2] >> (8 * (i & 3)));
       }
     };
 #pragma unroll
