@@ -1,47 +1,88 @@
 // Shape functions and the dispatch function of the 8-bit and the grouped products.  Integer arithmetic only; no HIP call.
 #include "grouped_internal.h"
 
-#include <cstdlib>
-#include <cstdio>
+#include <cmath>
 
 namespace nimble {
 
 static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// The members of the family that need rows of whole 16 bytes: tile, waves among which K is divided, workgroups that share a compute unit.
+struct Member {
+  int kernel, bm, bn, k_waves, per_cu;
+  double fixed_us;  // of a workgroup: launch, first loads, sums and stores
+};
+static const Member kMembers[] = {
+    {NIMBLE_PRODUCT_STREAM, 8, 32, 4, 3, 2.0}, {NIMBLE_PRODUCT_STREAM, 16, 32, 4, 3, 2.0}, {NIMBLE_PRODUCT_STREAM, 32, 32, 4, 2, 2.2},
+    {NIMBLE_PRODUCT_STREAM, 64, 64, 4, 1, 4.0}, {NIMBLE_PRODUCT_STREAM, 64, 64, 2, 2, 4.5}, {NIMBLE_PRODUCT_TILES, 128, 256, 1, 1, 5.0},
+};
+
+// The most tile rows there can be: a group adds at most one that is not full, and only if it has a row.
+static int64_t most_tile_rows(const ProductShape& s, int bm) {
+  return s.grouped ? s.rows / bm + (s.groups < s.rows ? s.groups : s.rows) : ceil_div(s.rows, bm);
+}
+
+// Estimated microseconds.  How the rows fall on the groups is not known: each group is taken to have rows where there are
+// enough, and its last tile to be half full.  A workgroup of the streaming kernel takes a fixed time and then what its stages take to
+// arrive, 75 KB per us and compute unit; the workgroups of a compute unit share that.  A large tile takes 0.59 us per stage (of 128 bytes of
+// K) on a chip that is nearly empty and 0.81 on a full one (by power), and its end 1.3 us, with a GELU that is not known here
+// more.  Weights come at 4.8 TB/s where they come from memory.  Measured / estimated, dense in 8 bits with bias:
+//   rows x N x K         8 x 32         32 x 32       64 x 64, 4 waves   64 x 64, 2 waves   128 x 256
+//   1 x 4096 x 1024      2.9 / 3.5      3.7 / 4.1     6.1 / 6.7          7.4 / 7.2          9.7 / 11.3
+//   64 x 4096 x 1024                    3.7 / 4.1     6.1 / 6.7          7.4 / 7.2          10.0 / 11.3
+//   200 x 1024 x 4096                   6.2 / 6.6     9.6 / 11.8         13.6 / 12.3        24.1 / 25.5
+//   512 x 1024 x 4096                   9.9 / 10.0    10.5 / 11.8        13.8 / 12.3        24.5 / 25.6
+//   512 x 4096 x 1024                   15.2 / 16.6   12.3 / 12.4        9.7 / 8.9          10.6 / 11.5
+static double product_us(const ProductShape& s, const Member& m) {
+  const double kCUs = kComputeUnits;
+  const double live = s.grouped ? (double)(s.groups < s.rows ? s.groups : s.rows) : 1.0;
+  double tile_rows = s.grouped ? (double)s.rows / m.bm + 0.5 * live : (double)ceil_div(s.rows, m.bm);
+  if (tile_rows < live) tile_rows = live;
+  const double tiles = tile_rows * (double)ceil_div(s.N, m.bn), stages = (double)ceil_div(s.row_bytes(), 128);
+  double us;
+  if (m.kernel == NIMBLE_PRODUCT_TILES) {
+    const double turns = ceil(tiles / kCUs);
+    us = 1.0 + m.fixed_us + turns * (stages * (0.59 + 0.22 * (tiles < kCUs ? tiles / kCUs : 1.0)) + 1.3);
+  } else {
+    const double per_cu = tiles < kCUs ? 1.0 : tiles / kCUs;
+    us = 1.0 + ceil(tiles / (kCUs * m.per_cu)) * m.fixed_us + per_cu * stages * (m.bm + m.bn) * 0.128 / 75.0;
+  }
+  const double weights_us = live * (double)s.N * (double)s.row_bytes() / 4.8e6;
+  return (us > weights_us ? us : weights_us) + 0.25 * us;
+}
+
 int plan_product(const ProductShape& s, nimble_product_plan* p) {
   nimble_product_plan out{};
-  const int64_t rb = s.row_bytes(), ks = ceil_div(rb, 128);
-  const bool tiles_ok = rb % 16 == 0 && rb <= kMostTileRowBytes && s.N <= kMostTileColumns && s.N % 8 == 0 && (rb % 128 == 0 ? ks >= 3 : ks >= 4);
-  const int64_t most_groups = s.grouped ? s.groups : 1;
-  static const char* fs = getenv("PRODUCT");  // k,bm
-  int fk = -1, fb = 0;
-  if (fs) sscanf(fs, "%d,%d", &fk, &fb);
-  int64_t most = kMostWorkgroups;
-  const bool stream_ok = rb % 16 == 0 && rb > 0 && rb <= kMostTileRowBytes;
-  if (fk == 1 ? tiles_ok : fk < 0 && tiles_ok && s.rows >= 256 * most_groups) {
-    out.kernel = NIMBLE_PRODUCT_TILES;
-    out.bm = 128;
-    out.bn = 256;
-    out.k_waves = 1;
-    out.block = 256;
-    most = 256;
-  } else if (stream_ok && fk != 0) {
-    out.kernel = NIMBLE_PRODUCT_STREAM;
-    out.bm = out.bn = fb ? fb : s.rows <= 16 * most_groups ? 16 : s.rows <= 64 * most_groups ? 32 : 64;
-    out.k_waves = 4;
-    out.block = 256;
-  } else {
+  const int64_t rb = s.row_bytes(), stages = ceil_div(rb, 128);
+  const Member* best = nullptr;
+  double best_us = 0;
+  if (rb % 16 == 0 && rb > 0 && rb <= kMostTileRowBytes) {
+    for (const Member& m : kMembers) {
+      // the large tiles' ring is three stages ahead, which a partly filled last stage must not reach, and their rows are stored in
+      // whole 16 bytes
+      if (m.kernel == NIMBLE_PRODUCT_TILES && (s.N % 8 != 0 || s.N > kMostTileColumns || stages < (rb % 128 ? 4 : 3))) continue;
+      const double us = product_us(s, m);
+      if (!best || us < best_us) best = &m, best_us = us;
+    }
+  }
+  if (best) {
+    out.kernel = best->kernel;
+    out.bm = best->bm;
+    out.bn = best->bn;
+    out.k_waves = best->k_waves;
+    out.block = best->kernel == NIMBLE_PRODUCT_TILES ? 256 : 64u * (unsigned)best->k_waves;
+  } else {  // 8177 x 4096 x 1024 in 64 x 64 tiles 198 us; up to 16 rows of a group in 16 x 16
+    const bool few = s.rows <= 16 * (s.grouped ? s.groups : 1);
     out.kernel = NIMBLE_PRODUCT_DIRECT;
-    out.bm = fb ? fb : s.rows <= 16 * most_groups ? 16 : 64;
-    out.bn = out.bm;
-    out.k_waves = out.bm == 16 ? 8 : 4;
+    out.bm = out.bn = few ? 16 : 64;
+    out.k_waves = few ? 8 : 4;
     out.block = 64u * (unsigned)out.k_waves;
   }
-  // a group adds at most one tile row that is not full, and only if it has a row
-  const int64_t tile_rows = s.grouped ? s.rows / out.bm + (s.groups < s.rows ? s.groups : s.rows) : ceil_div(s.rows, out.bm);
-  const int64_t tiles_n = ceil_div(s.N, out.bn);
+  const int64_t tile_rows = most_tile_rows(s, out.bm), tiles_n = ceil_div(s.N, out.bn);
   if (tile_rows > 0x7fffffffll / (tiles_n > 0 ? tiles_n : 1)) return fail(NIMBLE_ERR_ARG, "more than 2^31 tiles");
   out.tiles = tile_rows * tiles_n;
+  // the large tiles' workgroups go round; the others' do where a launch could not hold them
+  const int64_t most = out.kernel == NIMBLE_PRODUCT_TILES ? kComputeUnits : kMostWorkgroups;
   out.grid = (uint32_t)(out.tiles < most ? out.tiles : most);
   *p = out;
   return NIMBLE_OK;

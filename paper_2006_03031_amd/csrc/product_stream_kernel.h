@@ -14,13 +14,14 @@ namespace nimble {
 // the buffer descriptors give, at no cost in memory traffic: a single row of x is read as one.
 //   Bias and scales of the tile come to LDS with the first loads.
 // ---------------------------------------------------------------------------
-template <typename T, int GROUPS, int TM, int TN, int KW, int S>
+template <typename T, int GROUPS, int TM, int TN, int KW, int S, int XR = 16 * TM>
 __global__ void __launch_bounds__(KW * 64) product_stream_kernel(ProductArgs g, unsigned tiles, unsigned tiles_n) {
   constexpr int BM = 16 * TM, BN = 16 * TN;
-  constexpr int LD = 2 * (TM + TN);                 // loads of 8 rows per stage
-  constexpr int SLOT = (BM + BN) * 8;               // uint4
+  constexpr int XL = XR / 8, LD = XL + 2 * TN;      // loads of 8 rows per stage
+  constexpr int SLOT = (XR + BN) * 8;               // uint4
   constexpr int RING = S * SLOT;
   static_assert(S * LD <= 60, "the wait counter holds 63");
+  static_assert(XR == 16 * TM || (TM == 1 && XR == 8), "x rows");
   static_assert(RING >= TM * TN * 64, "a wave's sums go where its ring was");
   typedef typename T::Acc Acc;
   __shared__ __attribute__((aligned(16))) uint4 smem[KW][RING];
@@ -28,7 +29,7 @@ __global__ void __launch_bounds__(KW * 64) product_stream_kernel(ProductArgs g, 
   __shared__ GroupMap<GROUPS> map;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (GROUPS) {
-    map_groups<BM>(g, map);
+    map_groups<XR>(g, map);
     __syncthreads();
   }
   const int KS = (g.row_bytes + 127) >> 7, left = g.row_bytes - (KS - 1) * 128;
@@ -37,19 +38,21 @@ __global__ void __launch_bounds__(KW * 64) product_stream_kernel(ProductArgs g, 
   // chunk c of row r lies at c ^ ((r >> 1) & 7); the two loads of 16 rows differ in it
   const int ld_c[2] = {(lane & 7) ^ (ld_row >> 1), (lane & 7) ^ (4 + (ld_row >> 1))};
   const int fr_phys = fr_q ^ ((fr_row >> 1) & 7), half = (fr_phys ^ 4) - fr_phys;
+  // (8 rows of x: the matrix instruction's other 8 rows take them again, for results that nobody asks for)
+  const int x_row = XR == 8 ? fr_row & 7 : fr_row, x_phys = fr_q ^ ((x_row >> 1) & 7), x_half = (x_phys ^ 4) - x_phys, x_at = x_row * 8 + x_phys;
   const uint4* ring = smem[wave];
   const uint32_t ring_lds = __builtin_amdgcn_readfirstlane(lds_addr_of(ring));
   uint32_t off[LD];
 #pragma unroll
   for (int u = 0; u < LD; ++u) {
-    const int row = (u < 2 * TM ? 8 * u : 8 * (u - 2 * TM)) + ld_row;
-    off[u] = (uint32_t)(row * g.row_bytes + ld_c[u & 1] * 16);
+    const int row = (u < XL ? 8 * u : 8 * (u - XL)) + ld_row;
+    off[u] = (uint32_t)(row * g.row_bytes + ld_c[(u < XL ? u : u - XL) & 1] * 16);
   }
   const uint32_t past[2] = {ld_c[0] * 16 >= left ? 0x80000000u : 0u, ld_c[1] * 16 >= left ? 0x80000000u : 0u};
   for (unsigned b = blockIdx.x; b < tiles; b += gridDim.x) {
     ProductTile tile;
     const unsigned t = b / tiles_n;
-    if (!find_tile<BM, BN>(g, map, (int)t, (int)(b - t * tiles_n), tile)) return;
+    if (!find_tile<XR, BN>(g, map, (int)t, (int)(b - t * tiles_n), tile)) return;
     const int columns = min(BN, g.N - tile.n0);
     const long long c0 = (long long)tile.group * g.N + tile.n0;
     const rsrc_t xr = descriptor(g.x + (long long)tile.row0 * g.row_bytes, (uint32_t)tile.rows * (uint32_t)g.row_bytes);
@@ -62,7 +65,7 @@ __global__ void __launch_bounds__(KW * 64) product_stream_kernel(ProductArgs g, 
       w[2] = real ? w[2] : 0;
 #pragma unroll
       for (int u = 0; u < LD; ++u)
-        dma16_buffer(off[u] | (past[u & 1] & end), u < 2 * TM ? x : w, (uint32_t)(real ? ks : 0) * 128u, ring_lds + slot * SLOT * 16 + u * 1024);
+        dma16_buffer(off[u] | (past[(u < XL ? u : u - XL) & 1] & end), u < XL ? x : w, (uint32_t)(real ? ks : 0) * 128u, ring_lds + slot * SLOT * 16 + u * 1024);
     };
     if (wave == 0) {
       if (T::kInt8) {
@@ -82,12 +85,12 @@ __global__ void __launch_bounds__(KW * 64) product_stream_kernel(ProductArgs g, 
     int slot = 0;
     for (int ks = wave; ks < KS; ks += KW) {
       asm volatile("s_waitcnt vmcnt(%0)" ::"n"((S - 1) * LD) : "memory");
-      const uint4* rd = ring + slot * SLOT + fr_row * 8 + fr_phys;
+      const uint4 *rw = ring + slot * SLOT + (XR + fr_row) * 8 + fr_phys, *rx = ring + slot * SLOT + x_at;
       uint4 x[TM][2], w[TN][2];
 #pragma unroll
-      for (int i = 0; i < TN; ++i) w[i][0] = rd[(BM + 16 * i) * 8], w[i][1] = rd[(BM + 16 * i) * 8 + half];
+      for (int i = 0; i < TN; ++i) w[i][0] = rw[16 * i * 8], w[i][1] = rw[16 * i * 8 + half];
 #pragma unroll
-      for (int j = 0; j < TM; ++j) x[j][0] = rd[16 * j * 8], x[j][1] = rd[16 * j * 8 + half];
+      for (int j = 0; j < TM; ++j) x[j][0] = rx[16 * j * 8], x[j][1] = rx[16 * j * 8 + x_half];
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       load(ks + S * KW, slot);
 #pragma unroll
