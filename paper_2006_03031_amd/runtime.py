@@ -22,6 +22,7 @@ class _StepsOnly:
     """In place of the native one-call sequences where they cannot be loaded (not built, or built for another torch):
     leaves every call to the steps, which give the same results, and says so on the first call on a GPU."""
     dense = attention = fused_attention = lstm_sequence = vm_run = set_workspace = staticmethod(lambda *a: None)
+    quantize_rows = product = bind_products = staticmethod(lambda *a: None)
 
     def __init__(self, why: ImportError):
         self.why = why
@@ -61,6 +62,9 @@ def _bind_host_calls(device) -> None:
                            "nimble_lstm_seq_preferred", "nimble_lstm_seq_workspace_bytes", "nimble_lstm_seq_pre_dyn",
                            "nimble_lstm_seq_status")]
     _host_calls.bind(*addresses, torch._C._cuda_getDevice, _raw_stream, device.index or 0)
+    _host_calls.bind_products(*[ctypes.cast(getattr(lib, f), ctypes.c_void_p).value
+                                for f in ("nimble_quantize_rows_dyn", "nimble_dense_i8_dyn", "nimble_grouped_dense_dyn",
+                                          "nimble_grouped_dense_i8_dyn")])
     _bound = True
 
 
@@ -277,6 +281,9 @@ def quantize_rows(x: torch.Tensor, cols: int = 0) -> Tuple[torch.Tensor, torch.T
     """Rows of x [M, K] (bf16 or f32) as 8-bit codes q [M, cols] and a scale each (f32 [M]): x is about q * scale.  Codes past K are
     0; cols = 0 rounds K up to whole 128 bytes.  Serves tokens and, row by row of w [N, K], output channels alike; a stack of
     experts' weights w [E, N, K] is quantised as w.view(E * N, K) and its results viewed back."""
+    r = _host_calls.quantize_rows(x, cols)
+    if r is not None:
+        return r
     q_shape, s_shape = nb.quantize_rows_shape(tuple(x.shape), cols)
     if x.dtype not in (_BF, _F32):
         raise nb.NimbleError(-4, f"quantize_rows: x is {x.dtype}")
@@ -285,6 +292,8 @@ def quantize_rows(x: torch.Tensor, cols: int = 0) -> Tuple[torch.Tensor, torch.T
         q, scale = _alloc(q_shape, nb.I8, x.device), _alloc(s_shape, nb.F32, x.device)
         nb.nimble_quantize_rows_dyn(px, nb.BF16 if x.dtype is _BF else nb.F32, q.data_ptr(), scale.data_ptr(), x.shape[0], x.shape[1],
                                     q_shape[1], _stream())
+    if not _bound:
+        _bind_host_calls(x.device)
     return q, scale
 
 
@@ -292,12 +301,17 @@ def dense_i8(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_scale: t
              epilogue: int = nb.EPI_BIAS, out_dtype: int = nb.BF16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """dense in 8-bit integers: y = epi(x_scale[m] w_scale[n] x.w^T + bias), x [M, K] and w [N, K] int8 with their scales (the results of
     quantize_rows), sums exact in 32 bits."""
+    r = _host_calls.product(x, x_scale, w, w_scale, bias, None, epilogue, out_dtype, out)
+    if r is not None:
+        return r
     M, N = nb.dense_i8_shape(tuple(x.shape), tuple(x_scale.shape), tuple(w.shape), tuple(w_scale.shape))
     with _together(x=x, x_scale=x_scale, w=w, w_scale=w_scale, bias=bias, out=out):
         y = _output(out, (M, N), out_dtype, x.device, "dense_i8")
         nb.nimble_dense_i8_dyn(_ptr(x, torch.int8, "x"), _ptr(x_scale, _F32, "x_scale"), _ptr(w, torch.int8, "w"),
                                _ptr(w_scale, _F32, "w_scale"), _bias(bias, (N,), epilogue, "dense_i8"),
                                _ptr(y, _TORCH_DTYPE[out_dtype], "y"), M, N, x.shape[1], epilogue, out_dtype, _stream())
+    if not _bound:
+        _bind_host_calls(x.device)
     return y
 
 
@@ -306,12 +320,17 @@ def grouped_dense(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor]
     """dense for rows that belong to E groups (experts) with a weight each: rows offsets[e] .. offsets[e+1]-1 of x [R, K] times
     w[e] of [E, N, K], bias [E, N].  offsets [E+1] is int64 on the GPU and is not waited for.  Rows of no group are left as they
     were in `out` (unspecified in a new output)."""
+    r = _host_calls.product(x, None, w, None, bias, offsets, epilogue, out_dtype, out)
+    if r is not None:
+        return r
     R, N = nb.grouped_dense_shape(tuple(x.shape), tuple(w.shape), tuple(offsets.shape))
     with _together(x=x, w=w, bias=bias, offsets=offsets, out=out):
         y = _output(out, (R, N), out_dtype, x.device, "grouped_dense")
         nb.nimble_grouped_dense_dyn(_ptr(x, _BF, "x"), _ptr(w, _BF, "w"), _bias(bias, w.shape[:2], epilogue, "grouped_dense"),
                                     _ptr(offsets, torch.int64, "offsets"), _ptr(y, _TORCH_DTYPE[out_dtype], "y"), R, w.shape[0], N,
                                     x.shape[1], epilogue, out_dtype, _stream())
+    if not _bound:
+        _bind_host_calls(x.device)
     return y
 
 
@@ -319,6 +338,9 @@ def grouped_dense_i8(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_
                      offsets: torch.Tensor, epilogue: int = nb.EPI_BIAS, out_dtype: int = nb.BF16,
                      out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """grouped_dense in 8-bit integers: x [R, K] int8 with x_scale [R], w [E, N, K] int8 with w_scale [E, N]."""
+    r = _host_calls.product(x, x_scale, w, w_scale, bias, offsets, epilogue, out_dtype, out)
+    if r is not None:
+        return r
     R, N = nb.grouped_dense_shape(tuple(x.shape), tuple(w.shape), tuple(offsets.shape))
     if tuple(x_scale.shape) != (R,) or tuple(w_scale.shape) != tuple(w.shape[:2]):
         raise nb.NimbleError(-3, f"grouped_dense_i8: scales of {tuple(x_scale.shape)} and {tuple(w_scale.shape)} for x {tuple(x.shape)} "
@@ -329,6 +351,8 @@ def grouped_dense_i8(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_
                                        _ptr(w_scale, _F32, "w_scale"), _bias(bias, w.shape[:2], epilogue, "grouped_dense_i8"),
                                        _ptr(offsets, torch.int64, "offsets"), _ptr(y, _TORCH_DTYPE[out_dtype], "y"), R, w.shape[0], N,
                                        x.shape[1], epilogue, out_dtype, _stream())
+    if not _bound:
+        _bind_host_calls(x.device)
     return y
 
 
