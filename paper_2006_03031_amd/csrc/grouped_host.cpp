@@ -2,6 +2,7 @@
 #include "grouped_internal.h"
 
 #include <cmath>
+#include <cstdlib>
 
 namespace nimble {
 
@@ -15,6 +16,7 @@ struct Member {
 static const Member kMembers[] = {
     {NIMBLE_PRODUCT_STREAM, 8, 32, 4, 3, 2.0}, {NIMBLE_PRODUCT_STREAM, 16, 32, 4, 3, 2.0}, {NIMBLE_PRODUCT_STREAM, 32, 32, 4, 2, 2.2},
     {NIMBLE_PRODUCT_STREAM, 64, 64, 4, 1, 4.0}, {NIMBLE_PRODUCT_STREAM, 64, 64, 2, 2, 4.5}, {NIMBLE_PRODUCT_TILES, 128, 256, 1, 1, 5.0},
+    {NIMBLE_PRODUCT_TILES, 256, 256, 1, 1, 5.0},
 };
 
 // The most tile rows there can be: a group adds at most one that is not full, and only if it has a row.
@@ -56,8 +58,10 @@ int plan_product(const ProductShape& s, nimble_product_plan* p) {
   const int64_t rb = s.row_bytes(), stages = ceil_div(rb, 128);
   const Member* best = nullptr;
   double best_us = 0;
+  static const char* only = getenv("PRODUCT_BM");
   if (rb % 16 == 0 && rb > 0 && rb <= kMostTileRowBytes) {
     for (const Member& m : kMembers) {
+      if (only && m.kernel == NIMBLE_PRODUCT_TILES && m.bm != atoi(only)) continue;
       // the large tiles' ring is three stages ahead, which a partly filled last stage must not reach, and their rows are stored in
       // whole 16 bytes
       if (m.kernel == NIMBLE_PRODUCT_TILES && (s.N % 8 != 0 || s.N > kMostTileColumns || stages < (rb % 128 ? 4 : 3))) continue;

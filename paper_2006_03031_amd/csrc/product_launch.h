@@ -22,13 +22,15 @@ int launch_product(const ProductArgs& g, const nimble_product_plan& p, hipStream
     const int tiles_m = (int)(p.tiles / tiles_n), group_m = 8;
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, g, tiles_m, (int)tiles_n, group_m); };
     const bool gelu = g.epilogue == NIMBLE_EPI_BIAS_GELU_ERF;
-    if (g.out_f32) {
-      if (gelu) launch(product_tile_kernel<T, GROUPS, true, true, 128, 256, 3>);
-      else launch(product_tile_kernel<T, GROUPS, true, false, 128, 256, 3>);
-    } else {
-      if (gelu) launch(product_tile_kernel<T, GROUPS, false, true, 128, 256, 3>);
-      else launch(product_tile_kernel<T, GROUPS, false, false, 128, 256, 3>);
-    }
+    auto pick = [&](auto f32, auto with_gelu) {
+      constexpr bool F = decltype(f32)::value, G = decltype(with_gelu)::value;
+      if (p.bm == 256) launch(product_tile_kernel<T, GROUPS, F, G, 256, 256, 2>);
+      else launch(product_tile_kernel<T, GROUPS, F, G, 128, 256, 3>);
+    };
+    using Yes = std::true_type;
+    using No = std::false_type;
+    if (g.out_f32) gelu ? pick(Yes{}, Yes{}) : pick(Yes{}, No{});
+    else gelu ? pick(No{}, Yes{}) : pick(No{}, No{});
     return launched("product tile kernel launch");
   }
   if (p.kernel == NIMBLE_PRODUCT_STREAM) {

@@ -101,7 +101,8 @@ __device__ __forceinline__ void copy_sums(int32_t (&to)[4], const Acc& from) {
   }
 }
 
-__device__ __forceinline__ float read_sum(const int32_t& sum) {
+template <typename V>
+__device__ __forceinline__ float read_sum(const V& sum) {
   float v;
   asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v) : "a"(sum));
   return v;
@@ -132,6 +133,8 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
   constexpr int MFMAS = 2 * TM * TN;     // of a stage
   constexpr int UNITS = TM * TN / 2;     // blocks of 16 rows and 32 columns
   constexpr int PARTS = 7;               // stages over which they are finished
+  constexpr bool ASIDE = 2 * TM * TN * 4 <= 256;  // registers for two tiles' sums: a tile's end during the next one, else behind its own
+  constexpr int STORES = UNITS * (OUT_F32 ? 2 : 1);
   constexpr int OPS = (T::kInt8 ? 4 : 2) + (GELU ? 7 : 0), STEPS = 2 * OPS + 1;  // of a block, see unit_step
   constexpr int OS = OUT_F32 ? 4 : 2;
   typedef TileValues<BM, BN> Values;
@@ -206,7 +209,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
   auto b_step = [](int i) { return (OUT_F32 ? 16 * i : 32 * (i >> 1) + 4 * (i & 1)) * 8; };
 
   Acc acc[TN][TM];          // this tile's sums
-  int32_t done[TN][TM][4];  // the last one's
+  int32_t done[ASIDE ? TN : 1][ASIDE ? TM : 1][4];  // the last one's
   auto put_aside = [&](auto i, auto j) NIMBLE_INLINE { copy_sums<Acc>(done[decltype(i)::value][decltype(j)::value], acc[decltype(i)::value][decltype(j)::value]); };
 
   Values* const values = (Values*)(smem + S * SLOT);
@@ -282,7 +285,11 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
       if constexpr (n == 0 && j == 0) read_columns(p);
 #pragma unroll
       for (int k = n % 2 * 4; k < n % 2 * 4 + 4; ++k) {
-        if constexpr (op == 0) v[k] = read_sum(done[2 * p + (k >> 2)][j][k & 3]);
+        if constexpr (op == 0 && ASIDE) v[k] = read_sum(done[2 * p + (k >> 2)][j][k & 3]);
+        if constexpr (op == 0 && !ASIDE) {
+          const auto sum = acc[2 * p + (k >> 2)][j][k & 3];
+          v[k] = read_sum(sum);
+        }
         if constexpr (op == 1) v[k] = (float)__float_as_int(v[k]);
         if constexpr (op == 2) e[k] = xs[j] * ws[k];
         if constexpr (op == 3) v[k] = T::kInt8 ? fmaf(v[k], e[k], bs[k]) : v[k] + bs[k];
@@ -335,14 +342,27 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
 #pragma unroll
   for (int x = 0; x < TN; ++x) rd_b0(0, x);
 
-  // S - 1 whole stages may be in flight (stores in between count as loads: the wait is for a little more then)
-  auto sync = [&] {
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(FLIGHT) : "memory");
+  // S - 1 whole stages may be in flight (stores in between count as loads: the wait is for a little more then); with `lax` also the
+  // stores of the tile before, all of them behind the loads that are waited for
+  auto sync = [&](int lax) NIMBLE_INLINE {
+    constexpr int MOST = FLIGHT + STORES < 63 ? FLIGHT + STORES : 63;
+    if constexpr (ASIDE)
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(FLIGHT) : "memory");
+    else
+      asm volatile(
+          "s_waitcnt lgkmcnt(0)\n\t"
+          "s_cmp_eq_u32 %0, 0\n\t"
+          "s_cbranch_scc0 .Lnimble_product_lax_%=\n\t"
+          "s_waitcnt vmcnt(%2)\n"
+          ".Lnimble_product_lax_%=:\n\t"
+          "s_waitcnt vmcnt(%1)\n" ::"s"(__builtin_amdgcn_readfirstlane(lax)),
+          "n"(MOST), "n"(FLIGHT)
+          : "memory", "scc");
     __syncthreads();
   };
   // One stage.  FIRST: of a tile, its products start from zero and the sums move over to `done`.  PART < PARTS: with that part
   // of the last tile's end.
-  auto stage = [&](auto first_tag, auto part_tag, int slot, int next, int last) NIMBLE_INLINE {
+  auto stage = [&](auto first_tag, auto part_tag, int slot, int next, int last, int lax1, int lax2) NIMBLE_INLINE {
     constexpr bool FIRST = decltype(first_tag)::value;
     constexpr int PART = decltype(part_tag)::value;
     constexpr int U0 = PART * UNITS / PARTS, U1 = PART < PARTS ? (PART + 1) * UNITS / PARTS : U0;
@@ -359,7 +379,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
         constexpr int n = decltype(n_tag)::value, kh = n / (G * TH), i = n / TH % G, j = i & 1 ? TH - 1 - n % TH : n % TH;
         constexpr bool zero = FIRST && kh == 0;
         Acc& sum = acc[i0 + i][j0 + j];
-        if constexpr (zero) put_aside(Int<i0 + i>{}, Int<j0 + j>{});
+        if constexpr (zero && ASIDE) put_aside(Int<i0 + i>{}, Int<j0 + j>{});
         constexpr int m0 = (n * nops + N - 1) / N, m1 = ((n + 1) * nops + N - 1) / N;
         constexpr int load0 = m0 > nrd ? m0 : nrd;  // loads of this gap: the last one goes behind the MFMA
         each<m0, (m1 < nrd ? m1 : nrd)>([&](auto m) NIMBLE_INLINE {
@@ -383,11 +403,11 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
           });
       });
     };
-    sync();
+    sync(lax1);
     quarter(xa0, wb0, Int<H0>{}, Int<0>{}, Int<0>{}, Int<0>{}, [&](int m) NIMBLE_INLINE { rd_b1(slot, m); }, Int<TN>{}, Int<0>{}, Int<H0>{});
     quarter(xa0, wb1, Int<H0>{}, Int<0>{}, Int<G>{}, Int<2 * G * H0>{}, [&](int m) NIMBLE_INLINE { rd_a1(slot, m); }, Int<2 * H1>{}, Int<H0>{},
             Int<G>{});
-    sync();
+    sync(lax2);
     quarter(xa1, wb0, Int<H1>{}, Int<H0>{}, Int<0>{}, Int<4 * G * H0>{}, [&](int m) NIMBLE_INLINE { rd_a0(next, m); }, Int<2 * H0>{},
             Int<H0 + G>{}, Int<G>{});
     quarter(xa1, wb1, Int<H1>{}, Int<H0>{}, Int<G>{}, Int<4 * G * H0 + 2 * G * H1>{}, [&](int m) NIMBLE_INLINE { rd_b0(next, m); }, Int<TN>{},
@@ -397,6 +417,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
   at = S * 128;
   int slot = 0, parity = 0;
   bool pending = false;  // `done` holds the sums of the tile before
+  bool stored = false;   // the tile before has issued its stores behind this one's first S stages
   const int left = g.row_bytes - (KS - 1) * 128;  // bytes of the last stage
   for (int t = blockIdx.x;; t += gridDim.x) {
     const bool follows = t + (int)gridDim.x < tiles_total;
@@ -418,13 +439,13 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
         }
       }
       const int next = slot + 1 == S ? 0 : slot + 1;
-      stage(first_tag, part_tag, slot, next, ks + 1 >= KS);
+      stage(first_tag, part_tag, slot, next, ks + 1 >= KS, stored && ks < S, stored && ks < S - 1);
       slot = next;
       at += 128;
     };
     run_stage(0, std::true_type{}, Int<PARTS>{});
     int ks = 1;
-    if (pending) {
+    if constexpr (ASIDE) if (pending) {
       each<0, PARTS>([&](auto part) NIMBLE_INLINE { run_stage(1 + decltype(part)::value, No{}, part); });
       ks = 1 + PARTS;
     }
@@ -432,9 +453,10 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
     // (not before this tile's barriers: the values come where those of the tile before were)
     if (follows) fetch_values(next_tile, values + (parity ^ 1));
     end_of(tile, parity);
-    pending = follows && KS > PARTS;
+    pending = ASIDE && follows && KS > PARTS;
+    stored = true;
     if (!pending) {
-      each<0, TN>([&](auto i) NIMBLE_INLINE { each<0, TM>([&](auto j) NIMBLE_INLINE { put_aside(i, j); }); });
+      if constexpr (ASIDE) each<0, TN>([&](auto i) NIMBLE_INLINE { each<0, TM>([&](auto j) NIMBLE_INLINE { put_aside(i, j); }); });
       run_units();
     }
     if (!follows) break;
