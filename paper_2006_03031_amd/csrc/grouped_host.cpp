@@ -2,21 +2,23 @@
 #include "grouped_internal.h"
 
 #include <cmath>
-#include <cstdlib>
 
 namespace nimble {
 
 static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// The members of the family that need rows of whole 16 bytes: tile, waves among which K is divided, workgroups that share a compute unit.
+// The members of the family that need rows of whole 16 bytes: tile, waves among which K is divided, workgroups that share a compute unit,
+// stages that are loaded ahead; microseconds of a workgroup that do not depend on K (launch, first loads, sums and stores; of a large tile its
+// end) and of a large tile per stage of 128 bytes of K on a full chip.
 struct Member {
-  int kernel, bm, bn, k_waves, per_cu;
-  double fixed_us;  // of a workgroup: launch, first loads, sums and stores
+  int kernel, bm, bn, k_waves, per_cu, ahead;
+  double fixed_us, stage_us;
 };
 static const Member kMembers[] = {
-    {NIMBLE_PRODUCT_STREAM, 8, 32, 4, 3, 2.0}, {NIMBLE_PRODUCT_STREAM, 16, 32, 4, 3, 2.0}, {NIMBLE_PRODUCT_STREAM, 32, 32, 4, 2, 2.2},
-    {NIMBLE_PRODUCT_STREAM, 64, 64, 4, 1, 4.0}, {NIMBLE_PRODUCT_STREAM, 64, 64, 2, 2, 4.5}, {NIMBLE_PRODUCT_TILES, 128, 256, 1, 1, 5.0},
-    {NIMBLE_PRODUCT_TILES, 256, 256, 1, 1, 5.0},
+    {NIMBLE_PRODUCT_STREAM, 8, 32, 4, 3, 0, 2.0, 0},      {NIMBLE_PRODUCT_STREAM, 16, 32, 4, 3, 0, 2.0, 0},
+    {NIMBLE_PRODUCT_STREAM, 32, 32, 4, 2, 0, 2.2, 0},     {NIMBLE_PRODUCT_STREAM, 64, 64, 4, 1, 0, 4.0, 0},
+    {NIMBLE_PRODUCT_STREAM, 64, 64, 2, 2, 0, 4.5, 0},     {NIMBLE_PRODUCT_TILES, 128, 256, 1, 1, 3, 2.6, 0.90},
+    {NIMBLE_PRODUCT_TILES, 192, 256, 1, 1, 2, 3.8, 1.15}, {NIMBLE_PRODUCT_TILES, 256, 256, 1, 1, 2, 4.7, 1.47},
 };
 
 // The most tile rows there can be: a group adds at most one that is not full, and only if it has a row.
@@ -26,15 +28,18 @@ static int64_t most_tile_rows(const ProductShape& s, int bm) {
 
 // Estimated microseconds.  How the rows fall on the groups is not known: each group is taken to have rows where there are
 // enough, and its last tile to be half full.  A workgroup of the streaming kernel takes a fixed time and then what its stages take to
-// arrive, 75 KB per us and compute unit; the workgroups of a compute unit share that.  A large tile takes 0.59 us per stage (of 128 bytes of
-// K) on a chip that is nearly empty and 0.81 on a full one (by power), and its end 1.3 us, with a GELU that is not known here
-// more.  Weights come at 4.8 TB/s where they come from memory.  Measured / estimated, dense in 8 bits with bias:
-//   rows x N x K         8 x 32         32 x 32       64 x 64, 4 waves   64 x 64, 2 waves   128 x 256
-//   1 x 4096 x 1024      2.9 / 3.5      3.7 / 4.1     6.1 / 6.7          7.4 / 7.2          9.7 / 11.3
-//   64 x 4096 x 1024                    3.7 / 4.1     6.1 / 6.7          7.4 / 7.2          10.0 / 11.3
-//   200 x 1024 x 4096                   6.2 / 6.6     9.6 / 11.8         13.6 / 12.3        24.1 / 25.5
-//   512 x 1024 x 4096                   9.9 / 10.0    10.5 / 11.8        13.8 / 12.3        24.5 / 25.6
-//   512 x 4096 x 1024                   15.2 / 16.6   12.3 / 12.4        9.7 / 8.9          10.6 / 11.5
+// arrive, 75 KB per us and compute unit; the workgroups of a compute unit share that.  Large tiles go round the chip, on a nearly
+// empty one (less power) with stages a quarter shorter; with groups half a turn more, for the last one that is not full.
+// Weights come at 4.8 TB/s where they come from memory.  Measured / estimated, dense in 8 bits with bias:
+//   rows x N x K         8 x 32      32 x 32      64 x 64, 4 waves  64 x 64, 2 waves  128 x 256    192 x 256    256 x 256
+//   1 x 4096 x 1024      2.9 / 3.5   3.7 / 3.9    6.1 / 6.7         7.4 / 7.2         9.7 / 12
+//   200 x 1024 x 4096                6.2 / 6.6    9.6 / 12          13.6 / 12         24 / 28
+//   512 x 1024 x 4096                9.9 / 10     10.5 / 12         13.8 / 12         24.5 / 28
+//   512 x 4096 x 1024                15.2 / 16.6  12.3 / 12.4       9.7 / 8.9         10.6 / 12
+//   8192 x 1024 x 4096                                                                31.8 / 35    37.7 / 42    45.8 / 50
+//   16384 x 1024 x 4096                                                               61.7 / 67    71.3 / 85    54.5 / 56
+//   8192 x 4096 x 1024                                                                41.3 / 43    40.7 / 43    36.4 / 37
+// and 16354 rows over 32 groups x 1024 x 4096                                         102 / 90     91.6 / 89    107 / 95
 static double product_us(const ProductShape& s, const Member& m) {
   const double kCUs = kComputeUnits;
   const double live = s.grouped ? (double)(s.groups < s.rows ? s.groups : s.rows) : 1.0;
@@ -43,8 +48,10 @@ static double product_us(const ProductShape& s, const Member& m) {
   const double tiles = tile_rows * (double)ceil_div(s.N, m.bn), stages = (double)ceil_div(s.row_bytes(), 128);
   double us;
   if (m.kernel == NIMBLE_PRODUCT_TILES) {
-    const double turns = ceil(tiles / kCUs);
-    us = 1.0 + m.fixed_us + turns * (stages * (0.59 + 0.22 * (tiles < kCUs ? tiles / kCUs : 1.0)) + 1.3);
+    const double full = tiles < kCUs ? tiles / kCUs : 1.0;
+    double turns = s.grouped && s.groups > 1 ? tiles / kCUs + 0.5 : ceil(tiles / kCUs);
+    if (turns < 1.0) turns = 1.0;
+    us = 4.0 + turns * (stages * m.stage_us * (0.75 + 0.25 * full) + m.fixed_us);
   } else {
     const double per_cu = tiles < kCUs ? 1.0 : tiles / kCUs;
     us = 1.0 + ceil(tiles / (kCUs * m.per_cu)) * m.fixed_us + per_cu * stages * (m.bm + m.bn) * 0.128 / 75.0;
@@ -58,13 +65,10 @@ int plan_product(const ProductShape& s, nimble_product_plan* p) {
   const int64_t rb = s.row_bytes(), stages = ceil_div(rb, 128);
   const Member* best = nullptr;
   double best_us = 0;
-  static const char* only = getenv("PRODUCT_BM");
   if (rb % 16 == 0 && rb > 0 && rb <= kMostTileRowBytes) {
     for (const Member& m : kMembers) {
-      if (only && m.kernel == NIMBLE_PRODUCT_TILES && m.bm != atoi(only)) continue;
-      // the large tiles' ring is three stages ahead, which a partly filled last stage must not reach, and their rows are stored in
-      // whole 16 bytes
-      if (m.kernel == NIMBLE_PRODUCT_TILES && (s.N % 8 != 0 || s.N > kMostTileColumns || stages < (rb % 128 ? 4 : 3))) continue;
+      // a large tile's first loads must not reach a partly filled last stage, and its rows are stored in whole 16 bytes
+      if (m.kernel == NIMBLE_PRODUCT_TILES && (s.N % 8 != 0 || s.N > kMostTileColumns || stages < m.ahead + (rb % 128 ? 1 : 0))) continue;
       const double us = product_us(s, m);
       if (!best || us < best_us) best = &m, best_us = us;
     }

@@ -21,16 +21,14 @@ int launch_product(const ProductArgs& g, const nimble_product_plan& p, hipStream
   if (p.kernel == NIMBLE_PRODUCT_TILES) {
     const int tiles_m = (int)(p.tiles / tiles_n), group_m = 8;
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, g, tiles_m, (int)tiles_n, group_m); };
-    const bool gelu = g.epilogue == NIMBLE_EPI_BIAS_GELU_ERF;
-    auto pick = [&](auto f32, auto with_gelu) {
-      constexpr bool F = decltype(f32)::value, G = decltype(with_gelu)::value;
-      if (p.bm == 256) launch(product_tile_kernel<T, GROUPS, F, G, 256, 256, 2>);
-      else launch(product_tile_kernel<T, GROUPS, F, G, 128, 256, 3>);
+    auto pick = [&](auto f32) {
+      constexpr bool F = decltype(f32)::value;
+      if (p.bm == 256) launch(product_tile_kernel<T, GROUPS, F, 256, 256, 2>);
+      else if (p.bm == 192) launch(product_tile_kernel<T, GROUPS, F, 192, 256, 2>);
+      else launch(product_tile_kernel<T, GROUPS, F, 128, 256, 3>);
     };
-    using Yes = std::true_type;
-    using No = std::false_type;
-    if (g.out_f32) gelu ? pick(Yes{}, Yes{}) : pick(Yes{}, No{});
-    else gelu ? pick(No{}, Yes{}) : pick(No{}, No{});
+    if (g.out_f32) pick(std::true_type{});
+    else pick(std::false_type{});
     return launched("product tile kernel launch");
   }
   if (p.kernel == NIMBLE_PRODUCT_STREAM) {

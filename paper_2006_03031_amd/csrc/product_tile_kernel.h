@@ -9,20 +9,21 @@ namespace nimble {
 // Tiles of BM x BN by four waves in two rows and two columns, one wave per SIMD, one tile after the other: a ring of S stages
 // of 128 bytes of K in LDS, each stage multiplied in four quarters, the fragments that the next quarter needs read and the
 // stage S ahead loaded in between its MFMAs (the schedule of gemm_quarter_kernel.h).  A stage of 128 bytes takes the matrix cores the
-// same time in either type: 64 k of bf16, 128 k of int8.
-//   The end of a tile is computed during the next one.  With K = 1024 a tile is 8 (int8) or 16 stages, and scales, bias, GELU and stores
-// of its outputs took as long again, the matrix cores idle and all workgroups storing at once.  So a tile's sums are moved aside by the
-// first products of the next (which start from zero), and one to three blocks of 16 x 32 outputs are finished in each of the stages
-// behind, a step of eight instructions between two MFMAs, which leave three issue slots in four free.
+// same time in either type: 64 k of bf16, 128 k of int8.  Bound: MFMA and, with real data, the power that products, fragment reads and
+// loads take together; with short K also the ends of the tiles.
 //   Columns go to the matrix instruction's rows such that a lane holds eight neighbouring ones of bf16 (four of f32): 16 bytes, 64
 // contiguous ones with its three neighbours, stored from registers as they are.  The swizzle of the weights' rows in LDS
-// follows (see b_swizzle).
+// follows (see b_swizzle).  With the outputs brought into whole lines through LDS first, 8192 x 4096 x 1024 in 8 bits took 53.6 us, so 36.4.
+//   The loads past a tile's last stage are the next tile's first ones, and the stores of a tile's end stay in flight while the next
+// begins.  To put a tile's sums aside and finish them in between the next tile's products as well (128 x 256, twice 128 registers
+// of sums) gained nothing: 41.3 us, with it 40.3; one wave issues an instruction in four clocks at most, and products, reads and
+// loads leave it few.
 //   Loads go through buffer descriptors that end with the tile's last row (of its group, of the weight): rows past it, which
 // belong to another group or to nobody, come back as zeros, and so does, by an offset past every descriptor, what lies behind
 // the end of K in the last stage.  Stores past the last row or column are dropped in the same way.  So every tile runs the same code
 // whatever its number of rows.
-//   Tiles are told from the offsets of the groups (GroupMap), which the workgroup reads once.  The loads past a tile's last
-// stage are the next tile's first ones.
+//   Tiles are told from the offsets of the groups (GroupMap), which the workgroup reads once.
+//   Measured, 8 bits / bf16: 8192^3 396 / 737 us (2780 / 1490 T); 8192 x 4096 x 1024 with bias 36.4 / 62, with GELU 45.3 / 72.
 // ---------------------------------------------------------------------------
 #define NIMBLE_INLINE __attribute__((always_inline))
 template <int N>
@@ -36,7 +37,6 @@ __device__ __forceinline__ void each(F&& f) {
     each<FROM + 1, TO>(f);
   }
 }
-
 // 16 bytes per lane to the descriptor's byte voff + soff, through the L2 (see store_through); past its end nothing.
 __device__ __forceinline__ void store16_buffer(uint4 v, uint32_t voff, rsrc_t rsrc, uint32_t soff) {
   asm volatile("buffer_store_dwordx4 %0, %1, %2, %3 offen sc1\n\ts_nop 1" ::"v"(__builtin_bit_cast(i32x4, v)), "v"(voff),
@@ -91,19 +91,11 @@ NIMBLE_PRODUCT_MFMA(OfBf16, "v_mfma_f32_16x16x32_bf16")
 NIMBLE_PRODUCT_MFMA(OfInt8, "v_mfma_i32_16x16x64_i8")
 #undef NIMBLE_PRODUCT_MFMA
 
-// (A statement: as an ordinary copy the compiler would let either stand for both, and move 128 registers back in every stage.)
-template <typename Acc>
-__device__ __forceinline__ void copy_sums(int32_t (&to)[4], const Acc& from) {
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const auto one = from[k];
-    asm volatile("v_accvgpr_mov_b32 %0, %1" : "=a"(to[k]) : "a"(one));
-  }
-}
-
+// A sum out of its accumulation register, where the source has it: left to itself the compiler fetches all sums of a tile before it
+// needs them, and spills.
 template <typename V>
-__device__ __forceinline__ float read_sum(const V& sum) {
-  float v;
+__device__ __forceinline__ V read_sum(const V& sum) {
+  V v;
   asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v) : "a"(sum));
   return v;
 }
@@ -117,7 +109,7 @@ struct TileValues {
 template <int BM, int BN, int S>
 constexpr int kProductTileBytes = S * (BM + BN) * 128 + 2 * (int)sizeof(TileValues<BM, BN>);
 
-template <typename T, int GROUPS, bool OUT_F32, bool GELU, int BM, int BN, int S>
+template <typename T, int GROUPS, bool OUT_F32, int BM, int BN, int S>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1)))
     product_tile_kernel(ProductArgs g, int tiles_m, int tiles_n, int group_m) {
   constexpr int WM = BM / 2, WN = BN / 2;
@@ -131,11 +123,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
   constexpr int FLIGHT = (S - 1) * LDT;  // loads that may be in flight at a barrier
   static_assert(FLIGHT + G + H1 <= 63, "the wait counter holds 63");
   constexpr int MFMAS = 2 * TM * TN;     // of a stage
-  constexpr int UNITS = TM * TN / 2;     // blocks of 16 rows and 32 columns
-  constexpr int PARTS = 7;               // stages over which they are finished
-  constexpr bool ASIDE = 2 * TM * TN * 4 <= 256;  // registers for two tiles' sums: a tile's end during the next one, else behind its own
-  constexpr int STORES = UNITS * (OUT_F32 ? 2 : 1);
-  constexpr int OPS = (T::kInt8 ? 4 : 2) + (GELU ? 7 : 0), STEPS = 2 * OPS + 1;  // of a block, see unit_step
+  constexpr int STORES = TM * TN / 2 * (OUT_F32 ? 2 : 1);  // per wave, of a tile's end
   constexpr int OS = OUT_F32 ? 4 : 2;
   typedef TileValues<BM, BN> Values;
   typedef typename T::Acc Acc;
@@ -208,9 +196,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
   // rows of tile i behind those of tile 0 (the swizzle is the same: whole 16 rows, or 4 of which it does not depend on bit 2)
   auto b_step = [](int i) { return (OUT_F32 ? 16 * i : 32 * (i >> 1) + 4 * (i & 1)) * 8; };
 
-  Acc acc[TN][TM];          // this tile's sums
-  int32_t done[ASIDE ? TN : 1][ASIDE ? TM : 1][4];  // the last one's
-  auto put_aside = [&](auto i, auto j) NIMBLE_INLINE { copy_sums<Acc>(done[decltype(i)::value][decltype(j)::value], acc[decltype(i)::value][decltype(j)::value]); };
+  Acc acc[TN][TM];
 
   Values* const values = (Values*)(smem + S * SLOT);
   // 4 bytes per lane; past the end of the row or of the tile's rows nothing is needed, and zeros come
@@ -230,92 +216,52 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
     }
   };
 
-  // ---- the end of a tile, in blocks of two 16-column tiles 2 p, 2 p + 1 of 16 rows j, p first.  A lane's eight values are
-  // columns 8 fr_q .. + 7 of the 32 (bf16), or 4 fr_q .. + 3 of either 16 (f32), of row fr_row.
-  ProductTile from;                     // whose sums are in `done`
-  const Values* from_values = values;
-  rsrc_t out;
-  const uint32_t out_row = (uint32_t)g.N * OS * 16;  // 16 rows
+  // The end of a tile, in blocks of two 16-column tiles 2 p, 2 p + 1 and 16 rows j.  A lane's eight values are columns 8 fr_q .. + 7 of
+  // the 32 (bf16), or 4 fr_q .. + 3 of either 16 (f32), of row fr_row.
+  const uint32_t out_row = (uint32_t)g.N * OS * 16;   // 16 rows
   const int out_col = OUT_F32 ? 4 * fr_q : 8 * fr_q;  // first column of a lane within its 32
   const uint32_t out_off = (uint32_t)((wm * WM + fr_row) * g.N + wn * WN + out_col) * OS;
-  float v[8], e[8], t4[4], ws[8], bs[8], xs[TM];
-#pragma unroll
-  for (int k = 0; k < 8; ++k) v[k] = e[k] = 0.0f;
   auto column = [&](int p, int k) { return wn * WN + 32 * p + out_col + (OUT_F32 ? 16 * (k >> 2) + (k & 3) : k); };
-  auto read_rows = [&] {
+  auto finish = [&](const ProductTile& t, const Values& val, auto gelu) NIMBLE_INLINE {
+    const rsrc_t out = descriptor((unsigned char*)g.y + ((long long)t.row0 * g.N + t.n0) * OS,
+                                  (uint32_t)((t.rows - 1) * g.N + min(BN, g.N - t.n0)) * OS);
+    float xs[TM];
 #pragma unroll
-    for (int j = 0; j < TM; ++j) xs[j] = T::kInt8 ? from_values->x_scale[wm * WM + j * 16 + fr_row] : 1.0f;
-  };
-  auto read_columns = [&](int p) NIMBLE_INLINE {
+    for (int j = 0; j < TM; ++j) xs[j] = T::kInt8 ? val.x_scale[wm * WM + j * 16 + fr_row] : 1.0f;
+    each<0, TN / 2>([&](auto p_tag) NIMBLE_INLINE {
+      constexpr int p = decltype(p_tag)::value;
+      float ws[8], bs[8];
 #pragma unroll
-    for (int k = 0; k < 8; k += 4) {
-      const int c = column(p, k);
-      if (T::kInt8) {
-        const float4 w4 = *(const float4*)(from_values->w_scale + c);
+      for (int k = 0; k < 8; k += 4) {
+        const int c = column(p, k);
+        const float4 w4 = T::kInt8 ? *(const float4*)(val.w_scale + c) : make_float4(1.0f, 1.0f, 1.0f, 1.0f);
+        const uint2 bb = g.epilogue != NIMBLE_EPI_NONE ? *(const uint2*)(val.bias + c) : make_uint2(0, 0);
         ws[k] = w4.x, ws[k + 1] = w4.y, ws[k + 2] = w4.z, ws[k + 3] = w4.w;
+        bs[k] = bf2f((u16)(bb.x & 0xffff)), bs[k + 1] = bf2f((u16)(bb.x >> 16));
+        bs[k + 2] = bf2f((u16)(bb.y & 0xffff)), bs[k + 3] = bf2f((u16)(bb.y >> 16));
       }
-      const uint2 bb = *(const uint2*)(from_values->bias + c);
-      bs[k] = bf2f((u16)(bb.x & 0xffff)), bs[k + 1] = bf2f((u16)(bb.x >> 16));
-      bs[k + 2] = bf2f((u16)(bb.y & 0xffff)), bs[k + 3] = bf2f((u16)(bb.y >> 16));
-    }
-    if (g.epilogue == NIMBLE_EPI_NONE) {
+      const uint32_t c = (uint32_t)(t.n0 + wn * WN + 32 * p + out_col);
+      each<0, TM>([&](auto j_tag) NIMBLE_INLINE {
+        constexpr int j = decltype(j_tag)::value;
+        float v[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) bs[k] = 0.0f;
-    }
-  };
-  // Step n of a block: an operation on four values of the eight; the last one stores.  What a step leaves goes through an
-  // empty statement, which holds it to its place between the products.
-  auto unit_step = [&](auto unit_tag, auto n_tag) NIMBLE_INLINE {
-    constexpr int p = decltype(unit_tag)::value / TM, j = decltype(unit_tag)::value % TM, n = decltype(n_tag)::value;
-    if constexpr (n == STEPS - 1) {
-      const uint32_t c = (uint32_t)(from.n0 + wn * WN + 32 * p + out_col);
-      if constexpr (OUT_F32) {
-        each<0, 2>([&](auto x_tag) NIMBLE_INLINE {
-          constexpr int x = decltype(x_tag)::value;
-          store16_buffer(__builtin_bit_cast(uint4, make_float4(v[4 * x], v[4 * x + 1], v[4 * x + 2], v[4 * x + 3])),
-                         c + 16 * x < (uint32_t)g.N ? out_off + (32 * p + 16 * x) * OS : 0x80000000u, out, j * out_row);
-        });
-      } else {
-        store16_buffer(make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])),
-                       c < (uint32_t)g.N ? out_off + 32 * p * OS : 0x80000000u, out, j * out_row);
-      }
-    } else {
-      // the operation, those of bf16 and the GELU numbered as if all were there
-      constexpr int o = n / 2, op = T::kInt8 || o == 0 ? o : o + 2;
-      if constexpr (n == 0 && j == 0) read_columns(p);
-#pragma unroll
-      for (int k = n % 2 * 4; k < n % 2 * 4 + 4; ++k) {
-        if constexpr (op == 0 && ASIDE) v[k] = read_sum(done[2 * p + (k >> 2)][j][k & 3]);
-        if constexpr (op == 0 && !ASIDE) {
-          const auto sum = acc[2 * p + (k >> 2)][j][k & 3];
-          v[k] = read_sum(sum);
+        for (int k = 0; k < 8; ++k) {
+          const auto held = acc[2 * p + (k >> 2)][j][k & 3];
+          const float sum = (float)read_sum(held);
+          v[k] = T::kInt8 ? fmaf(sum, xs[j] * ws[k], bs[k]) : sum + bs[k];
         }
-        if constexpr (op == 1) v[k] = (float)__float_as_int(v[k]);
-        if constexpr (op == 2) e[k] = xs[j] * ws[k];
-        if constexpr (op == 3) v[k] = T::kInt8 ? fmaf(v[k], e[k], bs[k]) : v[k] + bs[k];
-        // the GELU of epilogue_of: v sigmoid(v (a + b t + c t^2)), t = min(v^2, 81)
-        if constexpr (op == 4) e[k] = v[k] * v[k];
-        if constexpr (op == 5) t4[k & 3] = fminf(e[k], 81.0f), e[k] = fmaf(0.0010142630f, t4[k & 3], -0.10677572f), e[k] = fmaf(e[k], t4[k & 3], -2.3011212f);
-        if constexpr (op == 6) e[k] = e[k] * v[k];
-        if constexpr (op == 7) e[k] = __builtin_amdgcn_exp2f(e[k]);
-        if constexpr (op == 8) e[k] = 1.0f + e[k];
-        if constexpr (op == 9) e[k] = __builtin_amdgcn_rcpf(e[k]);
-        if constexpr (op == 10) v[k] *= e[k];
-        if constexpr (op != 0) asm volatile("" : "+v"(v[k]), "+v"(e[k]));
-      }
-    }
-  };
-  // All blocks at once.
-  auto run_units = [&]() NIMBLE_INLINE {
-    each<0, UNITS>([&](auto u) NIMBLE_INLINE { each<0, STEPS>([&](auto n) NIMBLE_INLINE { unit_step(u, n); }); });
-  };
-  // `t` becomes the tile whose end is to be computed, its values in slot `parity`
-  auto end_of = [&](const ProductTile& t, int parity) {
-    from = t;
-    from_values = values + parity;
-    out = descriptor((unsigned char*)g.y + ((long long)t.row0 * g.N + t.n0) * OS,
-                     (uint32_t)((t.rows - 1) * g.N + min(BN, g.N - t.n0)) * OS);
-    read_rows();
+        epilogue_of<decltype(gelu)::value>(v);
+        if constexpr (OUT_F32) {
+#pragma unroll
+          for (int x = 0; x < 2; ++x)
+            store16_buffer(__builtin_bit_cast(uint4, make_float4(v[4 * x], v[4 * x + 1], v[4 * x + 2], v[4 * x + 3])),
+                           c + 16 * x < (uint32_t)g.N ? out_off + (32 * p + 16 * x) * OS : 0x80000000u, out, j * out_row);
+        } else {
+          store16_buffer(make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])),
+                         c < (uint32_t)g.N ? out_off + 32 * p * OS : 0x80000000u, out, j * out_row);
+        }
+      });
+    });
   };
 
   // ---- the walk
@@ -342,31 +288,24 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
 #pragma unroll
   for (int x = 0; x < TN; ++x) rd_b0(0, x);
 
-  // S - 1 whole stages may be in flight (stores in between count as loads: the wait is for a little more then); with `lax` also the
-  // stores of the tile before, all of them behind the loads that are waited for
+  // S - 1 whole stages may be in flight; with `lax` also the stores of the tile before, all of them behind the loads that are
+  // waited for
   auto sync = [&](int lax) NIMBLE_INLINE {
     constexpr int MOST = FLIGHT + STORES < 63 ? FLIGHT + STORES : 63;
-    if constexpr (ASIDE)
-      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(FLIGHT) : "memory");
-    else
-      asm volatile(
-          "s_waitcnt lgkmcnt(0)\n\t"
-          "s_cmp_eq_u32 %0, 0\n\t"
-          "s_cbranch_scc0 .Lnimble_product_lax_%=\n\t"
-          "s_waitcnt vmcnt(%2)\n"
-          ".Lnimble_product_lax_%=:\n\t"
-          "s_waitcnt vmcnt(%1)\n" ::"s"(__builtin_amdgcn_readfirstlane(lax)),
-          "n"(MOST), "n"(FLIGHT)
-          : "memory", "scc");
+    asm volatile(
+        "s_waitcnt lgkmcnt(0)\n\t"
+        "s_cmp_eq_u32 %0, 0\n\t"
+        "s_cbranch_scc0 .Lnimble_product_lax_%=\n\t"
+        "s_waitcnt vmcnt(%2)\n"
+        ".Lnimble_product_lax_%=:\n\t"
+        "s_waitcnt vmcnt(%1)\n" ::"s"(__builtin_amdgcn_readfirstlane(lax)),
+        "n"(MOST), "n"(FLIGHT)
+        : "memory", "scc");
     __syncthreads();
   };
-  // One stage.  FIRST: of a tile, its products start from zero and the sums move over to `done`.  PART < PARTS: with that part
-  // of the last tile's end.
-  auto stage = [&](auto first_tag, auto part_tag, int slot, int next, int last, int lax1, int lax2) NIMBLE_INLINE {
+  // One stage.  FIRST: of a tile, its products start from zero.
+  auto stage = [&](auto first_tag, int slot, int next, int last, int lax1, int lax2) NIMBLE_INLINE {
     constexpr bool FIRST = decltype(first_tag)::value;
-    constexpr int PART = decltype(part_tag)::value;
-    constexpr int U0 = PART * UNITS / PARTS, U1 = PART < PARTS ? (PART + 1) * UNITS / PARTS : U0;
-    constexpr int NSTEPS = (U1 - U0) * STEPS;
     const uint32_t dst = lds0 + slot * SLOT;
     // TH x G tiles over the stage's 128 bytes, from the stage's product number n0 on; in between `nrd` fragment reads, then the
     // loads u0 ... u0 + nld - 1
@@ -379,7 +318,6 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
         constexpr int n = decltype(n_tag)::value, kh = n / (G * TH), i = n / TH % G, j = i & 1 ? TH - 1 - n % TH : n % TH;
         constexpr bool zero = FIRST && kh == 0;
         Acc& sum = acc[i0 + i][j0 + j];
-        if constexpr (zero && ASIDE) put_aside(Int<i0 + i>{}, Int<j0 + j>{});
         constexpr int m0 = (n * nops + N - 1) / N, m1 = ((n + 1) * nops + N - 1) / N;
         constexpr int load0 = m0 > nrd ? m0 : nrd;  // loads of this gap: the last one goes behind the MFMA
         each<m0, (m1 < nrd ? m1 : nrd)>([&](auto m) NIMBLE_INLINE {
@@ -397,10 +335,6 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
           mfma_in_place_load<zero>(sum, w[i][kh], x[j][kh], off[u], src(u), at, dst, lds_off[u]);
         else
           mfma_in_place<zero>(sum, w[i][kh], x[j][kh]);
-        if constexpr (NSTEPS > 0)
-          each<(n0 + n) * NSTEPS / MFMAS, (n0 + n + 1) * NSTEPS / MFMAS>([&](auto m) NIMBLE_INLINE {
-            unit_step(Int<U0 + decltype(m)::value / STEPS>{}, Int<decltype(m)::value % STEPS>{});
-          });
       });
     };
     sync(lax1);
@@ -413,17 +347,15 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
     quarter(xa1, wb1, Int<H1>{}, Int<H0>{}, Int<G>{}, Int<4 * G * H0 + 2 * G * H1>{}, [&](int m) NIMBLE_INLINE { rd_b0(next, m); }, Int<TN>{},
             Int<H0 + TN>{}, Int<H1>{});
   };
-  using No = std::false_type;
   at = S * 128;
   int slot = 0, parity = 0;
-  bool pending = false;  // `done` holds the sums of the tile before
-  bool stored = false;   // the tile before has issued its stores behind this one's first S stages
+  bool stored = false;  // the tile before has issued its stores behind this one's first S stages
   const int left = g.row_bytes - (KS - 1) * 128;  // bytes of the last stage
   for (int t = blockIdx.x;; t += gridDim.x) {
     const bool follows = t + (int)gridDim.x < tiles_total;
     // Stage ks loads stage ks + S of this tile: of its last one the pieces past the end of K are zeros; behind it come the next
     // tile's first ones (there is none: nothing is read).
-    auto run_stage = [&](int ks, auto first_tag, auto part_tag) NIMBLE_INLINE {
+    auto run_stage = [&](int ks, auto first_tag) NIMBLE_INLINE {
       if (ks == KS - S - 1 && left < 128) {
 #pragma unroll
         for (int u = 0; u < LDT; ++u) off[u] = (of_a(u) ? ld_a : ld_b) * 16 < left ? off[u] : 0x80000000u;
@@ -439,27 +371,20 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
         }
       }
       const int next = slot + 1 == S ? 0 : slot + 1;
-      stage(first_tag, part_tag, slot, next, ks + 1 >= KS, stored && ks < S, stored && ks < S - 1);
+      stage(first_tag, slot, next, ks + 1 >= KS, stored && ks < S, stored && ks < S - 1);
       slot = next;
       at += 128;
     };
-    run_stage(0, std::true_type{}, Int<PARTS>{});
-    int ks = 1;
-    if constexpr (ASIDE) if (pending) {
-      each<0, PARTS>([&](auto part) NIMBLE_INLINE { run_stage(1 + decltype(part)::value, No{}, part); });
-      ks = 1 + PARTS;
-    }
-    for (; ks < KS; ++ks) run_stage(ks, No{}, Int<PARTS>{});
+    run_stage(0, std::true_type{});
+    for (int ks = 1; ks < KS; ++ks) run_stage(ks, std::false_type{});
     // (not before this tile's barriers: the values come where those of the tile before were)
     if (follows) fetch_values(next_tile, values + (parity ^ 1));
-    end_of(tile, parity);
-    pending = ASIDE && follows && KS > PARTS;
-    stored = true;
-    if (!pending) {
-      if constexpr (ASIDE) each<0, TN>([&](auto i) NIMBLE_INLINE { each<0, TM>([&](auto j) NIMBLE_INLINE { put_aside(i, j); }); });
-      run_units();
-    }
+    if (g.epilogue == NIMBLE_EPI_BIAS_GELU_ERF)
+      finish(tile, values[parity], std::true_type{});
+    else
+      finish(tile, values[parity], std::false_type{});
     if (!follows) break;
+    stored = true;
     tile = next_tile;
     parity ^= 1;
   }
