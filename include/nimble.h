@@ -356,6 +356,7 @@ int nimble_lstm_loop_dyn(const void* x, const void* pre, const void* w, const vo
  * dense in 8-bit integers: rows are codes of -127..127 with an f32 scale each (a token of x, an output channel of w).
  * Grouped dense: x [R,K] holds the rows of E groups (experts) one after the other, w [E,N,K] a weight for each; where the
  * groups begin is known on the device only.  No call here needs a workspace or waits, and any number may run at once.
+ * Outputs must not overlap operands.
  *
  * Shape function of nimble_quantize_rows_dyn: x (M,K) -> q (M, cols), scale (M).  cols = K rounded up to whole 128 bytes, the
  * width at which the products' loads are whole lines, where `cols` is 0; else `cols`, which must not be less than K. */

@@ -18,7 +18,8 @@ static const Member kMembers[] = {
     {NIMBLE_PRODUCT_STREAM, 8, 32, 4, 3, 0, 2.0, 0},      {NIMBLE_PRODUCT_STREAM, 16, 32, 4, 3, 0, 2.0, 0},
     {NIMBLE_PRODUCT_STREAM, 32, 32, 4, 2, 0, 2.2, 0},     {NIMBLE_PRODUCT_STREAM, 64, 64, 4, 1, 0, 4.0, 0},
     {NIMBLE_PRODUCT_STREAM, 64, 64, 2, 2, 0, 4.5, 0},     {NIMBLE_PRODUCT_TILES, 128, 256, 1, 1, 3, 2.6, 0.90},
-    {NIMBLE_PRODUCT_TILES, 192, 256, 1, 1, 2, 3.8, 1.15}, {NIMBLE_PRODUCT_TILES, 256, 256, 1, 1, 2, 4.7, 1.47},
+    {NIMBLE_PRODUCT_TILES, 160, 256, 1, 1, 2, 3.2, 1.01}, {NIMBLE_PRODUCT_TILES, 192, 256, 1, 1, 2, 3.8, 1.15},
+    {NIMBLE_PRODUCT_TILES, 224, 256, 1, 1, 2, 4.3, 1.32}, {NIMBLE_PRODUCT_TILES, 256, 256, 1, 1, 2, 4.7, 1.47},
 };
 
 // The most tile rows there can be: a group adds at most one that is not full, and only if it has a row.
@@ -29,7 +30,7 @@ static int64_t most_tile_rows(const ProductShape& s, int bm) {
 // Estimated microseconds.  How the rows fall on the groups is not known: each group is taken to have rows where there are
 // enough, and its last tile to be half full.  A workgroup of the streaming kernel takes a fixed time and then what its stages take to
 // arrive, 75 KB per us and compute unit; the workgroups of a compute unit share that.  Large tiles go round the chip, on a nearly
-// empty one (less power) with stages a quarter shorter; with groups half a turn more, for the last one that is not full.
+// empty one (less power) with stages a quarter shorter; groups may have a few tiles more than that.
 // Weights come at 4.8 TB/s where they come from memory.  Measured / estimated, dense in 8 bits with bias:
 //   rows x N x K         8 x 32      32 x 32      64 x 64, 4 waves  64 x 64, 2 waves  128 x 256    192 x 256    256 x 256
 //   1 x 4096 x 1024      2.9 / 3.5   3.7 / 3.9    6.1 / 6.7         7.4 / 7.2         9.7 / 12
@@ -49,9 +50,7 @@ static double product_us(const ProductShape& s, const Member& m) {
   double us;
   if (m.kernel == NIMBLE_PRODUCT_TILES) {
     const double full = tiles < kCUs ? tiles / kCUs : 1.0;
-    double turns = s.grouped && s.groups > 1 ? tiles / kCUs + 0.5 : ceil(tiles / kCUs);
-    if (turns < 1.0) turns = 1.0;
-    us = 4.0 + turns * (stages * m.stage_us * (0.75 + 0.25 * full) + m.fixed_us);
+    us = 4.0 + ceil(tiles * (s.grouped && s.groups > 1 ? 1.03 : 1.0) / kCUs) * (stages * m.stage_us * (0.75 + 0.25 * full) + m.fixed_us);
   } else {
     const double per_cu = tiles < kCUs ? 1.0 : tiles / kCUs;
     us = 1.0 + ceil(tiles / (kCUs * m.per_cu)) * m.fixed_us + per_cu * stages * (m.bm + m.bn) * 0.128 / 75.0;

@@ -23,9 +23,13 @@ int launch_product(const ProductArgs& g, const nimble_product_plan& p, hipStream
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, g, tiles_m, (int)tiles_n, group_m); };
     auto pick = [&](auto f32) {
       constexpr bool F = decltype(f32)::value;
-      if (p.bm == 256) launch(product_tile_kernel<T, GROUPS, F, 256, 256, 2>);
-      else if (p.bm == 192) launch(product_tile_kernel<T, GROUPS, F, 192, 256, 2>);
-      else launch(product_tile_kernel<T, GROUPS, F, 128, 256, 3>);
+      switch (p.bm) {
+        case 128: launch(product_tile_kernel<T, GROUPS, F, 128, 256, 3>); break;
+        case 160: launch(product_tile_kernel<T, GROUPS, F, 160, 256, 2>); break;
+        case 192: launch(product_tile_kernel<T, GROUPS, F, 192, 256, 2>); break;
+        case 224: launch(product_tile_kernel<T, GROUPS, F, 224, 256, 2>); break;
+        default: launch(product_tile_kernel<T, GROUPS, F, 256, 256, 2>); break;
+      }
     };
     if (g.out_f32) pick(std::true_type{});
     else pick(std::false_type{});

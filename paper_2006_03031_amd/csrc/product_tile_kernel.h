@@ -103,7 +103,7 @@ __device__ __forceinline__ V read_sum(const V& sum) {
 // Bias (bf16), column scales and row scales of a tile, in LDS.
 template <int BM, int BN>
 struct TileValues {
-  float w_scale[BN], x_scale[BM];
+  float w_scale[BN], x_scale[(BM + 63) / 64 * 64];  // (they come in pieces of 64)
   u16 bias[BN];
 };
 template <int BM, int BN, int S>
@@ -210,7 +210,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
       if (wave < BN / 64)
         dma4_buffer((uint32_t)(wave * 256 + lane * 4), descriptor(g.w_scale + c0, (uint32_t)columns * 4u),
                     __builtin_amdgcn_readfirstlane(lds_addr_of(to->w_scale)) + wave * 256);
-      if (wave < BM / 64)
+      if (wave < (BM + 63) / 64)
         dma4_buffer((uint32_t)(wave * 256 + lane * 4), descriptor(g.x_scale + t.row0, (uint32_t)t.rows * 4u),
                     __builtin_amdgcn_readfirstlane(lds_addr_of(to->x_scale)) + wave * 256);
     }

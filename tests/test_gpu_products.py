@@ -3,7 +3,8 @@
 Tolerances, from the roundings on the way (u = 2^-24 for f32; a second-order term is far below the slack of 1.01):
   8 bits: the sum is exact; to f32 u, product of the two scales u, their product with the sum u, sum with the bias u of the result.
   bf16:   K products, exact in f32, added in some order: K u sum |x w| at most; the bias as above.
-  GELU:   its fit is within 2.5e-5 of the erf form, its exp2 and reciprocal within 2^-21 of the value, its slope at most 1.13.
+  GELU:   its fit is within 2.5194e-5 of the erf form (test_the_gelus_fit evaluates both in float64 over every argument, on the
+          CPU), its exp2 and reciprocal within 2^-21 of the value, its slope at most 1.13.
   output in bf16: half a step, 2^-8 of the value."""
 import math
 import zlib
@@ -16,6 +17,7 @@ torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
 U = 2.0 ** -24
+FIT = 2.52e-5
 EPIS = {"none": nb.EPI_NONE, "bias": nb.EPI_BIAS, "gelu": nb.EPI_BIAS_GELU_ERF}
 DTYPES = {nb.BF16: torch.bfloat16, nb.F32: torch.float32}
 KEPT = 768.0   # content of rows and of memory that a call has to leave alone
@@ -64,7 +66,7 @@ def _reference(x, w, xs, ws, bias, epi):
     v = s if bias is None else s + bias.double()
     err = 1.01 * (err + U * v.abs()) + 1e-37
     if epi == "gelu":
-        err = 1.13 * err + 2.5e-5 + 2.0 ** -21 * v.abs()
+        err = 1.13 * err + FIT + 2.0 ** -21 * v.abs()
         v = 0.5 * v * (1 + torch.erf(v * math.sqrt(0.5)))
     return v, err
 
@@ -279,6 +281,58 @@ def test_offsets_that_do_not_keep_to_the_rows(rt, cuts, int8):
     else:
         rt.grouped_dense(_normal(g, (R, K)), _normal(g, (3, N, K)), None, offsets, nb.EPI_NONE, nb.F32, out=y)
     assert bool(torch.isfinite(y).all()) and bool((behind == KEPT).all())
+
+
+@pytest.mark.parametrize("epi", ["none", "gelu"])
+def test_no_k_at_all(rt, epi):
+    """Sums of nothing are 0: what comes out is the bias (or its GELU)."""
+    M, N, E = 70, 40, 3
+    bias = None if epi == "none" else _normal(_gen(9), (E, N))
+    x, w, xs, ws = (torch.empty((M, 0), dtype=torch.int8, device="cuda"), torch.empty((E, N, 0), dtype=torch.int8, device="cuda"),
+                    torch.ones(M, device="cuda"), torch.ones((E, N), device="cuda"))
+    off = torch.tensor([0, 30, 30, M], device="cuda")
+    group = torch.tensor([0] * 30 + [2] * 40, device="cuda")
+    v = torch.zeros((M, N), dtype=torch.float64, device="cuda") if bias is None else bias.double()[group]
+    if epi == "gelu":
+        v = 0.5 * v * (1 + torch.erf(v * math.sqrt(0.5)))
+    b0 = None if bias is None else bias[0]
+    err = FIT + 2.0 ** -21 * (v.abs() if bias is None else bias.double()[group].abs())
+    for y in (rt.grouped_dense_i8(x, xs, w, ws, bias, off, EPIS[epi], nb.F32), rt.grouped_dense(x.bfloat16(), w.bfloat16(), bias, off, EPIS[epi], nb.F32)):
+        _check(y, v, err)
+    _check(rt.dense_i8(x[:30], xs[:30], w[0], ws[0], b0, EPIS[epi], nb.F32), v[:30], err[:30])
+
+
+# Byte offsets past 2^32 in each operand: the streaming, the large-tile and the any-alignment kernel.
+@pytest.mark.parametrize("M,N,K", [(300000, 24, 16384), (600000, 16, 8191), (140000, 16384, 192), (24, 300000, 16384), (530000, 4099, 64)])
+def test_operands_past_4_gib(rt, M, N, K):
+    g = _gen(M, N, K)
+    x = torch.randint(-128, 128, (M, K), dtype=torch.int8, device="cuda", generator=g)
+    w = torch.randint(-128, 128, (N, K), dtype=torch.int8, device="cuda", generator=g)
+    xs, ws = _scales(g, (M,)), _scales(g, (N,))
+    y = rt.dense_i8(x, xs, w, ws, None, nb.EPI_NONE)
+    rows = torch.tensor(sorted({0, 1, M // 3, M // 2, M - 2, M - 1}), device="cuda")
+    v, err = _reference(x[rows], w, xs[rows], ws, None, "none")
+    _check(y[rows], v, err)
+    columns = torch.tensor(sorted({0, 1, N // 3, N // 2, N - 2, N - 1}), device="cuda")
+    v, err = _reference(x[-50:], w[columns], xs[-50:], ws[columns], None, "none")
+    _check(y[-50:][:, columns], v, err)
+    del y
+    torch.cuda.empty_cache()
+
+
+def test_grouped_weights_past_4_gib(rt):
+    """The last of many experts lies past 2^32 bytes of weights; a row for it, one for the first."""
+    E, N, K = 300, 2048, 4096
+    w = torch.zeros((E, N, K), dtype=torch.bfloat16, device="cuda")
+    g = _gen(1)
+    w[0], w[E - 1] = _normal(g, (N, K), 0.02), _normal(g, (N, K), 0.02)
+    for R in (2, 700):
+        x = _normal(g, (R, K))
+        off = torch.full((E + 1,), R // 2, dtype=torch.int64, device="cuda")
+        off[0], off[E] = 0, R
+        y = rt.grouped_dense(x, w, None, off, nb.EPI_NONE, nb.F32)
+        _check(y[:R // 2], *_reference(x[:R // 2], w[0], None, None, None, "none"))
+        _check(y[R // 2:], *_reference(x[R // 2:], w[E - 1], None, None, None, "none"))
 
 
 # --------------------------------------------------------------------------------------------- together

@@ -133,3 +133,20 @@ def test_the_grid_holds_the_tiles_of_every_split(in_dtype):
 def test_plan_struct_matches_the_header():
     from paper_2006_03031_amd import binding
     assert ctypes.sizeof(binding._CProductPlan) == 32
+
+
+def test_the_gelus_fit():
+    """The constants of the epilogue's GELU (v sigmoid of an odd quintic, csrc/device_common.h) in float64 against the erf form: the GPU
+    tests allow 2.52e-5 for it.  Beyond 9.5 either is v or 0 to within 1e-18."""
+    import math
+    import os
+    import re
+    from paper_2006_03031_amd import build
+    with open(os.path.join(build.CSRC, "device_common.h")) as f:
+        body = re.search(r"float gelu_exponent\(float v\) \{(.*?)\n\}", f.read(), re.S).group(1)
+    c2, c1, c0 = (torch.tensor(float(c)).double() for c in re.findall(r"(-?\d\.\d+)f", body)[-3:])
+    v = torch.linspace(-9.5, 9.5, 2000001, dtype=torch.float64)
+    t = (v * v).clamp(max=81.0)
+    fit = v / (1 + torch.exp2(((c2 * t + c1) * t + c0) * v))
+    worst = (fit - 0.5 * v * (1 + torch.erf(v * math.sqrt(0.5)))).abs().max().item()
+    assert 2.5e-5 < worst < 2.52e-5, worst
