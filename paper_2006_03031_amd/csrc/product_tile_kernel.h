@@ -23,7 +23,8 @@ namespace nimble {
 // the end of K in the last stage.  Stores past the last row or column are dropped in the same way.  So every tile runs the same code
 // whatever its number of rows.
 //   Tiles are told from the offsets of the groups (GroupMap), which the workgroup reads once.
-//   Measured, 8 bits / bf16: 8192^3 396 / 737 us (2780 / 1490 T); 8192 x 4096 x 1024 with bias 36.4 / 62, with GELU 45.3 / 72.
+//   Measured, 8 bits / bf16: 8192^3 396 / 737 us (2780 / 1490 T); 8192 x 4096 x 1024 with bias 36.4 / 62, with GELU 45.3 / 72 (half of
+// 16384 rows).
 // ---------------------------------------------------------------------------
 #define NIMBLE_INLINE __attribute__((always_inline))
 template <int N>

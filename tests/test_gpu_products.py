@@ -283,6 +283,52 @@ def test_offsets_that_do_not_keep_to_the_rows(rt, cuts, int8):
     assert bool(torch.isfinite(y).all()) and bool((behind == KEPT).all())
 
 
+# Each height of the large tiles, as the dispatch takes it: a last tile that is not full, N not of whole tiles, K not of whole stages,
+# tiles that follow others; K of exactly the stages that are loaded ahead.
+@pytest.mark.parametrize("bm,M,N,K", [(128, 4100, 520, 656), (160, 4100, 2040, 656), (192, 3000, 4088, 656), (224, 2048, 6136, 656),
+                                      (256, 8177, 4088, 656), (256, 8177, 4096, 256), (128, 4100, 520, 384)])
+@pytest.mark.parametrize("epi,out", [("none", nb.F32), ("gelu", nb.BF16), ("bias", nb.BF16)])
+def test_dense_i8_in_large_tiles(rt, bm, M, N, K, epi, out):
+    p = nb.product_plan(M, None, N, K)
+    assert (p.kernel, p.bm) == (1, bm)
+    g = _gen(M, N, K)
+    x, w, xs, ws = _codes(g, (M, K)), _codes(g, (N, K)), _scales(g, (M,)), _scales(g, (N,)) / K ** 0.5
+    bias = None if epi == "none" else _normal(g, (N,))
+    y, behind = _guarded((M, N), DTYPES[out])
+    rt.dense_i8(x, xs, w, ws, bias, EPIS[epi], out, out=y)
+    _check(y, *_reference(x, w, xs, ws, bias, epi))
+    assert bool((behind == KEPT).all())
+
+
+@pytest.mark.parametrize("bm,R,E,N,K", [(128, 1200, 2, 4088, 656), (160, 1500, 8, 4088, 656), (192, 2048, 8, 4088, 656), (224, 3000, 3, 4088, 656),
+                                        (256, 2048, 3, 6136, 656)])
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("epi,out", [("none", nb.F32), ("gelu", nb.BF16)])
+def test_grouped_in_large_tiles(rt, bm, R, E, N, K, int8, epi, out):
+    p = nb.product_plan(R, E, N, K, nb.I8 if int8 else nb.BF16)
+    assert (p.kernel, p.bm) == (1, bm)
+    g = _gen(R, E, N, K)
+    cuts = [7] + sorted(torch.randint(7, R - 8, (E - 1,), generator=g, device="cuda").tolist()) + [R - 9]
+    offsets = torch.tensor(cuts, device="cuda")
+    bias = None if epi == "none" else _normal(g, (E, N))
+    y, behind = _guarded((R, N), DTYPES[out])
+    for turn in range(2):   # the second time the groups lie elsewhere, the rest of the output is as it was
+        if int8:
+            x, w, xs, ws = _codes(g, (R, K)), _codes(g, (E, N, K)), _scales(g, (R,)), _scales(g, (E, N)) / K ** 0.5
+            rt.grouped_dense_i8(x, xs, w, ws, bias, offsets, EPIS[epi], out, out=y)
+        else:
+            x, w, xs, ws = _normal(g, (R, K)), _normal(g, (E, N, K), K ** -0.5), None, None
+            rt.grouped_dense(x, w, bias, offsets, EPIS[epi], out, out=y)
+        for e in range(E):
+            lo, hi = cuts[e], cuts[e + 1]
+            if lo < hi:
+                _check(y[lo:hi], *_reference(x[lo:hi], w[e], xs[lo:hi] if int8 else None, ws[e] if int8 else None,
+                                             None if bias is None else bias[e], epi))
+        assert bool((y[:cuts[0]] == KEPT).all()) and bool((y[cuts[E]:] == KEPT).all()) and bool((behind == KEPT).all())
+        cuts = [7] + [R - 9] * E   # all rows in the first group
+        offsets.copy_(torch.tensor(cuts))
+
+
 @pytest.mark.parametrize("epi", ["none", "gelu"])
 def test_no_k_at_all(rt, epi):
     """Sums of nothing are 0: what comes out is the bias (or its GELU)."""
