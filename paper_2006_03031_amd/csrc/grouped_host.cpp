@@ -9,17 +9,17 @@ static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // The members of the family that need rows of whole 16 bytes: tile, waves among which K is divided, workgroups that share a compute unit,
 // stages that are loaded ahead; microseconds of a workgroup that do not depend on K (launch, first loads, sums and stores; of a large tile its
-// end) and of a large tile per stage of 128 bytes of K on a full chip.
+// end); KB per us at which a compute unit's stages arrive (streaming), or microseconds of a stage of 128 bytes of K on a full chip (large tiles).
 struct Member {
   int kernel, bm, bn, k_waves, per_cu, ahead;
-  double fixed_us, stage_us;
+  double fixed_us, rate;
 };
 static const Member kMembers[] = {
-    {NIMBLE_PRODUCT_STREAM, 8, 32, 4, 3, 0, 2.0, 0},      {NIMBLE_PRODUCT_STREAM, 16, 32, 4, 3, 0, 2.0, 0},
-    {NIMBLE_PRODUCT_STREAM, 32, 32, 4, 2, 0, 2.2, 0},     {NIMBLE_PRODUCT_STREAM, 64, 64, 4, 1, 0, 4.0, 0},
-    {NIMBLE_PRODUCT_STREAM, 64, 64, 2, 2, 0, 4.5, 0},     {NIMBLE_PRODUCT_TILES, 128, 256, 1, 1, 3, 2.6, 0.90},
-    {NIMBLE_PRODUCT_TILES, 160, 256, 1, 1, 2, 3.2, 1.01}, {NIMBLE_PRODUCT_TILES, 192, 256, 1, 1, 2, 3.8, 1.15},
-    {NIMBLE_PRODUCT_TILES, 224, 256, 1, 1, 2, 4.3, 1.32}, {NIMBLE_PRODUCT_TILES, 256, 256, 1, 1, 2, 4.7, 1.47},
+    {NIMBLE_PRODUCT_STREAM, 8, 32, 4, 3, 0, 2.0, 66},    {NIMBLE_PRODUCT_STREAM, 16, 32, 4, 3, 0, 2.0, 75},
+    {NIMBLE_PRODUCT_STREAM, 32, 32, 4, 2, 0, 2.2, 100},  {NIMBLE_PRODUCT_STREAM, 64, 64, 4, 1, 0, 4.3, 93},
+    {NIMBLE_PRODUCT_STREAM, 64, 64, 2, 2, 0, 3.5, 56},   {NIMBLE_PRODUCT_TILES, 128, 256, 1, 1, 3, 2.6, 0.67},
+    {NIMBLE_PRODUCT_TILES, 160, 256, 1, 1, 2, 3.1, 0.91}, {NIMBLE_PRODUCT_TILES, 192, 256, 1, 1, 2, 2.8, 1.09},
+    {NIMBLE_PRODUCT_TILES, 224, 256, 1, 1, 2, 3.6, 1.22}, {NIMBLE_PRODUCT_TILES, 256, 256, 1, 1, 2, 4.1, 1.43},
 };
 
 // The most tile rows there can be: a group adds at most one that is not full, and only if it has a row.
@@ -28,19 +28,19 @@ static int64_t most_tile_rows(const ProductShape& s, int bm) {
 }
 
 // Estimated microseconds.  How the rows fall on the groups is not known: each group is taken to have rows where there are
-// enough, and its last tile to be half full.  A workgroup of the streaming kernel takes a fixed time and then what its stages take to
-// arrive, 75 KB per us and compute unit; the workgroups of a compute unit share that.  Large tiles go round the chip, on a nearly
-// empty one (less power) with stages a quarter shorter; groups may have a few tiles more than that.
-// Weights come at 4.8 TB/s where they come from memory.  Measured / estimated, dense in 8 bits with bias:
-//   rows x N x K         8 x 32      32 x 32      64 x 64, 4 waves  64 x 64, 2 waves  128 x 256    192 x 256    256 x 256
-//   1 x 4096 x 1024      2.9 / 3.5   3.7 / 3.9    6.1 / 6.7         7.4 / 7.2         9.7 / 12
-//   200 x 1024 x 4096                6.2 / 6.6    9.6 / 12          13.6 / 12         24 / 28
-//   512 x 1024 x 4096                9.9 / 10     10.5 / 12         13.8 / 12         24.5 / 28
-//   512 x 4096 x 1024                15.2 / 16.6  12.3 / 12.4       9.7 / 8.9         10.6 / 12
-//   8192 x 1024 x 4096                                                                31.8 / 35    37.7 / 42    45.8 / 50
-//   16384 x 1024 x 4096                                                               61.7 / 67    71.3 / 85    54.5 / 56
-//   8192 x 4096 x 1024                                                                41.3 / 43    40.7 / 43    36.4 / 37
-// and 16354 rows over 32 groups x 1024 x 4096                                         102 / 90     91.6 / 89    107 / 95
+// enough, and its last tile to be half full.  The workgroups of a compute unit share the rate at which stages arrive.  Large tiles go
+// round the chip, on a nearly empty one (less power) with stages a quarter shorter; groups may have a few tiles more than that.
+// Weights come at 4.8 TB/s where they come from memory, and then a quarter of the estimate still tells the members apart.
+// The constants are a fit to the ten members' times on 100 shapes of either type (K = 128 .. 8192, N = 128 .. 8192, 1 .. 16354 rows over
+// 1 .. 64 groups), where the choice costs 1 % more than the best member, and on 100 others 3 %.  Measured, dense in 8 bits with bias:
+//   rows x N x K         8 x 32   32 x 32   64 x 64, 4 waves  64 x 64, 2 waves  128 x 256   192 x 256   256 x 256
+//   1 x 4096 x 1024      2.9      3.7       6.1               7.4               9.7
+//   200 x 1024 x 4096             6.2       9.6               13.6              24
+//   512 x 1024 x 4096             9.9       10.5              13.8              24.5
+//   512 x 4096 x 1024             15.2      12.3              9.7               10.6
+//   8192 x 1024 x 4096                                                          31.8        37.7        45.8
+//   16384 x 1024 x 4096                                                         61.7        71.3        54.5
+//   8192 x 4096 x 1024                                                          41.3        40.7        36.4
 static double product_us(const ProductShape& s, const Member& m) {
   const double kCUs = kComputeUnits;
   const double live = s.grouped ? (double)(s.groups < s.rows ? s.groups : s.rows) : 1.0;
@@ -50,10 +50,11 @@ static double product_us(const ProductShape& s, const Member& m) {
   double us;
   if (m.kernel == NIMBLE_PRODUCT_TILES) {
     const double full = tiles < kCUs ? tiles / kCUs : 1.0;
-    us = 4.0 + ceil(tiles * (s.grouped && s.groups > 1 ? 1.03 : 1.0) / kCUs) * (stages * m.stage_us * (0.75 + 0.25 * full) + m.fixed_us);
+    const double walk = (stages < m.ahead ? m.ahead : stages) * m.rate * (0.73 + 0.27 * full);
+    us = 4.4 + ceil(tiles * (s.grouped && s.groups > 1 ? 1.03 : 1.0) / kCUs) * (walk + m.fixed_us);
   } else {
     const double per_cu = tiles < kCUs ? 1.0 : tiles / kCUs;
-    us = 1.0 + ceil(tiles / (kCUs * m.per_cu)) * m.fixed_us + per_cu * stages * (m.bm + m.bn) * 0.128 / 75.0;
+    us = 1.0 + ceil(tiles / (kCUs * m.per_cu)) * m.fixed_us + per_cu * stages * (m.bm + m.bn) * 0.128 / m.rate;
   }
   const double weights_us = live * (double)s.N * (double)s.row_bytes() / 4.8e6;
   return (us > weights_us ? us : weights_us) + 0.25 * us;
@@ -61,13 +62,12 @@ static double product_us(const ProductShape& s, const Member& m) {
 
 int plan_product(const ProductShape& s, nimble_product_plan* p) {
   nimble_product_plan out{};
-  const int64_t rb = s.row_bytes(), stages = ceil_div(rb, 128);
+  const int64_t rb = s.row_bytes();
   const Member* best = nullptr;
   double best_us = 0;
   if (rb % 16 == 0 && rb > 0 && rb <= kMostTileRowBytes) {
     for (const Member& m : kMembers) {
-      // a large tile's first loads must not reach a partly filled last stage, and its rows are stored in whole 16 bytes
-      if (m.kernel == NIMBLE_PRODUCT_TILES && (s.N % 8 != 0 || s.N > kMostTileColumns || stages < m.ahead + (rb % 128 ? 1 : 0))) continue;
+      if (m.kernel == NIMBLE_PRODUCT_TILES && (s.N % 8 != 0 || s.N > kMostTileColumns)) continue;  // (rows are stored in whole 16 bytes)
       const double us = product_us(s, m);
       if (!best || us < best_us) best = &m, best_us = us;
     }

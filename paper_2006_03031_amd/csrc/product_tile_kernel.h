@@ -143,7 +143,11 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
     find_tile<BM, BN>(g, map, tm, tn, tile);
   };
 
-  const int KS = (g.row_bytes + 127) >> 7;
+  // Stages of a tile: as many at least as are loaded ahead, those past the end of K of zeros.  `tight`: the pieces past the end of K lie
+  // in these first stages.
+  int KS = __builtin_amdgcn_readfirstlane(max((g.row_bytes + 127) >> 7, S));
+  asm volatile("" : "+s"(KS));  // (the compiler, once it knows that S stages follow each other, spills)
+  const bool tight = KS == S && g.row_bytes < S * 128;
   const int tid = threadIdx.x;
   const int lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -169,14 +173,22 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
     const int h = of_a(u) ? u >= H0 : u >= H0 + G, base = of_a(u) ? (h ? u - TN - H0 : u) * 32 : (u - H0 - G * h) * 32;
     return of_a(u) ? a_row(h, base + q) : b_row(h, base + q);
   };
-  auto set_off = [&] {
+  // for the loads of a stage: pieces past the end of K are asked for past the end of the descriptor.  (The lane's row goes through an
+  // empty statement: else the compiler keeps the addresses of every place that sets them alive beside each other, and spills.)
+  auto set_off = [&](int stage) {
+    int row = ld_row;
+    asm volatile("" : "+v"(row));
+    const int left = g.row_bytes - stage * 128;
 #pragma unroll
-    for (int u = 0; u < LDT; ++u) off[u] = (uint32_t)(row_of(u, ld_row) * g.row_bytes + (of_a(u) ? ld_a : ld_b) * 16);
+    for (int u = 0; u < LDT; ++u) {
+      const int c = (of_a(u) ? ld_a : ld_b) * 16;
+      off[u] = c < left ? (uint32_t)(row_of(u, row) * g.row_bytes + c) : 0x80000000u;
+    }
   };
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_addr_of(smem));
 #pragma unroll
   for (int u = 0; u < LDT; ++u) lds_off[u] = (of_a(u) ? 0 : BM * 128) + row_of(u, wave * 8) * 128;
-  set_off();
+  set_off(0);
   auto a_desc = [&](const ProductTile& t) {
     return descriptor(g.x + (long long)t.row0 * g.row_bytes, (uint32_t)t.rows * (uint32_t)g.row_bytes);
   };
@@ -273,6 +285,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
   fetch_values(tile, values);
 #pragma unroll
   for (int s = 0; s < S; ++s) {
+    if (tight) set_off(s);
 #pragma unroll
     for (int u = 0; u < LDT; ++u) dma16_buffer(off[u], src(u), s * 128, lds0 + s * SLOT + lds_off[u]);
   }
@@ -351,19 +364,17 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
   at = S * 128;
   int slot = 0, parity = 0;
   bool stored = false;  // the tile before has issued its stores behind this one's first S stages
-  const int left = g.row_bytes - (KS - 1) * 128;  // bytes of the last stage
+  const bool tail = !tight && (g.row_bytes & 127) != 0;
   for (int t = blockIdx.x;; t += gridDim.x) {
     const bool follows = t + (int)gridDim.x < tiles_total;
     // Stage ks loads stage ks + S of this tile: of its last one the pieces past the end of K are zeros; behind it come the next
     // tile's first ones (there is none: nothing is read).
     auto run_stage = [&](int ks, auto first_tag) NIMBLE_INLINE {
-      if (ks == KS - S - 1 && left < 128) {
-#pragma unroll
-        for (int u = 0; u < LDT; ++u) off[u] = (of_a(u) ? ld_a : ld_b) * 16 < left ? off[u] : 0x80000000u;
-      }
+      if (tail && ks == KS - S - 1) set_off(KS - 1);
+      if (tight) set_off(ks);  // (it loads that stage of the next tile)
       if (ks == KS - S) {
         at = 0;
-        if (left < 128) set_off();
+        if (tail) set_off(0);
         a_src = b_src = descriptor(g.x, 0);
         if (follows) {
           tile_at(t + (int)gridDim.x, next_tile);

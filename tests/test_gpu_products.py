@@ -284,9 +284,11 @@ def test_offsets_that_do_not_keep_to_the_rows(rt, cuts, int8):
 
 
 # Each height of the large tiles, as the dispatch takes it: a last tile that is not full, N not of whole tiles, K not of whole stages,
-# tiles that follow others; K of exactly the stages that are loaded ahead.
+# tiles that follow others; K of exactly the stages that are loaded ahead, and of fewer.
 @pytest.mark.parametrize("bm,M,N,K", [(128, 4100, 520, 656), (160, 4100, 2040, 656), (192, 3000, 4088, 656), (224, 2048, 6136, 656),
-                                      (256, 8177, 4088, 656), (256, 8177, 4096, 256), (128, 4100, 520, 384)])
+                                      (256, 8177, 2040, 656), (256, 8177, 2040, 256), (128, 4100, 520, 384), (128, 4100, 520, 272),
+                                      (128, 5000, 520, 48), (160, 4100, 4088, 80), (192, 4100, 2040, 128), (224, 2048, 6136, 144),
+                                      (256, 5000, 6136, 48), (256, 5000, 6136, 16)])
 @pytest.mark.parametrize("epi,out", [("none", nb.F32), ("gelu", nb.BF16), ("bias", nb.BF16)])
 def test_dense_i8_in_large_tiles(rt, bm, M, N, K, epi, out):
     p = nb.product_plan(M, None, N, K)
@@ -300,8 +302,9 @@ def test_dense_i8_in_large_tiles(rt, bm, M, N, K, epi, out):
     assert bool((behind == KEPT).all())
 
 
-@pytest.mark.parametrize("bm,R,E,N,K", [(128, 1200, 2, 4088, 656), (160, 1500, 8, 4088, 656), (192, 2048, 8, 4088, 656), (224, 3000, 3, 4088, 656),
-                                        (256, 2048, 3, 6136, 656)])
+@pytest.mark.parametrize("bm,R,E,N,K", [(128, 300, 3, 6136, 656), (160, 1500, 8, 4088, 656), (192, 2048, 8, 4088, 656), (224, 3000, 3, 4088, 656),
+                                        (256, 2048, 3, 6136, 656), (128, 700, 3, 3064, 48), (160, 4100, 8, 4088, 128), (192, 1200, 3, 6136, 80),
+                                        (224, 6000, 3, 2040, 144), (256, 1500, 8, 6136, 48)])
 @pytest.mark.parametrize("int8", [False, True])
 @pytest.mark.parametrize("epi,out", [("none", nb.F32), ("gelu", nb.BF16)])
 def test_grouped_in_large_tiles(rt, bm, R, E, N, K, int8, epi, out):
