@@ -78,8 +78,11 @@ int plan_product(const ProductShape& s, nimble_product_plan* p) {
     out.bn = best->bn;
     out.k_waves = best->k_waves;
     out.block = best->kernel == NIMBLE_PRODUCT_TILES ? 256 : 64u * (unsigned)best->k_waves;
-  } else {  // 8177 x 4096 x 1024 in 64 x 64 tiles 198 us; up to 16 rows of a group in 16 x 16
-    const bool few = s.rows <= 16 * (s.grouped ? s.groups : 1);
+  } else {
+    // 16 x 16 tiles where a group has no more than 16 rows or the chip holds all of them at once: 64 x 4096 x 1003 in 8 bits 8.4 us, in 64 x 64
+    // 10.9; 200 x 1024 x 4099 21.8 / 27.5; beyond that 512 x 1024 x 4096 35 / 20
+    const int64_t live = s.grouped ? (s.groups < s.rows ? s.groups : s.rows) : 1;
+    const bool few = s.rows <= 16 * live || most_tile_rows(s, 16) * ceil_div(s.N, 16) <= 4 * kComputeUnits;
     out.kernel = NIMBLE_PRODUCT_DIRECT;
     out.bm = out.bn = few ? 16 : 64;
     out.k_waves = few ? 8 : 4;

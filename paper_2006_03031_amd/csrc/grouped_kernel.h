@@ -132,6 +132,23 @@ __device__ __forceinline__ uint4 load16(const unsigned char* row, int at, int ro
   return v;
 }
 
+// 16 bytes from an address that is a whole number of words.
+__device__ __forceinline__ uint4 load16_at_word(const void* p) {
+  uint4 v;
+  __builtin_memcpy(&v, __builtin_assume_aligned(p, 4), 16);
+  return v;
+}
+// 16 bytes from any address, by words that start at whole words: loads that do not come from the L2 at a third of the rate.  Up to three
+// bytes ahead of them (of the row before) and three behind them are read too.
+__device__ __forceinline__ uint4 load16_words(const unsigned char* p) {
+  const uint32_t by = (uint32_t)(uintptr_t)p & 3u;
+  const uint32_t* a = (const uint32_t*)(p - by);
+  const uint4 v = load16_at_word(a);
+  const uint32_t next = a[by ? 4 : 3];
+  return make_uint4(__builtin_amdgcn_alignbyte(v.y, v.x, by), __builtin_amdgcn_alignbyte(v.z, v.y, by),
+                    __builtin_amdgcn_alignbyte(v.w, v.z, by), __builtin_amdgcn_alignbyte(next, v.w, by));
+}
+
 // Four consecutive outputs of a row from n on, as many as there are; `v` is scaled and has its bias.
 __device__ __forceinline__ void store4(const ProductArgs& g, float (&v)[4], long long row, int n) {
   const int n4 = g.N - n;
@@ -178,7 +195,10 @@ __device__ __forceinline__ bool find_tile(const ProductArgs& g, const GroupMap<M
 
 // ---------------------------------------------------------------------------
 // Any alignment: TM x TN blocks of 16 x 16 per workgroup, KW waves that take pieces of 64 bytes of K in turn, operands from
-// memory straight into the registers that the matrix instruction reads; the waves' sums meet in LDS.
+// memory straight into the registers that the matrix instruction reads; the waves' sums meet in LDS.  Bound: the L2s' answers to loads of rows
+// that start anywhere.  Loaded by whole words and shifted into place, not at their own addresses: 8177 x 4096 x 1003 in 8 bits 218 us,
+// 282; 200 x 1024 x 4099 27.5, 48.4; 4000 rows over 8 groups x 1024 x 1001 in bf16 61, 87.  A second register set for the pieces ahead took a
+// workgroup's place on the compute unit: 365 us.
 // ---------------------------------------------------------------------------
 template <typename T, int GROUPS, int TM, int TN, int KW>
 __global__ void __launch_bounds__(KW * 64) product_direct_kernel(ProductArgs g, unsigned tiles, unsigned tiles_n) {
@@ -208,16 +228,23 @@ __global__ void __launch_bounds__(KW * 64) product_direct_kernel(ProductArgs g, 
       for (int j = 0; j < TM; ++j) acc[i][j] = Acc{0, 0, 0, 0};
     uint4 x[TM], w[TN];
     int at = wave * 64;
-    for (; at + 64 <= g.row_bytes; at += KW * 64) {
+    auto walk = [&](auto whole_words) {
+      constexpr bool kWords = decltype(whole_words)::value;
+      for (; at + 64 + (kWords ? 0 : 3) <= g.row_bytes; at += KW * 64) {
 #pragma unroll
-      for (int i = 0; i < TN; ++i) __builtin_memcpy(&w[i], wp[i] + at + fr_at, 16);
+        for (int i = 0; i < TN; ++i) w[i] = kWords ? load16_at_word(wp[i] + at + fr_at) : load16_words(wp[i] + at + fr_at);
 #pragma unroll
-      for (int j = 0; j < TM; ++j) __builtin_memcpy(&x[j], xp[j] + at + fr_at, 16);
+        for (int j = 0; j < TM; ++j) x[j] = kWords ? load16_at_word(xp[j] + at + fr_at) : load16_words(xp[j] + at + fr_at);
 #pragma unroll
-      for (int i = 0; i < TN; ++i)
+        for (int i = 0; i < TN; ++i)
 #pragma unroll
-        for (int j = 0; j < TM; ++j) acc[i][j] = T::mfma(w[i], x[j], acc[i][j]);
-    }
+          for (int j = 0; j < TM; ++j) acc[i][j] = T::mfma(w[i], x[j], acc[i][j]);
+      }
+    };
+    if ((g.row_bytes & 3) == 0)
+      walk(std::true_type{});
+    else
+      walk(std::false_type{});
     if (at < g.row_bytes) {
 #pragma unroll
       for (int i = 0; i < TN; ++i) w[i] = load16(wp[i], at + fr_at, g.row_bytes);
