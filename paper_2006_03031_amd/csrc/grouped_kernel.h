@@ -149,10 +149,42 @@ __device__ __forceinline__ uint4 load16_words(const unsigned char* p) {
                     __builtin_amdgcn_alignbyte(v.w, v.z, by), __builtin_amdgcn_alignbyte(next, v.w, by));
 }
 
+// gelu(v) = v/2 (1 + erf(v / sqrt 2)) = max(v, 0) - |v| Q(|v|), Q the upper tail of the normal distribution.  log2 Q is smooth for
+// x >= 0 and -1 at 0, so Q is 2^P(x) with a polynomial P: one transcendental instruction per value, and the roundings of a small tail do not
+// reach a result that is not small.  P is the minimax fit of degree 10 to log2 Q on [0, 8], its error weighted by 1 / (1 + (x/2)^6).  With the
+// roundings of f32 and of the hardware's exp2 (1 ulp) a result is off by at most 2^-21 of itself for v >= 0 and by 2^-21 (1 + (v/2)^6) of itself
+// for -8 <= v < 0; f32 outputs ask for that, and bf16 ones are then the rounded exact ones but for values next to a border.  Below
+// -8 P falls on to minus infinity and the result stays under 2^-46; above 8, where it is v, x stays 8, so that infinity less nothing is infinity.
+// NaN stays NaN, and minus infinity gives NaN as the formula does.
+//   N values side by side, step by step (the empty statements keep the N results of a step together), as epilogue_of does it.
+template <int N>
+__device__ __forceinline__ void gelu_of(float (&v)[N]) {
+  constexpr float kTail[11] = {-1.0f,           -1.15110886f,    -0.459177405f,  -0.0525782481f,  0.00715400605f, -0.000172875938f,
+                               -0.000194635781f, 5.13012637e-05f, -6.58381487e-06f, 4.4570379e-07f, -1.26317756e-08f};
+  float x[N], p[N];
+  auto together = [&](float (&y)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+v"(y[i]));
+  };
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = fabsf(__builtin_elementwise_minimum(v[i], 8.0f)), p[i] = kTail[10];
+#pragma unroll
+  for (int k = 9; k >= 0; --k) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) p[i] = fmaf(p[i], x[i], kTail[k]);
+    together(p);
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) p[i] = __builtin_amdgcn_exp2f(p[i]);
+  together(p);
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = fmaf(-x[i], p[i], __builtin_elementwise_maximum(v[i], 0.0f));
+}
+
 // Four consecutive outputs of a row from n on, as many as there are; `v` is scaled and has its bias.
 __device__ __forceinline__ void store4(const ProductArgs& g, float (&v)[4], long long row, int n) {
   const int n4 = g.N - n;
-  if (g.epilogue == NIMBLE_EPI_BIAS_GELU_ERF) epilogue_of<true>(v);
+  if (g.epilogue == NIMBLE_EPI_BIAS_GELU_ERF) gelu_of(v);
   const long long at = row * g.N + n;
   if (g.out_f32) {
     float* y = (float*)g.y + at;

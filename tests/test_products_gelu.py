@@ -1,0 +1,106 @@
+"""The GELU of the 8-bit and the grouped products against float64.
+
+Tolerance: 2^-21 (1 + (min(v, 0) / 2)^6) of the value down to v = -8, below it 2^-46, as csrc/grouped_kernel.h states; the first test derives
+it from the constants there, in the arithmetic of f32.  Outputs in bf16: half a step, 2^-8 of the value, on top."""
+import math
+import os
+import re
+
+import pytest
+
+import paper_2006_03031_amd as nb
+
+torch = pytest.importorskip("torch")
+
+
+def _exact(v):
+    """float64: v Q(-v), by the complement so that small results keep their digits."""
+    v = v.double()
+    return 0.5 * v * torch.special.erfc(-v * math.sqrt(0.5))
+
+
+def _allowed(v, g):
+    tail = v.double().clamp(max=0)
+    return torch.where(v < -8, 2.0 ** -46, 2.0 ** -21 * (1 + (tail / 2) ** 6) * g.abs())
+
+
+def test_what_the_polynomial_and_f32_leave():
+    from paper_2006_03031_amd import build
+    with open(os.path.join(build.CSRC, "grouped_kernel.h")) as f:
+        body = re.search(r"kTail\[11\] = \{(.*?)\};", f.read(), re.S).group(1)
+    tail = [float(torch.tensor(float(c[:-1]), dtype=torch.float32)) for c in body.replace("\n", "").replace(" ", "").split(",")]
+    assert len(tail) == 11 and tail[0] == -1.0 and tail[10] < 0
+    v = torch.cat([torch.linspace(-40, 12, 2000001, dtype=torch.float64), -torch.logspace(-30, 18, 20001, dtype=torch.float64)]).float()
+    x = v.clamp(max=8).abs().double()
+    p = torch.full_like(x, tail[10])
+    for c in tail[9::-1]:      # (a product of two f32 is exact in f64)
+        p = (p * x + c).float().double()
+    g, off = _exact(v), 2.0 ** -23          # of the hardware's exp2
+    for q in (torch.exp2(p) * (1 + off), torch.exp2(p) * (1 - off)):
+        y = (v.double().clamp(min=0) - x * q).float().double()
+        assert bool(((y - g).abs() <= _allowed(v, g) + 2.0 ** -140).all())
+
+
+def _values():
+    v = torch.cat([torch.linspace(-9, 9, 6001), -torch.logspace(-6, 3, 500), torch.logspace(-6, 6, 500),
+                   torch.tensor([0.0, -0.0, 8.0, -8.0, 1e30, -1e30, 3e38, -3e38])])
+    return v[:v.numel() // 8 * 8]
+
+
+def _check(y, v):
+    g = _exact(v)
+    err = _allowed(v, g) + 2.0 ** -120      # (no results below the normal numbers)
+    if y.dtype == torch.bfloat16:
+        err = err + 2.0 ** -8 * (g.abs() + err)
+    bad = ~((y.cpu().double() - g).abs() <= err)
+    assert not bool(bad.any()), (v.expand_as(bad)[bad][:5], y.cpu()[bad][:5], g.expand_as(bad)[bad][:5])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("out", [nb.BF16, nb.F32])
+@pytest.mark.parametrize("M,K,kernel", [(1, 16, 2), (40, 32, 2), (3000, 48, 1), (1, 15, 0), (200, 7, 0)])
+def test_dense_i8(M, K, kernel, out):
+    """One code of 1 in each row and scales that are the values: the sums are the values themselves, times powers of two."""
+    from paper_2006_03031_amd import runtime as rt
+    v = _values()
+    N = v.numel()
+    assert nb.product_plan(M, None, N, K).kernel == kernel
+    x, w = torch.zeros((M, K), dtype=torch.int8), torch.zeros((N, K), dtype=torch.int8)
+    x[:, K - 1], w[:, K - 1] = 1, 1
+    xs = torch.exp2((torch.arange(M) % 5 - 4).float())
+    y = rt.dense_i8(x.cuda(), xs.cuda(), w.cuda(), v.cuda(), torch.zeros(N, dtype=torch.bfloat16, device="cuda"), nb.EPI_BIAS_GELU_ERF, out)
+    for m in sorted({0, 1, 2, 3, 4, M // 2, M - 1}):
+        if m < M:
+            _check(y[m], v * xs[m])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("out", [nb.BF16, nb.F32])
+@pytest.mark.parametrize("R,K,kernel", [(4, 8, 2), (1500, 32, 1), (30, 5, 0)])
+def test_grouped_dense(R, K, kernel, out):
+    from paper_2006_03031_amd import runtime as rt
+    v = _values().bfloat16()
+    N = v.numel()
+    assert nb.product_plan(R, 2, N, K, nb.BF16).kernel == kernel
+    x, w = torch.zeros((R, K), dtype=torch.bfloat16), torch.zeros((2, N, K), dtype=torch.bfloat16)
+    x[:, 0], w[0, :, 0], w[1, :, 0] = 1, v, v / 2
+    off, zero = torch.tensor([0, R // 2, R], device="cuda"), torch.zeros((2, N), dtype=torch.bfloat16, device="cuda")
+    y = rt.grouped_dense(x.cuda(), w.cuda(), zero, off, nb.EPI_BIAS_GELU_ERF, out)
+    for r in (0, R // 2 - 1, R // 2, R - 1):
+        _check(y[r], v.float() if r < R // 2 else v.float() / 2)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M,K", [(1, 16), (3000, 48), (1, 15)])
+def test_values_that_are_no_numbers(M, K):
+    """+inf stays, NaN stays, -inf is NaN, as v/2 (1 + erf) has it; nothing else in the row is touched."""
+    from paper_2006_03031_amd import runtime as rt
+    v = torch.linspace(-2, 2, 4096)
+    v[7], v[100], v[2001] = float("inf"), float("nan"), -float("inf")
+    x, w = torch.zeros((M, K), dtype=torch.int8, device="cuda"), torch.zeros((4096, K), dtype=torch.int8, device="cuda")
+    x[:, 0], w[:, 0] = 1, 1
+    y = rt.dense_i8(x, torch.ones(M, device="cuda"), w, v.cuda(), torch.zeros(4096, dtype=torch.bfloat16, device="cuda"),
+                    nb.EPI_BIAS_GELU_ERF, nb.F32).cpu()
+    assert bool((y[:, 7] == float("inf")).all()) and bool(y[:, 100].isnan().all()) and bool(y[:, 2001].isnan().all())
+    y[:, [7, 100, 2001]] = 0
+    assert bool(torch.isfinite(y).all())
