@@ -7,20 +7,27 @@ namespace nimble {
 
 static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// The members of the family that need rows of whole 16 bytes: tile, waves among which K is divided, workgroups that share a compute unit,
-// stages that are loaded ahead; microseconds of a workgroup that do not depend on K (launch, first loads, sums and stores; of a large tile its
-// end); KB per us at which a compute unit's stages arrive (streaming), or microseconds of a stage of 128 bytes of K on a full chip (large tiles).
+// The members of the family that need rows of whole 16 bytes: tile, waves among which K is divided, stages that are loaded ahead (large tiles);
+// microseconds of a workgroup that do not depend on K (launch, first loads, sums and stores; of a large tile its end); KB per us at which a
+// compute unit's stages arrive (streaming), or microseconds of a stage of 128 bytes of K on a full chip (large tiles).
 struct Member {
-  int kernel, bm, bn, k_waves, per_cu, ahead;
+  int kernel, bm, bn, k_waves, ahead;
   double fixed_us, rate;
 };
 static const Member kMembers[] = {
-    {NIMBLE_PRODUCT_STREAM, 8, 32, 4, 3, 0, 2.0, 66},    {NIMBLE_PRODUCT_STREAM, 16, 32, 4, 3, 0, 2.0, 75},
-    {NIMBLE_PRODUCT_STREAM, 32, 32, 4, 2, 0, 2.2, 100},  {NIMBLE_PRODUCT_STREAM, 64, 64, 4, 1, 0, 4.3, 93},
-    {NIMBLE_PRODUCT_STREAM, 64, 64, 2, 2, 0, 3.5, 56},   {NIMBLE_PRODUCT_TILES, 128, 256, 1, 1, 3, 2.6, 0.67},
-    {NIMBLE_PRODUCT_TILES, 160, 256, 1, 1, 2, 3.1, 0.91}, {NIMBLE_PRODUCT_TILES, 192, 256, 1, 1, 2, 2.8, 1.09},
-    {NIMBLE_PRODUCT_TILES, 224, 256, 1, 1, 2, 3.6, 1.22}, {NIMBLE_PRODUCT_TILES, 256, 256, 1, 1, 2, 4.1, 1.43},
+    {NIMBLE_PRODUCT_STREAM, 8, 32, 4, 0, 2.0, 66},    {NIMBLE_PRODUCT_STREAM, 16, 32, 4, 0, 2.0, 75},
+    {NIMBLE_PRODUCT_STREAM, 32, 32, 4, 0, 2.2, 100},  {NIMBLE_PRODUCT_STREAM, 64, 64, 4, 0, 4.3, 93},
+    {NIMBLE_PRODUCT_STREAM, 64, 64, 2, 0, 3.5, 56},   {NIMBLE_PRODUCT_TILES, 128, 256, 1, 3, 2.6, 0.67},
+    {NIMBLE_PRODUCT_TILES, 160, 256, 1, 2, 3.1, 0.91}, {NIMBLE_PRODUCT_TILES, 192, 256, 1, 2, 2.8, 1.09},
+    {NIMBLE_PRODUCT_TILES, 224, 256, 1, 2, 3.6, 1.22}, {NIMBLE_PRODUCT_TILES, 256, 256, 1, 2, 4.1, 1.43},
 };
+
+// Workgroups of a streaming member that share a compute unit, by their LDS: three of 8 x 32, two of 32 x 32 and of 64 x 64 by two waves, one of
+// 64 x 64 by four; of 16 x 32 three without groups (49920 bytes each), two with the map of the groups (58120).
+// (With three for either, 84 of 4000 grouped draws took 16 x 32 in what was thought to be fewer rounds, and 14 % longer on average.)
+static int stream_workgroups_per_cu(const ProductShape& s, const Member& m) {
+  return kComputeUnitLds / stream_lds_bytes(m.bm, m.bn, m.k_waves, kStreamStages, s.grouped ? kMostGroups : 0);
+}
 
 // The most tile rows there can be: a group adds at most one that is not full, and only if it has a row.
 static int64_t most_tile_rows(const ProductShape& s, int bm) {
@@ -54,7 +61,7 @@ static double product_us(const ProductShape& s, const Member& m) {
     us = 4.4 + ceil(tiles * (s.grouped && s.groups > 1 ? 1.03 : 1.0) / kCUs) * (walk + m.fixed_us);
   } else {
     const double per_cu = tiles < kCUs ? 1.0 : tiles / kCUs;
-    us = 1.0 + ceil(tiles / (kCUs * m.per_cu)) * m.fixed_us + per_cu * stages * (m.bm + m.bn) * 0.128 / m.rate;
+    us = 1.0 + ceil(tiles / (kCUs * stream_workgroups_per_cu(s, m))) * m.fixed_us + per_cu * stages * (m.bm + m.bn) * 0.128 / m.rate;
   }
   const double weights_us = live * (double)s.N * (double)s.row_bytes() / 4.8e6;
   return (us > weights_us ? us : weights_us) + 0.25 * us;

@@ -20,8 +20,14 @@ struct ProductArgs {
   int epilogue, out_f32;
 };
 
-// Groups whose first rows and tile counts a workgroup keeps in LDS.
-constexpr int kMostGroups = 1024, kFewGroups = 512;  // (the latter where two workgroups share a compute unit)
+// Groups whose first rows and tile counts a workgroup keeps in LDS (see GroupMap).
+constexpr int kMostGroups = 1024;
+constexpr int group_map_bytes(int most) { return most ? 2 * (most + 1) * 4 : 0; }
+// LDS of a streaming workgroup: a ring of `stages` of 128 bytes of its rows and columns for each wave, scales and bias, the map of the groups.
+constexpr int stream_lds_bytes(int rows, int columns, int k_waves, int stages, int groups) {
+  return k_waves * stages * (rows + columns) * 128 + 3 * 64 * 4 + group_map_bytes(groups);
+}
+constexpr int kStreamStages = 2, kComputeUnitLds = 160 * 1024;
 // A launch is of fewer than 2^32 threads; workgroups go round where there is more to do.
 constexpr int64_t kMostWorkgroups = 1 << 21;
 // 8-bit codes are down to -128: K * 128 * 128 stays below 2^31.

@@ -56,6 +56,7 @@ struct GroupMap {
   int ends[MOST + 1];
   int starts[MOST + 1];
 };
+static_assert(sizeof(GroupMap<kMostGroups>) == group_map_bytes(kMostGroups), "LDS of the map as the host takes it");
 // Filled by the first wave; the caller's barrier publishes it.
 template <int BM, int MOST>
 __device__ __forceinline__ void map_groups(const ProductArgs& g, GroupMap<MOST>& map) {

@@ -39,11 +39,11 @@ int launch_product(const ProductArgs& g, const nimble_product_plan& p, hipStream
   }
   if (p.kernel == NIMBLE_PRODUCT_STREAM) {
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, g, tiles, tiles_n); };
-    if (p.bm == 8) launch(product_stream_kernel<T, GROUPS, 1, 2, 4, 2, 8>);
-    else if (p.bm == 16) launch(product_stream_kernel<T, GROUPS, 1, 2, 4, 2>);
-    else if (p.bm == 32) launch(product_stream_kernel<T, GROUPS, 2, 2, 4, 2>);
-    else if (p.k_waves == 4) launch(product_stream_kernel<T, GROUPS, 4, 4, 4, 2>);
-    else launch(product_stream_kernel<T, GROUPS, 4, 4, 2, 2>);
+    if (p.bm == 8) launch(product_stream_kernel<T, GROUPS, 1, 2, 4, kStreamStages, 8>);
+    else if (p.bm == 16) launch(product_stream_kernel<T, GROUPS, 1, 2, 4, kStreamStages>);
+    else if (p.bm == 32) launch(product_stream_kernel<T, GROUPS, 2, 2, 4, kStreamStages>);
+    else if (p.k_waves == 4) launch(product_stream_kernel<T, GROUPS, 4, 4, 4, kStreamStages>);
+    else launch(product_stream_kernel<T, GROUPS, 4, 4, 2, kStreamStages>);
     return launched("product stream kernel launch");
   }
   if (p.bm == 16)

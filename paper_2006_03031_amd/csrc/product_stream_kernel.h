@@ -27,6 +27,7 @@ __global__ void __launch_bounds__(KW * 64) product_stream_kernel(ProductArgs g, 
   __shared__ __attribute__((aligned(16))) uint4 smem[KW][RING];
   __shared__ __attribute__((aligned(16))) float values[3][64];  // scales of rows and columns, bias
   __shared__ GroupMap<GROUPS> map;
+  static_assert(sizeof(smem) + sizeof(values) + group_map_bytes(GROUPS) == stream_lds_bytes(XR, BN, KW, S, GROUPS), "LDS as the host takes it");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (GROUPS) {
     map_groups<XR>(g, map);
