@@ -1,4 +1,4 @@
-// Shape functions and the dispatch function of the 8-bit and the grouped products.  Integer arithmetic only; no HIP call.
+// Shape functions and the dispatch function of the 8-bit and the grouped products: host arithmetic only, no HIP call.
 #include "grouped_internal.h"
 
 #include <cmath>
@@ -105,12 +105,11 @@ int plan_product(const ProductShape& s, nimble_product_plan* p) {
   return NIMBLE_OK;
 }
 
-static int check_product(int64_t R, int64_t E, int64_t N, int64_t K, bool grouped, bool int8) {
+static int check_product(int64_t R, int64_t E, int64_t N, int64_t K, bool int8) {
   if (R < 0 || E < 0 || N < 0 || K < 0) return fail(NIMBLE_ERR_ARG, "negative extent");
   if (E > kMostGroups) return fail(NIMBLE_ERR_ARG, "%lld groups, at most %d", (long long)E, kMostGroups);
   if (int8 && K > kMostK8) return fail(NIMBLE_ERR_ARG, "K = %lld: 32-bit sums of 8-bit products hold for K <= %lld", (long long)K, (long long)kMostK8);
   if (K > kMostK16 || N > (1ll << 30) || R > (1ll << 31) - 1) return fail(NIMBLE_ERR_ARG, "extent too large");
-  (void)grouped;
   return NIMBLE_OK;
 }
 
@@ -177,7 +176,7 @@ int nimble_product_plan_of(int64_t R, int64_t E, int64_t N, int64_t K, int in_dt
     return fail(NIMBLE_ERR_DTYPE, "unknown dtype %d or %d", in_dtype, out_dtype);
   const bool grouped = E != -1, int8 = in_dtype == NIMBLE_I8;
   if (!grouped && !int8) return fail(NIMBLE_ERR_ARG, "bf16 without groups is nimble_dense_plan's");
-  const int rc = check_product(R, grouped ? E : 1, N, K, grouped, int8);
+  const int rc = check_product(R, grouped ? E : 1, N, K, int8);
   if (rc != NIMBLE_OK) return rc;
   return plan_product(ProductShape{R, grouped ? E : 1, N, K, grouped, int8, out_dtype == NIMBLE_F32}, plan);
 }

@@ -3,7 +3,7 @@
 //   grouped_kernel.h         the map from workgroups to the tiles of groups that only the device knows, loads through buffer descriptors,
 //       and product_direct_kernel: operands of any alignment.
 //   product_stream_kernel.h  product_stream_kernel: small tiles, K divided among a workgroup's waves.
-//   product_tile_kernel.h    product_tile_kernel: large tiles by four waves, a tile's end computed during the next one.
+//   product_tile_kernel.h    product_tile_kernel: large tiles by four waves, the first stages of a tile loaded during the last ones of the tile before.
 #include <hip/hip_runtime.h>
 
 #include "grouped_internal.h"
@@ -70,14 +70,12 @@ int nimble_quantize_rows_dyn(const void* x, int x_dtype, void* q, void* scale, i
   const dim3 grid((unsigned)(groups < kMostWorkgroups ? groups : kMostWorkgroups)), block(256);
   auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, (hipStream_t)stream, g); };
   if (x_dtype == NIMBLE_F32) {
-    if (wave && K <= 1024) launch(quantize_rows_kernel<true, 1, 2>);
-    else if (wave) launch(quantize_rows_kernel<true, 1, 8>);
+    if (wave) launch(quantize_rows_kernel<true, 1, 2>);
     else if (K <= 4096) launch(quantize_rows_kernel<true, 4, 2>);
     else if (K <= 8192) launch(quantize_rows_kernel<true, 4, 4>);
     else launch(quantize_rows_kernel<true, 4, 8>);
   } else {
-    if (wave && K <= 1024) launch(quantize_rows_kernel<false, 1, 2>);
-    else if (wave) launch(quantize_rows_kernel<false, 1, 8>);
+    if (wave) launch(quantize_rows_kernel<false, 1, 2>);
     else if (K <= 4096) launch(quantize_rows_kernel<false, 4, 2>);
     else if (K <= 8192) launch(quantize_rows_kernel<false, 4, 4>);
     else launch(quantize_rows_kernel<false, 4, 8>);
