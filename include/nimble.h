@@ -57,8 +57,9 @@ typedef enum nimble_epilogue {
   NIMBLE_EPI_NONE = 0,          /* y = x.w^T                                     */
   NIMBLE_EPI_BIAS = 1,          /* y = x.w^T + b                                 */
   /* y = gelu(x.w^T + b), gelu(v)=v/2 (1+erf(v/sqrt 2)): of dense within 2.52e-5 (a fit, see
-   * csrc/device_common.h); of the 8-bit and the grouped products within 2^-21 of the value, times 1+(v/2)^6
-   * where v < 0 and within 2^-46 where v < -8 (csrc/grouped_kernel.h) */
+   * csrc/device_common.h); of the 8-bit and the grouped products within 2^-21 of the value for f32 outputs and,
+   * ahead of their rounding, 2^-20 for bf16 ones, times 1+(v/2)^6 and 1+(v/1.4)^6 where v < 0, and within 2^-46
+   * where v < -8 (csrc/grouped_kernel.h) */
   NIMBLE_EPI_BIAS_GELU_ERF = 2
 } nimble_epilogue;
 

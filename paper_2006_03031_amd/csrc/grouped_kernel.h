@@ -152,27 +152,33 @@ __device__ __forceinline__ uint4 load16_words(const unsigned char* p) {
 
 // gelu(v) = v/2 (1 + erf(v / sqrt 2)) = max(v, 0) - |v| Q(|v|), Q the upper tail of the normal distribution.  log2 Q is smooth for
 // x >= 0 and -1 at 0, so Q is 2^P(x) with a polynomial P: one transcendental instruction per value, and the roundings of a small tail do not
-// reach a result that is not small.  P is the minimax fit of degree 10 to log2 Q on [0, 8], its error weighted by 1 / (1 + (x/2)^6).  With the
-// roundings of f32 and of the hardware's exp2 (1 ulp) a result is off by at most 2^-21 of itself for v >= 0 and by 2^-21 (1 + (v/2)^6) of itself
-// for -8 <= v < 0; f32 outputs ask for that, and bf16 ones are then the rounded exact ones but for values next to a border.  Below
-// -8 P falls on to minus infinity and the result stays under 2^-46; above 8, where it is v, x stays 8, so that infinity less nothing is infinity.
+// reach a result that is not small.  P is a minimax fit to log2 Q on [0, 8].  With the roundings of f32 and of the hardware's exp2 (1 ulp) a
+// result is off by at most
+//   f32 outputs,  degree 10, the fit's error weighted by 1 / (1 + (x/2)^6):   2^-21 of itself for v >= 0, 2^-21 (1 + (v/2)^6) for -8 <= v < 0;
+//   bf16 outputs, degree 8, weighted by 1 / (1 + (x/1.4)^6):                  2^-20 of itself for v >= 0, 2^-20 (1 + (v/1.4)^6) for -8 <= v < 0,
+// 1/2000 of half a step of bf16 where results are not small: of 100000 results from values of spread 0.65 four are not the rounded exact ones, one
+// of them with degree 10.  (Two steps of the polynomial are 2 us of the 55 of 8177 x 4096 x 1024 in 8 bits, 5 of 121 of the same over 8 groups.)
+// Below -8 P falls on to minus infinity and the result stays under 2^-46; above 8, where it is v, x stays 8, so that infinity less nothing is infinity.
 // NaN stays NaN, and minus infinity gives NaN as the formula does.
 //   N values side by side, step by step (the empty statements keep the N results of a step together), as epilogue_of does it.
-template <int N>
+template <bool F32, int N>
 __device__ __forceinline__ void gelu_of(float (&v)[N]) {
-  constexpr float kTail[11] = {-1.0f,           -1.15110886f,    -0.459177405f,  -0.0525782481f,  0.00715400605f, -0.000172875938f,
-                               -0.000194635781f, 5.13012637e-05f, -6.58381487e-06f, 4.4570379e-07f, -1.26317756e-08f};
+  constexpr int kDegree = F32 ? 10 : 8;
+  constexpr float kTail32[11] = {-1.0f,           -1.15110886f,    -0.459177405f,  -0.0525782481f,  0.00715400605f, -0.000172875938f,
+                                 -0.000194635781f, 5.13012637e-05f, -6.58381487e-06f, 4.4570379e-07f, -1.26317756e-08f};
+  constexpr float kTail16[9] = {-1.0f, -1.15111983f, -0.459074169f, -0.0529038422f, 0.00763690891f,
+                                -0.000555595732f, -2.37187851e-05f, 7.77410787e-06f, -4.18191178e-07f};
   float x[N], p[N];
   auto together = [&](float (&y)[N]) {
 #pragma unroll
     for (int i = 0; i < N; ++i) asm volatile("" : "+v"(y[i]));
   };
 #pragma unroll
-  for (int i = 0; i < N; ++i) x[i] = fabsf(__builtin_elementwise_minimum(v[i], 8.0f)), p[i] = kTail[10];
+  for (int i = 0; i < N; ++i) x[i] = fabsf(__builtin_elementwise_minimum(v[i], 8.0f)), p[i] = F32 ? kTail32[10] : kTail16[8];
 #pragma unroll
-  for (int k = 9; k >= 0; --k) {
+  for (int k = kDegree - 1; k >= 0; --k) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) p[i] = fmaf(p[i], x[i], kTail[k]);
+    for (int i = 0; i < N; ++i) p[i] = fmaf(p[i], x[i], F32 ? kTail32[k] : kTail16[k < 8 ? k : 8]);
     together(p);
   }
 #pragma unroll
@@ -185,9 +191,10 @@ __device__ __forceinline__ void gelu_of(float (&v)[N]) {
 // Four consecutive outputs of a row from n on, as many as there are; `v` is scaled and has its bias.
 __device__ __forceinline__ void store4(const ProductArgs& g, float (&v)[4], long long row, int n) {
   const int n4 = g.N - n;
-  if (g.epilogue == NIMBLE_EPI_BIAS_GELU_ERF) gelu_of(v);
+  const bool gelu = g.epilogue == NIMBLE_EPI_BIAS_GELU_ERF;
   const long long at = row * g.N + n;
   if (g.out_f32) {
+    if (gelu) gelu_of<true>(v);
     float* y = (float*)g.y + at;
     if (n4 >= 4) {
       __builtin_memcpy(y, v, 16);
@@ -197,6 +204,7 @@ __device__ __forceinline__ void store4(const ProductArgs& g, float (&v)[4], long
         if (e < n4) y[e] = v[e];
     }
   } else {
+    if (gelu) gelu_of<false>(v);
     u16* y = (u16*)g.y + at;
     if (n4 >= 4) {
       const uint2 pk = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));

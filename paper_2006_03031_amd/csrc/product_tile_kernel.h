@@ -263,7 +263,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
           const float sum = (float)read_sum(held);
           v[k] = T::kInt8 ? fmaf(sum, xs[j] * ws[k], bs[k]) : sum + bs[k];
         }
-        if constexpr (decltype(gelu)::value) gelu_of(v);
+        if constexpr (decltype(gelu)::value) gelu_of<OUT_F32>(v);
         if constexpr (OUT_F32) {
 #pragma unroll
           for (int x = 0; x < 2; ++x)

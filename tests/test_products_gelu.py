@@ -1,7 +1,8 @@
 """The GELU of the 8-bit and the grouped products against float64.
 
-Tolerance: 2^-21 (1 + (min(v, 0) / 2)^6) of the value down to v = -8, below it 2^-46, as csrc/grouped_kernel.h states; the first test derives
-it from the constants there, in the arithmetic of f32.  Outputs in bf16: half a step, 2^-8 of the value, on top."""
+Tolerance: 2^-21 (1 + (min(v, 0) / 2)^6) of the value for f32 outputs, 2^-20 (1 + (min(v, 0) / 1.4)^6) for bf16 ones ahead of their rounding (half
+a step, 2^-8 of the value), down to v = -8, below it 2^-46, as csrc/grouped_kernel.h states; the first test derives it from the constants there,
+in the arithmetic of f32."""
 import math
 import os
 import re
@@ -19,26 +20,28 @@ def _exact(v):
     return 0.5 * v * torch.special.erfc(-v * math.sqrt(0.5))
 
 
-def _allowed(v, g):
+def _allowed(v, g, f32):
     tail = v.double().clamp(max=0)
-    return torch.where(v < -8, 2.0 ** -46, 2.0 ** -21 * (1 + (tail / 2) ** 6) * g.abs())
+    share = 2.0 ** -21 * (1 + (tail / 2) ** 6) if f32 else 2.0 ** -20 * (1 + (tail / 1.4) ** 6)
+    return torch.where(v < -8, 2.0 ** -46, share * g.abs())
 
 
-def test_what_the_polynomial_and_f32_leave():
+@pytest.mark.parametrize("name,degree", [("kTail32", 10), ("kTail16", 8)])
+def test_what_the_polynomial_and_f32_leave(name, degree):
     from paper_2006_03031_amd import build
     with open(os.path.join(build.CSRC, "grouped_kernel.h")) as f:
-        body = re.search(r"kTail\[11\] = \{(.*?)\};", f.read(), re.S).group(1)
+        body = re.search(name + r"\[\d+\] = \{(.*?)\};", f.read(), re.S).group(1)
     tail = [float(torch.tensor(float(c[:-1]), dtype=torch.float32)) for c in body.replace("\n", "").replace(" ", "").split(",")]
-    assert len(tail) == 11 and tail[0] == -1.0 and tail[10] < 0
+    assert len(tail) == degree + 1 and tail[0] == -1.0 and tail[degree] < 0
     v = torch.cat([torch.linspace(-40, 12, 2000001, dtype=torch.float64), -torch.logspace(-30, 18, 20001, dtype=torch.float64)]).float()
     x = v.clamp(max=8).abs().double()
-    p = torch.full_like(x, tail[10])
-    for c in tail[9::-1]:      # (a product of two f32 is exact in f64)
+    p = torch.full_like(x, tail[degree])
+    for c in tail[degree - 1::-1]:      # (a product of two f32 is exact in f64)
         p = (p * x + c).float().double()
     g, off = _exact(v), 2.0 ** -23          # of the hardware's exp2
     for q in (torch.exp2(p) * (1 + off), torch.exp2(p) * (1 - off)):
         y = (v.double().clamp(min=0) - x * q).float().double()
-        assert bool(((y - g).abs() <= _allowed(v, g) + 2.0 ** -140).all())
+        assert bool(((y - g).abs() <= _allowed(v, g, degree == 10) + 2.0 ** -140).all())
 
 
 def _values():
@@ -49,7 +52,7 @@ def _values():
 
 def _check(y, v):
     g = _exact(v)
-    err = _allowed(v, g) + 2.0 ** -120      # (no results below the normal numbers)
+    err = _allowed(v, g, y.dtype == torch.float32) + 2.0 ** -120      # (no results below the normal numbers)
     if y.dtype == torch.bfloat16:
         err = err + 2.0 ** -8 * (g.abs() + err)
     bad = ~((y.cpu().double() - g).abs() <= err)
