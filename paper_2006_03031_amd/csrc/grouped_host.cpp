@@ -17,9 +17,9 @@ struct Member {
 static const Member kMembers[] = {
     {NIMBLE_PRODUCT_STREAM, 8, 32, 4, 0, 2.0, 66},    {NIMBLE_PRODUCT_STREAM, 16, 32, 4, 0, 2.0, 75},
     {NIMBLE_PRODUCT_STREAM, 32, 32, 4, 0, 2.2, 100},  {NIMBLE_PRODUCT_STREAM, 64, 64, 4, 0, 4.3, 93},
-    {NIMBLE_PRODUCT_STREAM, 64, 64, 2, 0, 3.5, 56},   {NIMBLE_PRODUCT_TILES, 128, 256, 1, 3, 2.6, 0.67},
-    {NIMBLE_PRODUCT_TILES, 160, 256, 1, 2, 3.1, 0.91}, {NIMBLE_PRODUCT_TILES, 192, 256, 1, 2, 2.8, 1.09},
-    {NIMBLE_PRODUCT_TILES, 224, 256, 1, 2, 3.6, 1.22}, {NIMBLE_PRODUCT_TILES, 256, 256, 1, 2, 4.1, 1.43},
+    {NIMBLE_PRODUCT_STREAM, 64, 64, 2, 0, 3.5, 56},   {NIMBLE_PRODUCT_TILES, 128, 256, 1, 3, 2.3, 0.78},
+    {NIMBLE_PRODUCT_TILES, 160, 256, 1, 2, 3.1, 0.86}, {NIMBLE_PRODUCT_TILES, 192, 256, 1, 2, 2.8, 1.05},
+    {NIMBLE_PRODUCT_TILES, 224, 256, 1, 2, 3.5, 1.15}, {NIMBLE_PRODUCT_TILES, 256, 256, 1, 2, 3.8, 1.25},
 };
 
 // Workgroups of a streaming member that share a compute unit, by their LDS: three of 8 x 32, two of 32 x 32 and of 64 x 64 by two waves, one of
@@ -36,18 +36,21 @@ static int64_t most_tile_rows(const ProductShape& s, int bm) {
 
 // Estimated microseconds.  How the rows fall on the groups is not known: each group is taken to have rows where there are
 // enough, and its last tile to be half full.  The workgroups of a compute unit share the rate at which stages arrive.  Large tiles go
-// round the chip, on a nearly empty one (less power) with stages a quarter shorter; groups may have a few tiles more than that.
+// round the chip, on a nearly empty one (less power) with stages a third shorter; groups may have a few tiles more than that.
 // Weights come at 4.8 TB/s where they come from memory, and then a quarter of the estimate still tells the members apart.
-// The constants are a fit to the ten members' times on 100 shapes of either type (K = 128 .. 8192, N = 128 .. 8192, 1 .. 16354 rows over
-// 1 .. 64 groups), where the choice costs 1 % more than the best member, and on 100 others 3 %.  Measured, dense in 8 bits with bias:
+// The constants are a fit to the members' times, measured until the clocks have settled, on 400 shapes of either type (K = 128 .. 8192,
+// N = 128 .. 8192, 1 .. 16354 rows over 1 .. 64 groups), 54 large ones and 27 of wide layers, where the choice costs 2.4, 0.4 and 1.6 % more than
+// the best member; on 200 others it costs 2.9 %, on 36 other large ones 2.4 %.  (Fitted to short runs alone, large ones took 128 x 256 and 5 to 10 %
+// longer.)  Dense in 8 bits with bias, us:
 //   rows x N x K         8 x 32   32 x 32   64 x 64, 4 waves  64 x 64, 2 waves  128 x 256   192 x 256   256 x 256
-//   1 x 4096 x 1024      2.9      3.7       6.1               7.4               9.7
-//   200 x 1024 x 4096             6.2       9.6               13.6              24
-//   512 x 1024 x 4096             9.9       10.5              13.8              24.5
-//   512 x 4096 x 1024             15.2      12.3              9.7               10.6
-//   8192 x 1024 x 4096                                                          31.8        37.7        45.8
-//   16384 x 1024 x 4096                                                         61.7        71.3        54.5
-//   8192 x 4096 x 1024                                                          41.3        40.7        36.4
+//   1 x 4096 x 1024      2.9      3.3       6.0               6.3               10.1        12.1        14.8
+//   200 x 1024 x 4096    9.9      5.3       9.1               13.3              25.4        32.5        40.3
+//   512 x 1024 x 4096    19.5     9.4       10.6              13.8              26.2        33.1        41.3
+//   512 x 4096 x 1024    30.2     13.8      11.6              9.1               10.8        13.1        16.1
+//   8192 x 1024 x 4096                      79.2              65.4              31.5        34.6        42.0
+//   16384 x 1024 x 4096                     152               129               60.6        69.1        53.0
+//   8192 x 4096 x 1024                      163               117               40.7        40.0        34.9
+//   8192 x 8192 x 8192                      1091              1070              463         441         397
 static double product_us(const ProductShape& s, const Member& m) {
   const double kCUs = kComputeUnits;
   const double live = s.grouped ? (double)(s.groups < s.rows ? s.groups : s.rows) : 1.0;
@@ -57,8 +60,8 @@ static double product_us(const ProductShape& s, const Member& m) {
   double us;
   if (m.kernel == NIMBLE_PRODUCT_TILES) {
     const double full = tiles < kCUs ? tiles / kCUs : 1.0;
-    const double walk = (stages < m.ahead ? m.ahead : stages) * m.rate * (0.73 + 0.27 * full);
-    us = 4.4 + ceil(tiles * (s.grouped && s.groups > 1 ? 1.03 : 1.0) / kCUs) * (walk + m.fixed_us);
+    const double walk = (stages < m.ahead ? m.ahead : stages) * m.rate * (0.62 + 0.38 * full);
+    us = 3.7 + ceil(tiles * (s.grouped && s.groups > 1 ? 1.03 : 1.0) / kCUs) * (walk + m.fixed_us);
   } else {
     const double per_cu = tiles < kCUs ? 1.0 : tiles / kCUs;
     us = 1.0 + ceil(tiles / (kCUs * stream_workgroups_per_cu(s, m))) * m.fixed_us + per_cu * stages * (m.bm + m.bn) * 0.128 / m.rate;

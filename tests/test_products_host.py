@@ -158,3 +158,10 @@ def test_the_gelus_fit():
 def test_the_rounds_of_grouped_calls(R, E, N, K, tile):
     p = nb.product_plan(R, E, N, K)
     assert (p.bm, p.bn) == tile
+
+
+# Large products take tiles of 256 rows (53, 53, 397 and, N = 30528, 290 us; of 128 rows 61, 61, 463 and 340), one turn of 128 rows stays (31.5; 42.0 of 256).
+@pytest.mark.parametrize("M,N,K,bm", [(8177, 30528, 1024, 256), (16384, 1024, 4096, 256), (4096, 4096, 4096, 256), (8192, 8192, 8192, 256), (8192, 1024, 4096, 128)])
+def test_the_tiles_of_large_products(M, N, K, bm):
+    p = nb.product_plan(M, None, N, K)
+    assert (p.kernel, p.bm) == (1, bm)
