@@ -378,7 +378,8 @@ int nimble_dense_i8_shape(const int64_t* x_shape, int x_rank, const int64_t* x_s
 
 /* y[m,n] = epi( x_scale[m] w_scale[n] sum_k x[m,k] w[n,k] + bias[n] ): x [M,K], w [N,K] int8 (any value, -128 too), the scales f32,
  * bias [N] bf16 (NULL for NIMBLE_EPI_NONE), y [M,N] of out_dtype.  Sums in 32-bit integers, so exact: K is at most 131071
- * (NIMBLE_ERR_ARG).  Scales, bias and epilogue in f32.  K need not be a multiple of anything; rows of whole 16 bytes are the fast ones. */
+ * (NIMBLE_ERR_ARG).  Scales, bias and epilogue in f32; x_scale[m] w_scale[n] is formed first, so a pair of scales whose product is
+ * below 2^-126 loses digits and one whose product passes 2^128 gives no number.  K need not be a multiple of anything; rows of whole 16 bytes are the fast ones. */
 int nimble_dense_i8_dyn(const void* x, const void* x_scale, const void* w, const void* w_scale, const void* bias, void* y, int64_t M,
                         int64_t N, int64_t K, int epilogue, int out_dtype, void* stream);
 

@@ -19,8 +19,9 @@ int launch_product(const ProductArgs& g, const nimble_product_plan& p, hipStream
   const unsigned tiles = (unsigned)p.tiles, tiles_n = (unsigned)((g.N + p.bn - 1) / p.bn);
   const dim3 grid(p.grid), block(p.block);
   if (p.kernel == NIMBLE_PRODUCT_TILES) {
-    // tiles in flight are blocks of 8 rows of tiles: 8192^3 in 8 bits 394 us, with 2 / 4 / 16 / 32 rows 408 / 395 / 407 / 432; 16354 rows over 8
-    // groups x 4096 x 1024 165, 179 / 159 / 170 / 172
+    // tiles in flight are blocks of 8 rows of tiles.  Settled clocks, 8 rows / 4: 8 bits 16384 x 4096 x 4096 208 / 214 us, 8192 x 30528 x 1024
+    // 294 / 297, 8192^3 388 / 384; bf16 16354 rows over 8 groups x 4096 x 1024 140 / 143, over 32 158 / 162.  2, 16 and 32 rows: 3 to 10 % longer
+    // at 8192^3
     const int tiles_m = (int)(p.tiles / tiles_n), group_m = 8;
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, g, tiles_m, (int)tiles_n, group_m); };
     auto pick = [&](auto f32) {

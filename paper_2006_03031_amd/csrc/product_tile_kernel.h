@@ -13,7 +13,8 @@ namespace nimble {
 // loads take together; with short K also the ends of the tiles.
 //   Columns go to the matrix instruction's rows such that a lane holds eight neighbouring ones of bf16 (four of f32): 16 bytes, 64
 // contiguous ones with its three neighbours, stored from registers as they are.  The swizzle of the weights' rows in LDS
-// follows (see b_swizzle).  With the outputs brought into whole lines through LDS first, 8192 x 4096 x 1024 in 8 bits took 53.6 us, so 36.4.
+// follows (see b_swizzle).  With the outputs brought into whole lines through LDS first, 8192 x 4096 x 1024 in 8 bits took 53.6 us, stored from
+// registers 36.4.
 //   The loads past a tile's last stage are the next tile's first ones, and the stores of a tile's end stay in flight while the next
 // begins.  To put a tile's sums aside and finish them in between the next tile's products as well (128 x 256, twice 128 registers
 // of sums) gained nothing: 41.3 us, with it 40.3; one wave issues an instruction in four clocks at most, and products, reads and
@@ -23,8 +24,8 @@ namespace nimble {
 // the end of K in the last stage.  Stores past the last row or column are dropped in the same way.  So every tile runs the same code
 // whatever its number of rows.
 //   Tiles are told from the offsets of the groups (GroupMap), which the workgroup reads once.
-//   Measured, 8 bits / bf16: 8192^3 396 / 737 us (2780 / 1490 T); 8192 x 4096 x 1024 with bias 36.4 / 62, with GELU 45.3 / 72 (half of
-// 16384 rows).
+//   Measured with settled clocks, 8 bits / bf16: 8192^3 394 / 820 us (2790 / 1340 T); 8192 x 4096 x 1024 with bias 34.3-35.1 / 61.4-63.6, with GELU
+// to bf16 42.7-45.5 / 69-74 (half of 16384 rows), to f32 47.7-50.4: the spread is that of two cards.
 // ---------------------------------------------------------------------------
 #define NIMBLE_INLINE __attribute__((always_inline))
 template <int N>

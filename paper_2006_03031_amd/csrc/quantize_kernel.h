@@ -15,9 +15,10 @@ namespace nimble {
 //   Rows below 2^-100 are taken times 2^100 first, since 127 / a would overflow, and rows beyond 2^100 times 2^-100, since 127 x would
 // (exact but for elements so small that their code is 0 anyway); rows with an infinity or a NaN get codes 0
 //   and scale NaN, which makes every result of the row NaN.
-//   Bound: memory (2 or 4 bytes read and one written per element): 8177 x 4096 bf16 24.0 us, 4.2 TB/s of the 5.2 that a copy reaches (75 us with
-// the border decided in f64 for every element group and values held as f32); 4096 x 4096 f32 15.2.  A row stays in registers, as it was read, between the maximum
-// and the codes.
+//   Bound: memory (2 or 4 bytes read and one written per element): 8177 x 4096 bf16 21.6 us, 4.7 TB/s of the 5.2 that a copy reaches (75 us with
+// the border decided in f64 for every element group and values held as f32); 8177 x 1024 9.8-11.7, 8177 x 8192 38.8, 4096 x 16384 52 (3.8 TB/s; with
+// eight groups held two waves per SIMD are left), 4096 x 4096 f32 15.8, 4096 x 16384 f32 74.  A row stays in registers, as it was read, between the
+// maximum and the codes; of one longer than 16384 the rest is read twice: 2000 x 30522 bf16 74 us, 2.5 TB/s.
 // ---------------------------------------------------------------------------
 struct QuantizeArgs {
   const void* x;
