@@ -417,6 +417,111 @@ typedef struct nimble_product_plan {
 } nimble_product_plan;
 int nimble_product_plan_of(int64_t R, int64_t E, int64_t N, int64_t K, int in_dtype, int out_dtype, nimble_product_plan* plan);
 
+/* ---- positions, a paged cache of keys and values, and attention over it --------------------
+ * A layer of a decoder serves sequences whose tokens come a few at a time: the rows of all sequences lie one after the other, what
+ * a sequence has computed before is in a cache of pages, and how many rows and tokens each has is known on the device only.  No call
+ * here waits for the device, so that one captured graph serves all lengths up to the width of the page table.
+ *
+ * nimble_sequences describes one call's rows (device pointers, read when the kernels run):
+ *   offsets [count+1] int64   rows offsets[s] .. offsets[s+1]-1 are sequence s, n of them; not falling, within 0..rows.  Rows of no
+ *                             sequence (ahead of offsets[0], from offsets[count] on) are left as they were in every output
+ *   lengths [count] int64     tokens of the sequence, these rows being its last n: row i is at position lengths[s]-n+i.  0..width*page
+ *   pages [count, width] int32  position p is in slot p % page of page pages[s, p / page].  Entries of pages that no call needs may
+ *                             hold anything
+ * nimble_cache is the cache (device pointers): k, v [pages, kv_heads, page, D] bf16, or int8 with an f32 scale per token and head,
+ * k_scale, v_scale [pages, kv_heads, page].  page is a power of two from 16 to 1024, D 64 or 128 (NIMBLE_ERR_ARG).
+ * The host sees none of the device's numbers: what does not keep to the above gives rows, or pages that the call may write, of
+ * unspecified content, but no access outside the tensors.  Pages may be shared by sequences that only read them; slots that two rows
+ * of one call write hold either, or a mixture.
+ * Rows of queries, keys and values may lie `stride` elements apart (a multiple of 8, not less than a row's heads * D), so that the parts of
+ * one product's output are taken as they are.  Outputs must not overlap operands, but for what is said below. */
+typedef struct nimble_sequences {
+  const void* offsets;
+  const void* lengths;
+  const void* pages;
+  int64_t count, width, rows;
+} nimble_sequences;
+typedef struct nimble_cache {
+  void* k;
+  void* v;
+  void* k_scale; /* NULL unless dtype is NIMBLE_I8 */
+  void* v_scale;
+  int64_t pages, kv_heads, page, D;
+  int32_t dtype; /* NIMBLE_BF16 or NIMBLE_I8 */
+} nimble_cache;
+
+/* Shape functions.  rotary: x (T,H,D), positions (T), table (P,R,2) with 2R <= D -> (T,H,D). */
+int nimble_rotary_shape(const int64_t* x_shape, int x_rank, const int64_t* positions_shape, int positions_rank, const int64_t* table_shape,
+                        int table_rank, int64_t* out_shape);
+/* The check of a cache and a batch against each other: k, v (P,G,page,D), scales (P,G,page) with dtype NIMBLE_I8 (else NULL),
+ * offsets (S+1), lengths (S), pages (S,W). */
+int nimble_cache_check(const int64_t* k_shape, int k_rank, const int64_t* v_shape, int v_rank, const int64_t* k_scale_shape,
+                       int k_scale_rank, const int64_t* v_scale_shape, int v_scale_rank, int dtype, const int64_t* offsets_shape,
+                       int offsets_rank, const int64_t* lengths_shape, int lengths_rank, const int64_t* pages_shape, int pages_rank);
+/* cache_write: k, v (T,G,D) and, where q_rank is not 0, q (T,H,D), for a cache (.,G,.,D) -> q's (T,H,D). */
+int nimble_cache_write_shape(const int64_t* cache_shape, const int64_t* k_shape, int k_rank, const int64_t* v_shape, int v_rank,
+                             const int64_t* q_shape, int q_rank, int64_t* q_out_shape);
+/* cache_read: rows T of a cache (.,G,.,D) -> (T,G,D), of keys and of values. */
+int nimble_cache_read_shape(const int64_t* cache_shape, int64_t rows, int64_t* out_shape);
+/* paged_attention: q (T,H,D), H a multiple of G -> (T,H,D). */
+int nimble_paged_attention_shape(const int64_t* q_shape, int q_rank, const int64_t* cache_shape, int64_t* out_shape);
+
+/* table [positions, rot/2, 2] f32: magnitude * cos and sin of position * f_i, computed in f64.  f_i = base^(-2i/rot); for contexts longer
+ * than a model was trained on, f_i is blended with f_i / factor: f_i (k + (1-k) / factor), k = (turns - low) / (high - low) clamped to
+ * 0..1, turns = trained f_i / 2 pi (the turns that pair i makes within the trained length).  factor = 1: plain angles; trained = 0: every
+ * angle is divided.  base > 0, factor > 0, high > low, trained >= 0, all finite (NIMBLE_ERR_ARG). */
+int nimble_rotary_table_dyn(void* table, int64_t positions, int64_t rot, double base, double factor, double trained, double low,
+                            double high, double magnitude, void* stream);
+
+/* Rotary positions: y[t,h] is x[t,h] with its first 2R elements turned in pairs, the rest copied.  With (c,s) = table[positions[t], i]:
+ *   y_a = x_a c - x_b s,  y_b = x_b c + x_a s,   (a,b) = (i, i+R), or (2i, 2i+1) where interleaved != 0;   i = 0 .. R-1.
+ * x, y [T,H,D] bf16 (y may be x), rows x_stride and y_stride elements apart, any D and R with 2R <= D; positions [T] int64 (held to
+ * 0..table_rows-1), table [table_rows, R, 2] f32.  f32, rounded once.  Aligned heads of whole 32 bytes with R a
+ * multiple of 8 are the fast ones; other widths, alignments and strides are taken too: x and y need 2 bytes, table and positions 8. */
+int nimble_rotary_dyn(const void* x, int64_t x_stride, const void* positions, const void* table, int64_t table_rows, void* y,
+                      int64_t y_stride, int64_t T, int64_t H, int64_t D, int64_t R, int interleaved, void* stream);
+
+/* Keys and values of new rows into the cache, k turned by its position first where table is given (R a multiple of 8; 2R <= D), and the
+ * queries with them: q_out = rotary(q) where q is given (q_out [rows, heads, D] contiguous, may be q itself; with no table a copy).
+ * bf16: rotary's rounding.  int8: the codes and scales of nimble_quantize_rows_dyn for each token and head, of the turned keys before any
+ * rounding.  Rows at positions below 0, or that the page table does not reach, or whose page is not one of the cache's, are not written. */
+int nimble_cache_write_dyn(const nimble_cache* cache, const nimble_sequences* seqs, const void* k, int64_t k_stride, const void* v,
+                           int64_t v_stride, const void* q, int64_t q_stride, void* q_out, int64_t heads, const void* table,
+                           int64_t table_rows, int64_t R, int interleaved, void* stream);
+
+/* The inverse: the rows' keys and values out of the cache, k_out and v_out [rows, G, D] of out_dtype (NIMBLE_BF16 or NIMBLE_F32), 8-bit
+ * codes times their scale.  offsets that count each sequence's whole length read all of it.  Rows that cache_write would not have
+ * written are left as they were. */
+int nimble_cache_read_dyn(const nimble_cache* cache, const nimble_sequences* seqs, void* k_out, void* v_out, int out_dtype, void* stream);
+
+/* Attention of the rows over the cache, their own keys and values included (write them first):
+ *   o[r,h] = sum_j softmax_j(alpha q[r,h].k[j,h/(H/G)]) v[j,h/(H/G)] over the positions max(0, p-window+1) <= j <= p of r's sequence,
+ * p the position of r; window = 0: all j <= p.  A row that sees nothing (p < 0) gives zeros.  q [rows,H,D] bf16, o [rows,H,D] bf16
+ * contiguous; H a multiple of G; alpha > 0 and finite, window >= 0.  Scores, softmax and sums in f32, the probabilities (times the
+ * values' scales) rounded to bf16 before the product with v.  What a row does not see has no part in its result, whatever it holds.
+ * Long sequences are cut on the device, by the lengths, and joined by a second launch; the result depends on the lengths of all
+ * sequences of the call, but not on the run.
+ * workspace: nimble_paged_attention_plan_of's workspace_bytes, used by one call at a time; nothing in it carries over. */
+int nimble_paged_attention_dyn(const void* q, int64_t q_stride, const nimble_cache* cache, const nimble_sequences* seqs, void* o,
+                               int64_t heads, float alpha, int64_t window, void* workspace, size_t workspace_bytes, void* stream);
+
+/* What the dispatch function decides for a call of nimble_paged_attention_dyn (host only; it looks at numbers, not at pointers). */
+typedef enum nimble_paged_kernel {
+  NIMBLE_PAGED_TOKENS = 0, /* 16 rows (query heads that share keys, tokens) per workgroup, its waves share the keys among them */
+  NIMBLE_PAGED_CHUNKS = 1, /* 128 rows per workgroup, 32 a wave                                                              */
+  NIMBLE_PAGED_COUNT = 2
+} nimble_paged_kernel;
+typedef struct nimble_paged_plan {
+  int32_t kernel;           /* nimble_paged_kernel                                                     */
+  int32_t rows;             /* rows of a tile                                                          */
+  int32_t parts;            /* 1: sequences may be cut into parts, and a second launch joins them      */
+  uint32_t grid, join_grid[2], block;
+  int64_t slots;            /* parts that the workspace holds                                          */
+  uint64_t workspace_bytes;
+} nimble_paged_plan;
+int nimble_paged_attention_plan_of(int64_t rows, int64_t count, int64_t width, int64_t heads, int64_t kv_heads, int64_t page, int64_t D,
+                                   int dtype, int64_t window, nimble_paged_plan* plan);
+
 #ifdef __cplusplus
 }
 #endif

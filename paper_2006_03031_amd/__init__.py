@@ -14,5 +14,7 @@ from .binding import (  # noqa: F401
     lstm_loop_supported, lstm_loop_preferred, lstm_loop_workspace_bytes, nimble_lstm_loop_dyn,
     I8, ProductPlan, quantize_rows_shape, dense_i8_shape, grouped_dense_shape, product_plan, nimble_quantize_rows_dyn, nimble_dense_i8_dyn,
     nimble_grouped_dense_dyn, nimble_grouped_dense_i8_dyn,
+    PagedPlan, rotary_shape, cache_check, cache_write_shape, cache_read_shape, paged_attention_shape, paged_attention_plan, sequences, cache,
+    nimble_rotary_table_dyn, nimble_rotary_dyn, nimble_cache_write_dyn, nimble_cache_read_dyn, nimble_paged_attention_dyn,
     variant_name, exported_symbols, nimble_probe_mfma_bf16, nimble_probe_hbm_read, nimble_probe_lstm_loop,
 )

@@ -45,6 +45,35 @@ class _CProductPlan(ctypes.Structure):
                 ("tiles", ctypes.c_int64), ("grid", ctypes.c_uint32), ("block", ctypes.c_uint32)]
 
 
+class _CSequences(ctypes.Structure):
+    _fields_ = [("offsets", ctypes.c_void_p), ("lengths", ctypes.c_void_p), ("pages", ctypes.c_void_p),
+                ("count", ctypes.c_int64), ("width", ctypes.c_int64), ("rows", ctypes.c_int64)]
+
+
+class _CCache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("pages", ctypes.c_int64), ("kv_heads", ctypes.c_int64), ("page", ctypes.c_int64), ("D", ctypes.c_int64),
+                ("dtype", ctypes.c_int32)]
+
+
+class _CPagedPlan(ctypes.Structure):
+    _fields_ = [("kernel", ctypes.c_int32), ("rows", ctypes.c_int32), ("parts", ctypes.c_int32), ("grid", ctypes.c_uint32),
+                ("join_grid", ctypes.c_uint32 * 2), ("block", ctypes.c_uint32), ("slots", ctypes.c_int64),
+                ("workspace_bytes", ctypes.c_uint64)]
+
+
+@dataclass
+class PagedPlan:
+    kernel: int
+    rows: int
+    parts: int
+    grid: int
+    join_grid: Tuple[int, int]
+    block: int
+    slots: int
+    workspace_bytes: int
+
+
 @dataclass
 class ProductPlan:
     kernel: int
@@ -153,6 +182,18 @@ def load():
     lib.nimble_grouped_dense_dyn.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, i64, i32, i32, vp]
     lib.nimble_grouped_dense_i8_dyn.argtypes = [vp, vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, i32, i32, vp]
     lib.nimble_product_plan_of.argtypes = [i64, i64, i64, i64, i32, i32, ctypes.POINTER(_CProductPlan)]
+    f64, cache, seqs = ctypes.c_double, ctypes.POINTER(_CCache), ctypes.POINTER(_CSequences)
+    lib.nimble_rotary_shape.argtypes = [ip, i32, ip, i32, ip, i32, ip]
+    lib.nimble_cache_check.argtypes = [ip, i32, ip, i32, ip, i32, ip, i32, i32, ip, i32, ip, i32, ip, i32]
+    lib.nimble_cache_write_shape.argtypes = [ip, ip, i32, ip, i32, ip, i32, ip]
+    lib.nimble_cache_read_shape.argtypes = [ip, i64, ip]
+    lib.nimble_paged_attention_shape.argtypes = [ip, i32, ip, ip]
+    lib.nimble_rotary_table_dyn.argtypes = [vp, i64, i64, f64, f64, f64, f64, f64, f64, vp]
+    lib.nimble_rotary_dyn.argtypes = [vp, i64, vp, vp, i64, vp, i64, i64, i64, i64, i64, i32, vp]
+    lib.nimble_cache_write_dyn.argtypes = [cache, seqs, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, i64, i32, vp]
+    lib.nimble_cache_read_dyn.argtypes = [cache, seqs, vp, vp, i32, vp]
+    lib.nimble_paged_attention_dyn.argtypes = [vp, i64, cache, seqs, vp, i64, ctypes.c_float, i64, vp, ctypes.c_size_t, vp]
+    lib.nimble_paged_attention_plan_of.argtypes = [i64, i64, i64, i64, i64, i64, i64, i32, i64, ctypes.POINTER(_CPagedPlan)]
     _lib = lib
     return lib
 
@@ -389,6 +430,49 @@ def product_plan(R: int, E: Optional[int], N: int, K: int, in_dtype: int = I8, o
     return ProductPlan(c.kernel, c.bm, c.bn, c.k_waves, c.tiles, c.grid, c.block)
 
 
+def rotary_shape(x_shape, positions_shape, table_shape) -> Tuple[int, int, int]:
+    out = (ctypes.c_int64 * 3)(-1, -1, -1)
+    _check(load().nimble_rotary_shape(_arr(x_shape), len(x_shape), _arr(positions_shape), len(positions_shape), _arr(table_shape),
+                                      len(table_shape), out))
+    return int(out[0]), int(out[1]), int(out[2])
+
+
+def cache_check(k_shape, v_shape, k_scale_shape, v_scale_shape, dtype: int, offsets_shape, lengths_shape, pages_shape) -> None:
+    """The extents of a cache and of a batch against each other; scales None unless dtype is I8."""
+    ks, vs = ((None, 0) if s is None else (_arr(s), len(s)) for s in (k_scale_shape, v_scale_shape))
+    _check(load().nimble_cache_check(_arr(k_shape), len(k_shape), _arr(v_shape), len(v_shape), *ks, *vs, dtype, _arr(offsets_shape),
+                                     len(offsets_shape), _arr(lengths_shape), len(lengths_shape), _arr(pages_shape), len(pages_shape)))
+
+
+def cache_write_shape(cache_shape, k_shape, v_shape, q_shape=None) -> Optional[Tuple[int, int, int]]:
+    """The shape of the turned queries, None without any."""
+    out = (ctypes.c_int64 * 3)(-1, -1, -1)
+    q = () if q_shape is None else q_shape
+    if q_shape is not None and len(q) == 0:
+        raise NimbleError(-2, "cache_write: q has rank 0, 3 needed")
+    _check(load().nimble_cache_write_shape(_arr(cache_shape), _arr(k_shape), len(k_shape), _arr(v_shape), len(v_shape), _arr(q), len(q), out))
+    return None if q_shape is None else (int(out[0]), int(out[1]), int(out[2]))
+
+
+def cache_read_shape(cache_shape, rows: int) -> Tuple[int, int, int]:
+    out = (ctypes.c_int64 * 3)(-1, -1, -1)
+    _check(load().nimble_cache_read_shape(_arr(cache_shape), rows, out))
+    return int(out[0]), int(out[1]), int(out[2])
+
+
+def paged_attention_shape(q_shape, cache_shape) -> Tuple[int, int, int]:
+    out = (ctypes.c_int64 * 3)(-1, -1, -1)
+    _check(load().nimble_paged_attention_shape(_arr(q_shape), len(q_shape), _arr(cache_shape), out))
+    return int(out[0]), int(out[1]), int(out[2])
+
+
+def paged_attention_plan(rows: int, count: int, width: int, heads: int, kv_heads: int, page: int, D: int, dtype: int = BF16,
+                         window: int = 0) -> PagedPlan:
+    c = _CPagedPlan()
+    _check(load().nimble_paged_attention_plan_of(rows, count, width, heads, kv_heads, page, D, dtype, window, ctypes.byref(c)))
+    return PagedPlan(c.kernel, c.rows, c.parts, c.grid, (c.join_grid[0], c.join_grid[1]), c.block, c.slots, c.workspace_bytes)
+
+
 # ---------------------------------------------------------------- device side
 # Pointers are integers (tensor.data_ptr()); `stream` is a hipStream_t handle as
 # an integer (torch.cuda.current_stream().cuda_stream), 0 for the default one.
@@ -484,3 +568,36 @@ def nimble_grouped_dense_dyn(x: int, w: int, bias: int, offsets: int, y: int, R:
 def nimble_grouped_dense_i8_dyn(x: int, x_scale: int, w: int, w_scale: int, bias: int, offsets: int, y: int, R: int, E: int, N: int,
                                 K: int, epilogue: int, out_dtype: int = BF16, stream: int = 0) -> None:
     _check(load().nimble_grouped_dense_i8_dyn(x, x_scale, w, w_scale, bias, offsets, y, R, E, N, K, epilogue, out_dtype, stream))
+
+
+def sequences(offsets: int, lengths: int, pages: int, count: int, width: int, rows: int) -> _CSequences:
+    return _CSequences(offsets, lengths, pages, count, width, rows)
+
+
+def cache(k: int, v: int, k_scale: int, v_scale: int, pages: int, kv_heads: int, page: int, D: int, dtype: int) -> _CCache:
+    return _CCache(k, v, k_scale, v_scale, pages, kv_heads, page, D, dtype)
+
+
+def nimble_rotary_table_dyn(table: int, positions: int, rot: int, base: float, factor: float, trained: float, low: float, high: float,
+                            magnitude: float, stream: int = 0) -> None:
+    _check(load().nimble_rotary_table_dyn(table, positions, rot, base, factor, trained, low, high, magnitude, stream))
+
+
+def nimble_rotary_dyn(x: int, x_stride: int, positions: int, table: int, table_rows: int, y: int, y_stride: int, T: int, H: int, D: int,
+                      R: int, interleaved: bool, stream: int = 0) -> None:
+    _check(load().nimble_rotary_dyn(x, x_stride, positions, table, table_rows, y, y_stride, T, H, D, R, int(bool(interleaved)), stream))
+
+
+def nimble_cache_write_dyn(cache: _CCache, seqs: _CSequences, k: int, k_stride: int, v: int, v_stride: int, q: int, q_stride: int, q_out: int,
+                           heads: int, table: int, table_rows: int, R: int, interleaved: bool, stream: int = 0) -> None:
+    _check(load().nimble_cache_write_dyn(cache, seqs, k, k_stride, v, v_stride, q, q_stride, q_out, heads, table, table_rows, R,
+                                         int(bool(interleaved)), stream))
+
+
+def nimble_cache_read_dyn(cache: _CCache, seqs: _CSequences, k_out: int, v_out: int, out_dtype: int = BF16, stream: int = 0) -> None:
+    _check(load().nimble_cache_read_dyn(cache, seqs, k_out, v_out, out_dtype, stream))
+
+
+def nimble_paged_attention_dyn(q: int, q_stride: int, cache: _CCache, seqs: _CSequences, o: int, heads: int, alpha: float, window: int = 0,
+                               workspace: int = 0, workspace_bytes: int = 0, stream: int = 0) -> None:
+    _check(load().nimble_paged_attention_dyn(q, q_stride, cache, seqs, o, heads, alpha, window, workspace, workspace_bytes, stream))

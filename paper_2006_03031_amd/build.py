@@ -10,7 +10,8 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libnimble_hip.so")
 HOST_CALLS = os.path.join(PKG, "_host_calls.so")
 SOURCES = ["nimble_host.cpp", "grouped_host.cpp", "nimble_vm.cpp", "nimble_kernels.hip", "grouped_kernels.hip",
-           "product_bf16_grouped.hip", "product_i8_grouped.hip", "product_i8.hip"]  # the .h files under csrc/ hold the kernels
+           "product_bf16_grouped.hip", "product_i8_grouped.hip", "product_i8.hip",
+           "cache_host.cpp", "cache_kernels.hip", "paged_attention.hip"]  # the .h files under csrc/ hold the kernels
 
 
 FLAGS = [

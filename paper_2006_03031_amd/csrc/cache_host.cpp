@@ -1,0 +1,197 @@
+// Shape functions, checks and the dispatch function of the paged cache's operators: host arithmetic only, no HIP call.
+#include "cache_internal.h"
+
+#include <cmath>
+
+namespace nimble {
+
+static bool misaligned(const void* p, unsigned to = 16) { return ((uintptr_t)p & (to - 1)) != 0; }
+
+static int check_layout(int64_t pages, int64_t kv_heads, int64_t page, int64_t D, int dtype) {
+  if (dtype != NIMBLE_BF16 && dtype != NIMBLE_I8) return fail(NIMBLE_ERR_DTYPE, "cache: dtype %d, bf16 or int8 needed", dtype);
+  if (pages < 0 || kv_heads < 0 || page < 0 || D < 0) return fail(NIMBLE_ERR_ARG, "negative extent");
+  if (D != 64 && D != 128) return fail(NIMBLE_ERR_ARG, "cache: heads of %lld, 64 or 128 needed", (long long)D);
+  if (page < 16 || page > 1024 || (page & (page - 1))) return fail(NIMBLE_ERR_ARG, "cache: pages of %lld, a power of two from 16 to 1024 needed", (long long)page);
+  if (kv_heads < 1 || kv_heads > 1024) return fail(NIMBLE_ERR_ARG, "cache: %lld heads, 1 to 1024 needed", (long long)kv_heads);
+  if (pages > (1ll << 31) - 1) return fail(NIMBLE_ERR_ARG, "extent too large");
+  return NIMBLE_OK;
+}
+
+int check_cache(const nimble_cache* c) {
+  if (!c) return fail(NIMBLE_ERR_NULL, "null cache");
+  const int rc = check_layout(c->pages, c->kv_heads, c->page, c->D, c->dtype);
+  if (rc != NIMBLE_OK) return rc;
+  if (c->pages == 0) return NIMBLE_OK;
+  const bool int8 = c->dtype == NIMBLE_I8;
+  if (!c->k || !c->v || (int8 && (!c->k_scale || !c->v_scale))) return fail(NIMBLE_ERR_NULL, "null cache pointer");
+  if (misaligned(c->k) || misaligned(c->v) || (int8 && (misaligned(c->k_scale) || misaligned(c->v_scale))))
+    return fail(NIMBLE_ERR_ALIGN, "device pointers must be 16-byte aligned");
+  return NIMBLE_OK;
+}
+
+static int check_counts(int64_t rows, int64_t count, int64_t width, int64_t page) {
+  if (rows < 0 || count < 0 || width < 0) return fail(NIMBLE_ERR_ARG, "negative extent");
+  if (rows > kMostRows || count > kMostSequences) return fail(NIMBLE_ERR_ARG, "%lld rows of %lld sequences, at most %lld of %lld", (long long)rows, (long long)count,
+                                                              (long long)kMostRows, (long long)kMostSequences);
+  if (width > kMostPositions / page) return fail(NIMBLE_ERR_ARG, "page table of %lld pages of %lld: more than 2^30 positions", (long long)width, (long long)page);
+  return NIMBLE_OK;
+}
+
+int check_sequences(const nimble_sequences* s, int64_t page) {
+  if (!s) return fail(NIMBLE_ERR_NULL, "null sequences");
+  const int rc = check_counts(s->rows, s->count, s->width, page);
+  if (rc != NIMBLE_OK) return rc;
+  if (s->rows == 0 || s->count == 0) return NIMBLE_OK;
+  if (!s->offsets || !s->lengths || (s->width > 0 && !s->pages)) return fail(NIMBLE_ERR_NULL, "null sequences pointer");
+  if (misaligned(s->offsets, 8) || misaligned(s->lengths, 8) || misaligned(s->pages, 4))
+    return fail(NIMBLE_ERR_ALIGN, "offsets and lengths must be 8-byte aligned, pages 4-byte");
+  return NIMBLE_OK;
+}
+
+CacheArgs cache_args(const nimble_cache& c) {
+  CacheArgs a{(unsigned char*)c.k, (unsigned char*)c.v, (float*)c.k_scale, (float*)c.v_scale, (unsigned)c.pages, (int)c.kv_heads, 0};
+  while ((1ll << a.page_shift) < c.page) ++a.page_shift;
+  return a;
+}
+
+SequencesArgs sequences_args(const nimble_sequences& s) {
+  return SequencesArgs{(const long long*)s.offsets, (const long long*)s.lengths, (const int*)s.pages, (int)s.count, (int)s.width, (int)s.rows};
+}
+
+// ------------------------------------------------------------------------------------------------ attention
+// Workgroups that a compute unit holds at once, and the least number of key blocks that is worth a part of its own.
+struct PagedMember {
+  int rows, block_keys, target_units, least_blocks;
+};
+static const PagedMember kPagedMembers[NIMBLE_PAGED_COUNT] = {{16, 32, 512, 8}, {128, 64, 256, 4}};
+
+static int plan_paged(int64_t rows, int64_t count, int64_t width, int64_t heads, int64_t kv_heads, int64_t page, int64_t D, int dtype,
+                      int64_t window, nimble_paged_plan* p) {
+  int rc = check_layout(0, kv_heads, page, D, dtype);
+  if (rc == NIMBLE_OK) rc = check_counts(rows, count, width, page);
+  if (rc != NIMBLE_OK) return rc;
+  if (heads < 1 || heads > 65536 || heads % kv_heads) return fail(heads < 1 || heads > 65536 ? NIMBLE_ERR_ARG : NIMBLE_ERR_SHAPE, "%lld query heads over %lld of the cache", (long long)heads, (long long)kv_heads);
+  if (window < 0) return fail(NIMBLE_ERR_ARG, "negative window");
+  nimble_paged_plan out{};
+  out.kernel = NIMBLE_PAGED_TOKENS;
+  const PagedMember& m = kPagedMembers[out.kernel];
+  const int64_t group = heads / kv_heads, live = count < rows ? count : rows;
+  const int64_t tiles = rows * group / m.rows + live;   // a sequence adds at most one that is not full
+  // the keys that a tile can see
+  int64_t keys = width * page;
+  if (window > 0 && window + m.rows < keys) keys = window + m.rows;
+  out.rows = m.rows;
+  out.block = 256;
+  out.parts = keys > (int64_t)m.block_keys * m.least_blocks;
+  if (tiles * kv_heads > kMostPagedGrid) return fail(NIMBLE_ERR_ARG, "more than 2^23 tiles");
+  out.grid = (uint32_t)(tiles * kv_heads + (out.parts ? m.target_units : 0));
+  if (out.parts) {
+    out.slots = 2 * m.target_units + 8;
+    const int64_t items = tiles * kv_heads < out.slots / 2 ? tiles * kv_heads : out.slots / 2;
+    out.join_grid[0] = (uint32_t)items;
+    out.join_grid[1] = (uint32_t)(rows * group < m.rows ? rows * group : m.rows);
+    out.workspace_bytes = (uint64_t)out.slots * m.rows * (D * 4 + 8) + (uint64_t)(1 + out.slots / 2) * kPagedItemWords * 4;
+  }
+  *p = out;
+  return NIMBLE_OK;
+}
+
+}  // namespace nimble
+
+using namespace nimble;
+
+extern "C" {
+
+int nimble_rotary_shape(const int64_t* x_shape, int x_rank, const int64_t* positions_shape, int positions_rank, const int64_t* table_shape,
+                        int table_rank, int64_t* out_shape) {
+  clear_error();
+  if (!x_shape || !positions_shape || !table_shape || !out_shape) return fail(NIMBLE_ERR_NULL, "null shape pointer");
+  if (x_rank != 3 || positions_rank != 1 || table_rank != 3)
+    return fail(NIMBLE_ERR_RANK, "rotary: ranks of x, positions, table are %d, %d, %d; 3, 1, 3 needed", x_rank, positions_rank, table_rank);
+  for (int i = 0; i < 3; ++i)
+    if (x_shape[i] < 0 || table_shape[i] < 0) return fail(NIMBLE_ERR_ARG, "negative extent");
+  if (positions_shape[0] != x_shape[0])
+    return fail(NIMBLE_ERR_SHAPE, "rotary: %lld positions for %lld rows", (long long)positions_shape[0], (long long)x_shape[0]);
+  if (table_shape[2] != 2 || table_shape[1] > x_shape[2] / 2)
+    return fail(NIMBLE_ERR_SHAPE, "rotary: a table of (%lld, %lld, %lld) for heads of %lld; (positions, pairs, 2) needed", (long long)table_shape[0],
+                (long long)table_shape[1], (long long)table_shape[2], (long long)x_shape[2]);
+  for (int i = 0; i < 3; ++i) out_shape[i] = x_shape[i];
+  return NIMBLE_OK;
+}
+
+int nimble_cache_check(const int64_t* k_shape, int k_rank, const int64_t* v_shape, int v_rank, const int64_t* k_scale_shape,
+                       int k_scale_rank, const int64_t* v_scale_shape, int v_scale_rank, int dtype, const int64_t* offsets_shape,
+                       int offsets_rank, const int64_t* lengths_shape, int lengths_rank, const int64_t* pages_shape, int pages_rank) {
+  clear_error();
+  const bool int8 = dtype == NIMBLE_I8;
+  if (!k_shape || !v_shape || !offsets_shape || !lengths_shape || !pages_shape || (int8 && (!k_scale_shape || !v_scale_shape)))
+    return fail(NIMBLE_ERR_NULL, "null shape pointer");
+  if (k_rank != 4 || v_rank != 4 || (int8 && (k_scale_rank != 3 || v_scale_rank != 3)))
+    return fail(NIMBLE_ERR_RANK, "cache: keys and values of rank 4 and scales of rank 3 needed");
+  if (offsets_rank != 1 || lengths_rank != 1 || pages_rank != 2)
+    return fail(NIMBLE_ERR_RANK, "sequences: ranks of offsets, lengths, pages are %d, %d, %d; 1, 1, 2 needed", offsets_rank, lengths_rank, pages_rank);
+  const int rc = check_layout(k_shape[0], k_shape[1], k_shape[2], k_shape[3], dtype);
+  if (rc != NIMBLE_OK) return rc;
+  for (int i = 0; i < 4; ++i)
+    if (v_shape[i] != k_shape[i]) return fail(NIMBLE_ERR_SHAPE, "cache: keys and values differ in extent %d", i);
+  for (int i = 0; int8 && i < 3; ++i)
+    if (k_scale_shape[i] != k_shape[i] || v_scale_shape[i] != k_shape[i]) return fail(NIMBLE_ERR_SHAPE, "cache: scales differ from the codes in extent %d", i);
+  if (lengths_shape[0] < 0 || pages_shape[0] < 0 || pages_shape[1] < 0) return fail(NIMBLE_ERR_ARG, "negative extent");
+  if (offsets_shape[0] != lengths_shape[0] + 1 || pages_shape[0] != lengths_shape[0])
+    return fail(NIMBLE_ERR_SHAPE, "sequences: %lld offsets and %lld rows of pages for %lld lengths", (long long)offsets_shape[0], (long long)pages_shape[0],
+                (long long)lengths_shape[0]);
+  return check_counts(0, lengths_shape[0], pages_shape[1], k_shape[2]);
+}
+
+int nimble_cache_write_shape(const int64_t* cache_shape, const int64_t* k_shape, int k_rank, const int64_t* v_shape, int v_rank,
+                             const int64_t* q_shape, int q_rank, int64_t* q_out_shape) {
+  clear_error();
+  if (!cache_shape || !k_shape || !v_shape || (q_rank && (!q_shape || !q_out_shape))) return fail(NIMBLE_ERR_NULL, "null shape pointer");
+  if (k_rank != 3 || v_rank != 3 || (q_rank && q_rank != 3))
+    return fail(NIMBLE_ERR_RANK, "cache_write: ranks of k, v, q are %d, %d, %d; 3 needed", k_rank, v_rank, q_rank);
+  for (int i = 0; i < 3; ++i) {
+    if (k_shape[i] < 0 || v_shape[i] < 0 || (q_rank && q_shape[i] < 0)) return fail(NIMBLE_ERR_ARG, "negative extent");
+    if (k_shape[i] != v_shape[i]) return fail(NIMBLE_ERR_SHAPE, "cache_write: keys and values differ in extent %d", i);
+  }
+  if (k_shape[1] != cache_shape[1] || k_shape[2] != cache_shape[3])
+    return fail(NIMBLE_ERR_SHAPE, "cache_write: %lld heads of %lld for a cache of %lld of %lld", (long long)k_shape[1], (long long)k_shape[2],
+                (long long)cache_shape[1], (long long)cache_shape[3]);
+  if (!q_rank) return NIMBLE_OK;
+  if (q_shape[0] != k_shape[0] || q_shape[2] != k_shape[2])
+    return fail(NIMBLE_ERR_SHAPE, "cache_write: queries (%lld, ., %lld), keys (%lld, ., %lld)", (long long)q_shape[0], (long long)q_shape[2],
+                (long long)k_shape[0], (long long)k_shape[2]);
+  for (int i = 0; i < 3; ++i) q_out_shape[i] = q_shape[i];
+  return NIMBLE_OK;
+}
+
+int nimble_cache_read_shape(const int64_t* cache_shape, int64_t rows, int64_t* out_shape) {
+  clear_error();
+  if (!cache_shape || !out_shape) return fail(NIMBLE_ERR_NULL, "null shape pointer");
+  if (rows < 0 || cache_shape[1] < 0 || cache_shape[3] < 0) return fail(NIMBLE_ERR_ARG, "negative extent");
+  out_shape[0] = rows;
+  out_shape[1] = cache_shape[1];
+  out_shape[2] = cache_shape[3];
+  return NIMBLE_OK;
+}
+
+int nimble_paged_attention_shape(const int64_t* q_shape, int q_rank, const int64_t* cache_shape, int64_t* out_shape) {
+  clear_error();
+  if (!q_shape || !cache_shape || !out_shape) return fail(NIMBLE_ERR_NULL, "null shape pointer");
+  if (q_rank != 3) return fail(NIMBLE_ERR_RANK, "paged_attention: q has rank %d, 3 needed", q_rank);
+  for (int i = 0; i < 3; ++i)
+    if (q_shape[i] < 0) return fail(NIMBLE_ERR_ARG, "negative extent");
+  if (q_shape[2] != cache_shape[3]) return fail(NIMBLE_ERR_SHAPE, "paged_attention: heads of %lld, of the cache %lld", (long long)q_shape[2], (long long)cache_shape[3]);
+  if (q_shape[1] < 1 || cache_shape[1] < 1 || q_shape[1] % cache_shape[1])
+    return fail(NIMBLE_ERR_SHAPE, "paged_attention: %lld query heads over %lld of the cache", (long long)q_shape[1], (long long)cache_shape[1]);
+  for (int i = 0; i < 3; ++i) out_shape[i] = q_shape[i];
+  return NIMBLE_OK;
+}
+
+int nimble_paged_attention_plan_of(int64_t rows, int64_t count, int64_t width, int64_t heads, int64_t kv_heads, int64_t page, int64_t D,
+                                   int dtype, int64_t window, nimble_paged_plan* plan) {
+  clear_error();
+  if (!plan) return fail(NIMBLE_ERR_NULL, "null plan pointer");
+  return plan_paged(rows, count, width, heads, kv_heads, page, D, dtype, window, plan);
+}
+
+}  // extern "C"

@@ -1,0 +1,40 @@
+// What the paged cache's operators share between host and device: arguments, limits.
+#ifndef NIMBLE_CACHE_INTERNAL_H_
+#define NIMBLE_CACHE_INTERNAL_H_
+#include "nimble_internal.h"
+
+namespace nimble {
+
+// nimble_sequences and nimble_cache as the kernels take them.
+struct SequencesArgs {
+  const long long* offsets;
+  const long long* lengths;
+  const int* pages;
+  int count, width, rows;
+};
+struct CacheArgs {
+  unsigned char* k;
+  unsigned char* v;
+  float* k_scale;
+  float* v_scale;
+  unsigned pages;
+  int kv_heads, page_shift;
+};
+
+// A launch is of fewer than 2^32 threads.
+constexpr int64_t kMostPagedGrid = 1 << 23;
+// Sequences are looked for 64 by 64 (PagedUnit), positions and rows are 32-bit numbers.
+constexpr int64_t kMostSequences = 1 << 16, kMostPositions = 1ll << 30, kMostRows = 1ll << 24;
+constexpr int kPagedItemWords = 8;
+
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+int check_hip_launch(const char* what);
+
+int check_cache(const nimble_cache* c);
+int check_sequences(const nimble_sequences* s, int64_t page);
+CacheArgs cache_args(const nimble_cache& c);
+SequencesArgs sequences_args(const nimble_sequences& s);
+
+}  // namespace nimble
+#endif

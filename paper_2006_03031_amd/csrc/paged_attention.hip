@@ -1,0 +1,70 @@
+// Device entry point of attention over a paged cache (kernels: paged_attention_kernel.h).
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+
+#include "paged_attention_kernel.h"
+
+namespace nimble {
+
+int check_rows(const void* p, int64_t stride, int64_t heads, int64_t D, const char* what);  // (cache_kernels.hip)
+
+template <int D>
+static void launch_paged(const PagedArgs& g, const nimble_paged_plan& p, bool int8, hipStream_t stream) {
+  if (int8)
+    hipLaunchKernelGGL((paged_tokens_kernel<D, true>), dim3(p.grid), dim3(p.block), 0, stream, g);
+  else
+    hipLaunchKernelGGL((paged_tokens_kernel<D, false>), dim3(p.grid), dim3(p.block), 0, stream, g);
+  if (p.parts) hipLaunchKernelGGL((paged_join_kernel<16, D>), dim3(p.join_grid[0], p.join_grid[1]), dim3(256), 0, stream, g);
+}
+
+}  // namespace nimble
+
+using namespace nimble;
+
+extern "C" {
+
+int nimble_paged_attention_dyn(const void* q, int64_t q_stride, const nimble_cache* cache, const nimble_sequences* seqs, void* o,
+                               int64_t heads, float alpha, int64_t window, void* workspace, size_t workspace_bytes, void* stream) {
+  clear_error();
+  int rc = check_cache(cache);
+  if (rc == NIMBLE_OK) rc = check_sequences(seqs, cache->page);
+  if (rc != NIMBLE_OK) return rc;
+  if (!(alpha > 0) || !std::isfinite(alpha)) return fail(NIMBLE_ERR_ARG, "paged_attention: alpha = %g, more than 0 needed", (double)alpha);
+  nimble_paged_plan p;
+  rc = nimble_paged_attention_plan_of(seqs->rows, seqs->count, seqs->width, heads, cache->kv_heads, cache->page, cache->D, cache->dtype, window, &p);
+  if (rc != NIMBLE_OK) return rc;
+  if (seqs->rows == 0 || seqs->count == 0) return NIMBLE_OK;
+  rc = check_rows(q, q_stride, heads, cache->D, "paged_attention: q");
+  if (rc != NIMBLE_OK) return rc;
+  if (!o) return fail(NIMBLE_ERR_NULL, "null tensor pointer");
+  if (((uintptr_t)o | (uintptr_t)workspace) & 15) return fail(NIMBLE_ERR_ALIGN, "device pointers must be 16-byte aligned");
+  if (p.workspace_bytes && (!workspace || workspace_bytes < p.workspace_bytes))
+    return fail(NIMBLE_ERR_WORKSPACE, "paged_attention: workspace of %llu bytes needed", (unsigned long long)p.workspace_bytes);
+  PagedArgs g{};
+  g.cache = cache_args(*cache);
+  g.seqs = sequences_args(*seqs);
+  if (cache->pages == 0) g.seqs.width = 0;  // nothing is cached
+  g.q = (const uint16_t*)q;
+  g.o = (uint16_t*)o;
+  g.q_stride = q_stride;
+  g.heads = (int)heads;
+  g.group = (int)(heads / cache->kv_heads);
+  g.window = (int)(window < kMostPositions ? window : 0);  // (2^30 and beyond: all)
+  g.a2 = alpha * 1.4426950408889634f;
+  if (!std::isfinite(g.a2)) return fail(NIMBLE_ERR_ARG, "paged_attention: alpha = %g is too large", (double)alpha);
+  if (p.parts) {
+    g.slots = (int)p.slots;
+    g.target_units = (int)(p.slots - 8) / 2;
+    g.part = (float*)workspace;
+    g.stat = (float2*)(g.part + p.slots * p.rows * cache->D);
+    g.items = (int*)(g.stat + p.slots * p.rows);
+  }
+  if (cache->D == 64)
+    launch_paged<64>(g, p, cache->dtype == NIMBLE_I8, (hipStream_t)stream);
+  else
+    launch_paged<128>(g, p, cache->dtype == NIMBLE_I8, (hipStream_t)stream);
+  return check_hip_launch("paged attention kernel launch");
+}
+
+}  // extern "C"

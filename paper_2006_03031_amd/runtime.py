@@ -11,7 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import warnings
-from typing import Optional, Tuple
+from typing import NamedTuple, Optional, Tuple
 
 import torch
 
@@ -353,6 +353,143 @@ def grouped_dense_i8(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_
                                        x.shape[1], epilogue, out_dtype, _stream())
     if not _bound:
         _bind_host_calls(x.device)
+    return y
+
+
+class Sequences(NamedTuple):
+    """The rows of one call, on the GPU: rows offsets[s] .. offsets[s+1]-1 are the new tokens of sequence s, the last of its lengths[s];
+    position p of it is in slot p % page of page pages[s, p // page].  offsets [S+1] and lengths [S] int64, pages [S, W] int32."""
+    offsets: torch.Tensor
+    lengths: torch.Tensor
+    pages: torch.Tensor
+
+
+class PagedCache(NamedTuple):
+    """Keys and values of sequences in pages: k, v [pages, kv_heads, page, D] bf16, or int8 with scales [pages, kv_heads, page] f32.  page is a
+    power of two from 16 to 1024, D 64 or 128."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: Optional[torch.Tensor] = None
+    v_scale: Optional[torch.Tensor] = None
+
+    @staticmethod
+    def empty(pages: int, kv_heads: int, page: int, D: int, dtype: int = nb.BF16, device="cuda") -> "PagedCache":
+        shape = (pages, kv_heads, page, D)
+        scales = shape[:3] if dtype == nb.I8 else None
+        nb.cache_check(shape, shape, scales, scales, dtype, (1,), (0,), (0, 0))
+        k, v = (_alloc(shape, dtype, device) for _ in range(2))
+        return PagedCache(k, v, *((_alloc(scales, nb.F32, device) for _ in range(2)) if scales else (None, None)))
+
+
+def _paged(cache: PagedCache, sequences: Sequences, rows: int):
+    """The checked descriptions of a cache and a batch as the C ABI takes them."""
+    k, v, ks, vs = cache
+    if k.dtype not in (_BF, torch.int8):
+        raise nb.NimbleError(-4, f"cache: keys are {k.dtype}, bf16 or int8 needed")
+    int8 = k.dtype is torch.int8
+    if int8 and (ks is None or vs is None):
+        raise nb.NimbleError(-1, "cache: 8-bit codes need scales")
+    off, lengths, pages = sequences
+    dtype = nb.I8 if int8 else nb.BF16
+    nb.cache_check(tuple(k.shape), tuple(v.shape), tuple(ks.shape) if int8 else None, tuple(vs.shape) if int8 else None, dtype,
+                   tuple(off.shape), tuple(lengths.shape), tuple(pages.shape))
+    c = nb.cache(_ptr(k, k.dtype, "k"), _ptr(v, k.dtype, "v"), _ptr(ks, _F32, "k_scale") if int8 else 0,
+                 _ptr(vs, _F32, "v_scale") if int8 else 0, *k.shape, dtype)
+    s = nb.sequences(_ptr(off, torch.int64, "offsets"), _ptr(lengths, torch.int64, "lengths"), _ptr(pages, torch.int32, "pages"),
+                     lengths.shape[0], pages.shape[1], rows)
+    return c, s
+
+
+def _rows_ptr(t: torch.Tensor, what: str) -> Tuple[int, int]:
+    """Address and row stride of heads [T, H, D] that lie one after the other within a row, the rows any stride apart."""
+    if t.dtype is not _BF or not t.is_cuda or (t.numel() and (t.stride(2) != 1 and t.shape[2] > 1 or t.stride(1) != t.shape[2] and t.shape[1] > 1)):
+        raise nb.NimbleError(-4 if t.dtype is not _BF else -8, f"{what}: need a {_BF} tensor on the GPU whose heads are contiguous, got {t.dtype}, "
+                                                               f"device {t.device}, strides {tuple(t.stride())}")
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+def rotary_table(positions: int, rot: int, base: float = 10000.0, factor: float = 1.0, trained: float = 0.0, low: float = 1.0,
+                 high: float = 32.0, magnitude: float = 1.0, device="cuda") -> torch.Tensor:
+    """cos and sin, times `magnitude`, of the angles position * f_i of `rot` turned elements: f32 [positions, rot/2, 2], computed in f64.
+    f_i = base^(-2i/rot).  For contexts `factor` times as long as the trained ones f_i is divided by factor where pair i makes fewer than `low`
+    turns within `trained` positions, kept where it makes more than `high`, blended between; trained = 0: all are divided."""
+    shape = (int(positions), int(rot) // 2, 2)
+    table = _alloc(shape, nb.F32, device)
+    with _together(table=table):
+        nb.nimble_rotary_table_dyn(table.data_ptr(), positions, rot, base, factor, trained, low, high, magnitude, _stream())
+    return table
+
+
+def rotary(x: torch.Tensor, positions: torch.Tensor, table: torch.Tensor, interleaved: bool = False,
+           out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Rotary positions: the first 2R elements of each head of x [T, H, D] (bf16, rows any stride apart) turned in pairs (i, i + R), or (2i, 2i + 1)
+    where interleaved, by table[positions[t]] of [P, R, 2] (rotary_table); the rest copied.  positions [T] int64; out may be x."""
+    shape = nb.rotary_shape(tuple(x.shape), tuple(positions.shape), tuple(table.shape))
+    with _together(x=x, positions=positions, table=table, out=out):
+        y = out if out is not None else _alloc(shape, nb.BF16, x.device)
+        if tuple(y.shape) != shape:
+            raise nb.NimbleError(-3, f"rotary: out is {tuple(y.shape)}, the shape function gives {shape}")
+        px, xs = _rows_ptr(x, "x")
+        py, ys = _rows_ptr(y, "out")
+        nb.nimble_rotary_dyn(px, xs, _ptr(positions, torch.int64, "positions"), _ptr(table, _F32, "table"), table.shape[0], py, ys, *shape,
+                             table.shape[1], interleaved, _stream())
+    return y
+
+
+def cache_write(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, sequences: Sequences, q: Optional[torch.Tensor] = None,
+                table: Optional[torch.Tensor] = None, interleaved: bool = False, out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """Keys and values k, v [T, kv_heads, D] of a batch's rows into their places of the cache; with a table (rotary_table) the keys are
+    turned by their positions first, and the queries q [T, heads, D] with them: returns these, contiguous (`out` may be q), or None without q.
+    An 8-bit cache holds each token and head as quantize_rows does.  k, v and q may be parts of wider rows."""
+    shape = nb.cache_write_shape(tuple(cache.k.shape), tuple(k.shape), tuple(v.shape), None if q is None else tuple(q.shape))
+    if table is not None and (table.dim() != 3 or table.shape[2] != 2):
+        raise nb.NimbleError(-3, f"cache_write: a table of {tuple(table.shape)}, (positions, pairs, 2) needed")
+    if q is None and out is not None:
+        raise nb.NimbleError(-8, "cache_write: out without q")
+    with _together(k=k, v=v, q=q, table=table, out=out, cache_k=cache.k, cache_v=cache.v, k_scale=cache.k_scale, v_scale=cache.v_scale,
+                   **sequences._asdict()):
+        c, s = _paged(cache, sequences, k.shape[0])
+        y = out
+        if q is not None and out is None:
+            y = _alloc(shape, nb.BF16, k.device)
+        elif q is not None and tuple(out.shape) != shape:
+            raise nb.NimbleError(-3, f"cache_write: out is {tuple(out.shape)}, the shape function gives {shape}")
+        nb.nimble_cache_write_dyn(c, s, *_rows_ptr(k, "k"), *_rows_ptr(v, "v"), *(_rows_ptr(q, "q") if q is not None else (0, 0)),
+                                  _ptr(y, _BF, "out") if q is not None else 0, q.shape[1] if q is not None else 0,
+                                  *((_ptr(table, _F32, "table"), table.shape[0], table.shape[1]) if table is not None else (0, 0, 0)),
+                                  interleaved, _stream())
+    return y
+
+
+def cache_read(cache: PagedCache, sequences: Sequences, rows: int, out_dtype: int = nb.BF16,
+               out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """The keys and values of a batch's rows back out of the cache, each [rows, kv_heads, D] of out_dtype: the inverse of cache_write.  offsets that
+    count each sequence's whole length read all of it.  Rows of no sequence are left as they were in `out`."""
+    shape = nb.cache_read_shape(tuple(cache.k.shape), rows)
+    ko, vo = out if out is not None else (None, None)
+    with _together(cache_k=cache.k, cache_v=cache.v, k_scale=cache.k_scale, v_scale=cache.v_scale, k_out=ko, v_out=vo, **sequences._asdict()):
+        c, s = _paged(cache, sequences, rows)
+        ko, vo = (_output(t, shape, out_dtype, cache.k.device, "cache_read") for t in (ko, vo))
+        nb.nimble_cache_read_dyn(c, s, _ptr(ko, _TORCH_DTYPE[out_dtype], "k_out"), _ptr(vo, _TORCH_DTYPE[out_dtype], "v_out"), out_dtype, _stream())
+    return ko, vo
+
+
+def paged_attention(q: torch.Tensor, cache: PagedCache, sequences: Sequences, alpha: Optional[float] = None, window: int = 0,
+                    out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of a batch's rows q [T, heads, D] over their sequences in the cache, what cache_write has just put there included: row i of a
+    sequence, at position p, sees the keys max(0, p - window + 1) .. p (window = 0: all up to p); heads is a multiple of the cache's, whose
+    heads / kv_heads query heads share keys.  alpha: 1 / sqrt(D) unless given.  A token of each sequence and chunks of many are served alike.
+    workspace: of nb.paged_attention_plan's size, for one call at a time; by default a new one, so that calls may overlap."""
+    shape = nb.paged_attention_shape(tuple(q.shape), tuple(cache.k.shape))
+    with _together(q=q, out=out, workspace=workspace, cache_k=cache.k, cache_v=cache.v, k_scale=cache.k_scale, v_scale=cache.v_scale,
+                   **sequences._asdict()):
+        c, s = _paged(cache, sequences, q.shape[0])
+        y = _output(out, shape, nb.BF16, q.device, "paged_attention")
+        if workspace is None:
+            need = nb.paged_attention_plan(shape[0], s.count, s.width, shape[1], c.kv_heads, c.page, c.D, c.dtype, window).workspace_bytes
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        nb.nimble_paged_attention_dyn(*_rows_ptr(q, "q"), c, s, _ptr(y, _BF, "out"), shape[1], alpha if alpha is not None else shape[2] ** -0.5,
+                                      window, workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream())
     return y
 
 

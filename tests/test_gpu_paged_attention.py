@@ -1,0 +1,250 @@
+"""paged_attention against the formula in 64 bits: types, head layouts, pages, lengths, masks that leave nothing, values behind masks, graphs."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+import paged_util as pu
+from paged_util import BF, Batch
+
+
+def _q(batch, H, D, seed=3):
+    return torch.randn(batch.rows, H, D, generator=torch.Generator().manual_seed(seed)).to(BF)
+
+
+def _run(q, cache, batch, **kw):
+    from paper_2006_03031_amd import runtime as rt
+    kw = {k: v.cuda() if torch.is_tensor(v) else v for k, v in kw.items()}
+    return rt.paged_attention(q.cuda(), pu.to_gpu(cache), batch.on_gpu(), **kw)
+
+
+def _check(got, q, cache, batch, window=0, alpha=None):
+    want, bound = pu.attention(q, cache, batch, window, alpha)
+    got = got.double().cpu()
+    rows = [r for _, r, _ in batch.each()]
+    off = ((got - want).abs() - bound)[rows]
+    assert bool((off <= 0).all()), f"beyond the bound by up to {float(off.max())} (NaN: {int(got[rows].isnan().sum())})"
+
+
+SHAPES = [(1, 1), (4, 1), (6, 2), (16, 16), (24, 8), (20, 1), (32, 2)]
+SIZES = {
+    "one": [(0, 1)],
+    "two_tokens": [(0, 2)],
+    "short": [(4, 1), (0, 1), (16, 1), (14, 1), (31, 1), (32, 1), (63, 1)],
+    "empty_ones": [(0, 0), (30, 1), (0, 0), (5, 3), (0, 0)],
+    "ragged": [(0, 37), (100, 1), (63, 5), (0, 1), (257, 20), (15, 2)],
+    "long": [(700, 1), (3, 1)],
+}
+
+
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("H,G", SHAPES)
+@pytest.mark.parametrize("sizes", SIZES)
+def test_formula(sizes, H, G, D, int8):
+    batch = Batch(SIZES[sizes], 16)
+    cache, q = pu.random_cache(batch, G, D, int8), _q(batch, H, D)
+    _check(_run(q, cache, batch), q, cache, batch)
+
+
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("page", [16, 32, 64, 128, 1024])
+def test_pages(page, D, int8):
+    batch = Batch([(0, 19), (100, 7), (page - 1, 1), (page, 1), (2 * page - 3, 9)], page)
+    cache, q = pu.random_cache(batch, 2, D, int8), _q(batch, 6, D)
+    _check(_run(q, cache, batch), q, cache, batch)
+
+
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("window", [1, 2, 15, 16, 17, 33, 100, 5000])
+def test_window(window, D, int8):
+    batch = Batch([(0, 40), (300, 1), (77, 50), (0, 1), (1000, 3)], 16)
+    cache, q = pu.random_cache(batch, 2, D, int8), _q(batch, 4, D)
+    _check(_run(q, cache, batch, window=window), q, cache, batch, window)
+
+
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("sizes", [[(4999, 1)], [(3000, 1), (0, 1), (1000, 1), (9000, 1)], [(2000, 40), (6000, 3)], [(2047, 1), (2048, 1), (2049, 2)]])
+@pytest.mark.parametrize("H,G,D", [(8, 2, 64), (5, 1, 128)])
+def test_sequences_that_are_cut(H, G, D, sizes, int8):
+    batch = Batch(sizes, 32)
+    cache, q = pu.random_cache(batch, G, D, int8), _q(batch, H, D)
+    _check(_run(q, cache, batch), q, cache, batch)
+
+
+@pytest.mark.parametrize("count", [65, 300])
+def test_many_sequences(count):
+    batch = Batch([(i * 7 % 90, i % 3) for i in range(count)], 16)
+    cache, q = pu.random_cache(batch, 2, 64, False), _q(batch, 4, 64)
+    _check(_run(q, cache, batch), q, cache, batch)
+
+
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("alpha", [1e-3, 1.0, 30.0])
+def test_scale(alpha, int8):
+    batch = Batch([(50, 3), (700, 1)], 16)
+    cache, q = pu.random_cache(batch, 1, 64, int8), _q(batch, 2, 64)
+    _check(_run(q, cache, batch, alpha=alpha), q, cache, batch, alpha=alpha)
+
+
+def test_rows_of_no_sequence_are_left():
+    batch = Batch([(20, 3), (0, 5)], 16, ahead=3, behind=4)
+    cache, q = pu.random_cache(batch, 2, 64, False), _q(batch, 4, 64)
+    out = torch.full((batch.rows, 4, 64), 7.0, dtype=BF)
+    got = _run(q, cache, batch, out=out)
+    _check(got, q, cache, batch)
+    assert bool((got[:3] == 7).all()) and bool((got[-4:] == 7).all())
+
+
+@pytest.mark.parametrize("int8", [False, True])
+def test_rows_that_see_nothing_are_zero(int8):
+    """More new rows than the sequence has tokens: the first are at positions below 0."""
+    batch = Batch([(-4, 9), (30, 2), (-3, 3)], 16)
+    cache, q = pu.random_cache(batch, 2, 64, int8), _q(batch, 4, 64)
+    got = _run(q, cache, batch)
+    _check(got, q, cache, batch)
+    assert bool((got[:4] == 0).all()) and bool((got[-3:] == 0).all())
+
+
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("old", [20, 900])
+def test_what_a_row_does_not_see_has_no_part(old, bad):
+    """Values and keys of later rows, of keys ahead of the window and of slots behind the sequence that are infinite or NaN."""
+    batch = Batch([(old, 6), (40, 1)], 16)
+    cache, q = pu.random_cache(batch, 2, 64, False), _q(batch, 4, 64)
+    want, bound = pu.attention(q, cache, batch, 11)
+    k, v = cache[0].clone(), cache[1].clone()
+    page, slot = batch.slots(0, torch.tensor([old + 5]))    # the last row's own
+    v[page, 0, slot, 3] = bad
+    k[page, 1, slot, 3] = bad
+    page, slot = batch.slots(0, torch.tensor([old - 11]))   # just ahead of every window
+    v[page, :, slot] = bad
+    k[page, :, slot] = bad
+    tail = torch.arange(41, 48)                              # behind the second sequence, on its last page
+    page, slot = batch.slots(1, tail)
+    v[page, :, slot] = bad
+    k[page, :, slot] = bad
+    got = _run(q, (k, v, None, None), batch, window=11).double().cpu()
+    rows = [0, 1, 2, 3, 4, 6]
+    assert bool((got[rows] - want[rows]).abs().le(bound[rows]).all())
+    assert not bool(got[5, :2, 3].isfinite().any())         # the row that sees it, the heads that share it
+    keep = [d for d in range(64) if d != 3]
+    assert bool((got[5, :2][:, keep] - want[5, :2][:, keep]).abs().le(bound[5, :2][:, keep]).all())
+
+
+def test_pages_ahead_of_the_window_may_be_gone():
+    batch = Batch([(500, 3)], 16)
+    cache, q = pu.random_cache(batch, 2, 64, False), _q(batch, 4, 64)
+    want, bound = pu.attention(q, cache, batch, 40)
+    batch.pages[0, :(500 - 40) // 16] = -1
+    got = _run(q, cache, batch, window=40).double().cpu()
+    assert bool((got - want).abs().le(bound).all())
+
+
+def test_nan_scales_of_hidden_keys():
+    batch = Batch([(20, 4)], 16)
+    cache, q = pu.random_cache(batch, 1, 64, True), _q(batch, 4, 64)
+    want, bound = pu.attention(q, cache, batch)
+    page, slot = batch.slots(0, torch.tensor([23]))
+    cache[2][page, 0, slot] = math.nan
+    cache[3][page, 0, slot] = math.nan
+    got = _run(q, cache, batch).double().cpu()
+    assert bool((got[:3] - want[:3]).abs().le(bound[:3]).all()) and bool(got[3].isnan().all())
+
+
+def test_pages_out_of_range_stay_inside_the_cache():
+    """Every access is held to the cache: rows of sequences whose pages are in range are as ever, the others' content is unspecified."""
+    batch = Batch([(60, 2), (60, 2)], 16)
+    cache, q = pu.random_cache(batch, 2, 64, False), _q(batch, 4, 64)
+    want, bound = pu.attention(q, cache, batch)
+    batch.pages[1, 1] = batch.count
+    batch.pages[1, 2] = 2 ** 31 - 1
+    batch.pages[1, 0] = -7
+    got = _run(q, cache, batch).double().cpu()
+    assert bool((got[:2] - want[:2]).abs().le(bound[:2]).all())
+
+
+def test_lengths_beyond_the_page_table_are_held_to_it():
+    batch = Batch([(60, 2)], 16, extra_columns=0)
+    cache, q = pu.random_cache(batch, 2, 64, False), _q(batch, 4, 64)
+    batch.lengths[0] = 1 << 40
+    assert bool(_run(q, cache, batch).isfinite().all())
+    batch.lengths[0] = -5
+    assert bool((_run(q, cache, batch) == 0).all())
+
+
+def test_queries_out_of_wider_rows():
+    batch = Batch([(60, 5), (9, 1)], 16)
+    cache = pu.random_cache(batch, 2, 64, False)
+    rows = torch.randn(batch.rows, 9, 64, generator=torch.Generator().manual_seed(5)).to(BF)
+    from paper_2006_03031_amd import runtime as rt
+    q = rows[:, 1:7]
+    got = rt.paged_attention(rows.cuda()[:, 1:7], pu.to_gpu(cache), batch.on_gpu())
+    _check(got, q, cache, batch)
+
+
+def test_same_bits_every_time_and_on_another_stream():
+    from paper_2006_03031_amd import runtime as rt
+    batch = Batch([(3000, 1), (0, 70), (900, 2)], 32)
+    cache, q = pu.to_gpu(pu.random_cache(batch, 2, 128, False)), _q(batch, 8, 128).cuda()
+    seqs = batch.on_gpu()
+    first = rt.paged_attention(q, cache, seqs)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        again = [rt.paged_attention(q, cache, seqs) for _ in range(3)]
+    side.synchronize()
+    assert all(torch.equal(first, x) for x in again)
+
+
+def test_a_captured_call_follows_the_lengths():
+    from paper_2006_03031_amd import runtime as rt
+    batch = Batch([(4000, 1), (200, 1)], 32, extra_columns=0)
+    cpu = pu.random_cache(batch, 2, 64, False)
+    q = _q(batch, 4, 64)
+    cache, seqs, qg = pu.to_gpu(cpu), batch.on_gpu(), q.cuda()
+    rt.paged_attention(qg, cache, seqs)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        o = rt.paged_attention(qg, cache, seqs)
+    for lengths in ((4001, 201), (1, 201), (300, 7), (0, 150), (4001, 1)):
+        batch.lengths = torch.tensor(lengths)
+        seqs.lengths.copy_(batch.lengths)
+        o.fill_(3.0)
+        eager = rt.paged_attention(qg, cache, seqs)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(eager, o), lengths
+        _check(o, q, cpu, batch)
+
+
+def test_a_cache_past_4_gib():
+    """Rows whose byte offsets pass 32 bits, in codes and in scales' neighbours."""
+    from paper_2006_03031_amd import runtime as rt
+    pages, G, page, D = 5 * 2 ** 30 // (8 * 64 * 128 * 2) + 3, 8, 64, 128
+    k, v = (torch.empty(pages, G, page, D, dtype=BF, device="cuda") for _ in range(2))
+    batch = Batch([(150, 2), (3, 1)], page, extra_columns=0)
+    small = pu.random_cache(batch, G, D, False)
+    high = pages - batch.count
+    k[high:], v[high:] = small[0].cuda(), small[1].cuda()
+    q = _q(batch, 8, D)
+    seqs = batch.on_gpu()
+    seqs.pages[seqs.pages >= 0] += high
+    _check(rt.paged_attention(q.cuda(), rt.PagedCache(k, v), seqs), q, small, batch)
+
+
+def test_nothing_to_do():
+    from paper_2006_03031_amd import runtime as rt
+    batch = Batch([(0, 0), (0, 0)], 16)
+    cache = pu.to_gpu(pu.random_cache(batch, 2, 64, False))
+    assert rt.paged_attention(torch.empty(0, 4, 64, dtype=BF, device="cuda"), cache, batch.on_gpu()).shape == (0, 4, 64)
+    none = rt.Sequences(torch.zeros(1, dtype=torch.int64, device="cuda"), torch.zeros(0, dtype=torch.int64, device="cuda"),
+                        torch.zeros(0, 0, dtype=torch.int32, device="cuda"))
+    out = torch.full((2, 4, 64), 5.0, dtype=BF, device="cuda")
+    assert bool((rt.paged_attention(torch.zeros(2, 4, 64, dtype=BF, device="cuda"), cache, none, out=out) == 5).all())
