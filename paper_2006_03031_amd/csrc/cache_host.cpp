@@ -63,7 +63,7 @@ SequencesArgs sequences_args(const nimble_sequences& s) {
 struct PagedMember {
   int rows, block_keys, target_units, least_blocks;
 };
-static const PagedMember kPagedMembers[NIMBLE_PAGED_COUNT] = {{16, 32, 512, 8}, {128, 64, 256, 4}};
+static const PagedMember kPagedMembers[NIMBLE_PAGED_COUNT] = {{16, 32, 512, 8}, {128, 64, 512, 4}};
 
 static int plan_paged(int64_t rows, int64_t count, int64_t width, int64_t heads, int64_t kv_heads, int64_t page, int64_t D, int dtype,
                       int64_t window, nimble_paged_plan* p) {
@@ -73,9 +73,9 @@ static int plan_paged(int64_t rows, int64_t count, int64_t width, int64_t heads,
   if (heads < 1 || heads > 65536 || heads % kv_heads) return fail(heads < 1 || heads > 65536 ? NIMBLE_ERR_ARG : NIMBLE_ERR_SHAPE, "%lld query heads over %lld of the cache", (long long)heads, (long long)kv_heads);
   if (window < 0) return fail(NIMBLE_ERR_ARG, "negative window");
   nimble_paged_plan out{};
-  out.kernel = NIMBLE_PAGED_TOKENS;
-  const PagedMember& m = kPagedMembers[out.kernel];
   const int64_t group = heads / kv_heads, live = count < rows ? count : rows;
+  out.kernel = rows * group > 32 * live ? NIMBLE_PAGED_CHUNKS : NIMBLE_PAGED_TOKENS;
+  const PagedMember& m = kPagedMembers[out.kernel];
   const int64_t tiles = rows * group / m.rows + live;   // a sequence adds at most one that is not full
   // the keys that a tile can see
   int64_t keys = width * page;

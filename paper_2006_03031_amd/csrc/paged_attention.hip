@@ -1,9 +1,10 @@
-// Device entry point of attention over a paged cache (kernels: paged_attention_kernel.h).
+// Device entry point of attention over a paged cache (kernels: paged_tokens_kernel.h, paged_chunks_kernel.h; the parts of long sequences: paged_common.h).
 #include <hip/hip_runtime.h>
 
 #include <cmath>
 
-#include "paged_attention_kernel.h"
+#include "paged_chunks_kernel.h"
+#include "paged_tokens_kernel.h"
 
 namespace nimble {
 
@@ -11,11 +12,19 @@ int check_rows(const void* p, int64_t stride, int64_t heads, int64_t D, const ch
 
 template <int D>
 static void launch_paged(const PagedArgs& g, const nimble_paged_plan& p, bool int8, hipStream_t stream) {
-  if (int8)
-    hipLaunchKernelGGL((paged_tokens_kernel<D, true>), dim3(p.grid), dim3(p.block), 0, stream, g);
-  else
-    hipLaunchKernelGGL((paged_tokens_kernel<D, false>), dim3(p.grid), dim3(p.block), 0, stream, g);
-  if (p.parts) hipLaunchKernelGGL((paged_join_kernel<16, D>), dim3(p.join_grid[0], p.join_grid[1]), dim3(256), 0, stream, g);
+  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(p.grid), dim3(p.block), 0, stream, g); };
+  const bool chunks = p.kernel == NIMBLE_PAGED_CHUNKS;
+  if (chunks) {
+    if (int8) launch(paged_chunks_kernel<D, true>);
+    else launch(paged_chunks_kernel<D, false>);
+  } else {
+    if (int8) launch(paged_tokens_kernel<D, true>);
+    else launch(paged_tokens_kernel<D, false>);
+  }
+  if (!p.parts) return;
+  auto join = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(p.join_grid[0], p.join_grid[1]), dim3(256), 0, stream, g); };
+  if (chunks) join(paged_join_kernel<128, D>);
+  else join(paged_join_kernel<16, D>);
 }
 
 }  // namespace nimble
@@ -55,7 +64,7 @@ int nimble_paged_attention_dyn(const void* q, int64_t q_stride, const nimble_cac
   if (!std::isfinite(g.a2)) return fail(NIMBLE_ERR_ARG, "paged_attention: alpha = %g is too large", (double)alpha);
   if (p.parts) {
     g.slots = (int)p.slots;
-    g.target_units = (int)(p.slots - 8) / 2;
+    g.target_units = (int)(p.slots - 8) / 2;  // (see plan_paged)
     g.part = (float*)workspace;
     g.stat = (float2*)(g.part + p.slots * p.rows * cache->D);
     g.items = (int*)(g.stat + p.slots * p.rows);

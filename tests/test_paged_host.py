@@ -240,7 +240,7 @@ def test_grid_and_workspace_hold_every_batch():
         if not 0 < rows * group * kv_heads < 1 << 26:
             continue
         p = nb.paged_attention_plan(rows, S, width, group * kv_heads, kv_heads, page, D, rng.choice((nb.BF16, nb.I8)), window)
-        member = {0: (32, 512, 8), 1: (64, 256, 4)}[p.kernel]
+        member = {0: (32, 512, 8), 1: (64, 512, 4)}[p.kernel]
         units, slots, cut = _units(p, sizes, group, kv_heads, window, width * page, *member)
         assert units <= p.grid, (sizes, p)
         if p.parts:
