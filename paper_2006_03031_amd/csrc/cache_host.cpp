@@ -59,11 +59,16 @@ SequencesArgs sequences_args(const nimble_sequences& s) {
 }
 
 // ------------------------------------------------------------------------------------------------ attention
-// Workgroups that a compute unit holds at once, and the least number of key blocks that is worth a part of its own.
+// Rows of a tile, keys of a block, the least number of blocks that is worth a part of its own.
 struct PagedMember {
-  int rows, block_keys, target_units, least_blocks;
+  int rows, block_keys, least_blocks;
 };
-static const PagedMember kPagedMembers[NIMBLE_PAGED_COUNT] = {{16, 32, 512, 8}, {128, 64, 512, 4}};
+static const PagedMember kPagedMembers[NIMBLE_PAGED_COUNT] = {{16, 32, 8}, {128, 64, 4}};
+// Workgroups that a compute unit holds at once, by their LDS (tokens) and registers: as many parts as fill the chip once are aimed at.
+static int paged_workgroups_per_cu(int kernel, int64_t D, int dtype) {
+  if (kernel == NIMBLE_PAGED_CHUNKS) return 2;
+  return (D == 128 ? 1 : 2) * (dtype == NIMBLE_I8 ? 2 : 1);
+}
 
 static int plan_paged(int64_t rows, int64_t count, int64_t width, int64_t heads, int64_t kv_heads, int64_t page, int64_t D, int dtype,
                       int64_t window, nimble_paged_plan* p) {
@@ -82,14 +87,17 @@ static int plan_paged(int64_t rows, int64_t count, int64_t width, int64_t heads,
   if (window > 0 && window + m.rows < keys) keys = window + m.rows;
   out.rows = m.rows;
   out.block = 256;
-  out.parts = keys > (int64_t)m.block_keys * m.least_blocks;
+  // Nothing is cut where tiles alone fill the chip twice and none can take long: the second launch is saved.
+  const int64_t target = (int64_t)kComputeUnits * paged_workgroups_per_cu(out.kernel, D, dtype);
+  const bool plenty = rows * group / m.rows * kv_heads >= 2 * target && keys <= 1024;
+  out.parts = keys > (int64_t)m.block_keys * m.least_blocks && !plenty;
   if (tiles * kv_heads > kMostPagedGrid) return fail(NIMBLE_ERR_ARG, "more than 2^23 tiles");
-  out.grid = (uint32_t)(tiles * kv_heads + (out.parts ? m.target_units : 0));
+  out.grid = (uint32_t)(tiles * kv_heads + (out.parts ? target : 0));
   if (out.parts) {
-    out.slots = 2 * m.target_units + 8;
-    const int64_t items = tiles * kv_heads < out.slots / 2 ? tiles * kv_heads : out.slots / 2;
-    out.join_grid[0] = (uint32_t)items;
-    out.join_grid[1] = (uint32_t)(rows * group < m.rows ? rows * group : m.rows);
+    out.slots = 2 * target + 8;
+    out.join_rows = (int32_t)(rows * group < m.rows ? rows * group : m.rows);
+    const int64_t items = tiles * kv_heads < out.slots / 2 ? tiles * kv_heads : out.slots / 2, most = items * out.join_rows;
+    out.join_grid = (uint32_t)(most < 1024 ? most : 1024);  // (its workgroups go round)
     out.workspace_bytes = (uint64_t)out.slots * m.rows * (D * 4 + 8) + (uint64_t)(1 + out.slots / 2) * kPagedItemWords * 4;
   }
   *p = out;

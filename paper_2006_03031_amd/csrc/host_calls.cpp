@@ -29,6 +29,11 @@ decltype(&nimble_quantize_rows_dyn) g_quantize_rows;
 decltype(&nimble_dense_i8_dyn) g_dense_i8;
 decltype(&nimble_grouped_dense_dyn) g_grouped_dense;
 decltype(&nimble_grouped_dense_i8_dyn) g_grouped_dense_i8;
+decltype(&nimble_rotary_dyn) g_rotary;
+decltype(&nimble_cache_write_dyn) g_cache_write;
+decltype(&nimble_cache_read_dyn) g_cache_read;
+decltype(&nimble_paged_attention_plan_of) g_paged_plan;
+decltype(&nimble_paged_attention_dyn) g_paged_attention;
 decltype(&nimble_vm_run) g_vm_run;
 decltype(&nimble_lstm_seq_preferred) g_seq_preferred;
 decltype(&nimble_lstm_seq_workspace_bytes) g_seq_workspace_bytes;
@@ -54,12 +59,17 @@ bool modes_active() {
          c10::impl::tls_is_dispatch_key_included(c10::DispatchKey::Tracer);
 }
 
-const at::Tensor* plain(PyObject* o, at::ScalarType dtype) {
+// An ordinary GPU tensor of any strides.
+const at::Tensor* strided(PyObject* o, at::ScalarType dtype) {
   if (!THPVariable_CheckExact(o)) return nullptr;
   const at::Tensor& t = THPVariable_Unpack(o);
-  if (!t.defined() || t.scalar_type() != dtype || !t.is_cuda() || !t.is_contiguous()) return nullptr;
+  if (!t.defined() || t.scalar_type() != dtype || !t.is_cuda()) return nullptr;
   if (!g_raw_stream || (t.key_set() != g_plain && t.key_set() != g_inference)) return nullptr;
   return &t;
+}
+const at::Tensor* plain(PyObject* o, at::ScalarType dtype) {
+  const at::Tensor* t = strided(o, dtype);
+  return t && t->is_contiguous() ? t : nullptr;
 }
 
 // The current device's current stream; false with a Python error set.
@@ -277,6 +287,192 @@ PyObject* product(PyObject*, PyObject* const* args, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// Heads [T, H, D] one after the other within a row, the rows any stride apart.
+const at::Tensor* rows_of(PyObject* o, int64_t* stride) {
+  const at::Tensor* t = strided(o, at::kBFloat16);
+  if (!t || t->dim() != 3 || t->numel() == 0 || (t->size(2) > 1 && t->stride(2) != 1) || (t->size(1) > 1 && t->stride(1) != t->size(2))) return nullptr;
+  *stride = t->size(0) > 1 ? t->stride(0) : t->size(1) * t->size(2);
+  return t;
+}
+
+// rotary(x, positions, table, interleaved, out or None) -> y or None.  One token of 16 heads: 13.1 us a call through the steps, ROTARY_US here.
+PyObject* rotary(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 5 || !g_rotary || modes_active() || !PyBool_Check(args[3])) Py_RETURN_NONE;
+  int64_t xs = 0, ys = 0;
+  const at::Tensor *x = rows_of(args[0], &xs), *positions = plain(args[1], at::kLong), *table = plain(args[2], at::kFloat), *given = nullptr;
+  if (!x || !positions || !table || positions->dim() != 1 || table->dim() != 3 || table->size(2) != 2) Py_RETURN_NONE;
+  const int64_t T = x->size(0), H = x->size(1), D = x->size(2);
+  if (positions->size(0) != T || 2 * table->size(1) > D) Py_RETURN_NONE;
+  if (args[4] != Py_None && (!(given = rows_of(args[4], &ys)) || given->sizes() != x->sizes())) Py_RETURN_NONE;
+  for (const at::Tensor* t : {positions, table, given})
+    if (t && t->get_device() != x->get_device()) Py_RETURN_NONE;
+  void* stream;
+  const int here = current_stream_of(x->get_device(), &stream);
+  if (here < 0) return nullptr;
+  if (!here) Py_RETURN_NONE;
+  at::Tensor y = given ? *given : empty_like(*x, {T, H, D}, at::kBFloat16);
+  if (!given) ys = H * D;
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = g_rotary(x->data_ptr(), xs, positions->data_ptr(), table->data_ptr(), table->size(0), y.data_ptr(), ys, T, H, D, table->size(1),
+                args[3] == Py_True, stream);
+  Py_END_ALLOW_THREADS
+  if (rc != NIMBLE_OK) Py_RETURN_NONE;
+  if (given) {
+    Py_INCREF(args[4]);
+    return args[4];
+  }
+  return THPVariable_Wrap(std::move(y));
+  END_HANDLE_TH_ERRORS
+}
+
+// A cache (k, v, k_scale, v_scale) and a batch (offsets, lengths, pages) as the C ABI takes them; all on one device.
+struct Paged {
+  const at::Tensor* k;
+  nimble_cache cache;
+  nimble_sequences seqs;
+};
+bool paged_of(PyObject* cache, PyObject* batch, int64_t rows, Paged* p) {
+  if (!PyTuple_Check(cache) || PyTuple_GET_SIZE(cache) != 4 || !PyTuple_Check(batch) || PyTuple_GET_SIZE(batch) != 3) return false;
+  const at::Tensor *k = plain(PyTuple_GET_ITEM(cache, 0), at::kBFloat16), *ks = nullptr, *vs = nullptr;
+  const bool int8 = !k;
+  if (int8) k = plain(PyTuple_GET_ITEM(cache, 0), at::kChar);
+  if (!k || k->dim() != 4) return false;
+  const at::Tensor* v = plain(PyTuple_GET_ITEM(cache, 1), k->scalar_type());
+  if (!v || v->sizes() != k->sizes()) return false;
+  if (int8) {
+    ks = plain(PyTuple_GET_ITEM(cache, 2), at::kFloat);
+    vs = plain(PyTuple_GET_ITEM(cache, 3), at::kFloat);
+    if (!ks || !vs || ks->sizes() != k->sizes().slice(0, 3) || vs->sizes() != k->sizes().slice(0, 3)) return false;
+  }
+  const at::Tensor *offsets = plain(PyTuple_GET_ITEM(batch, 0), at::kLong), *lengths = plain(PyTuple_GET_ITEM(batch, 1), at::kLong);
+  const at::Tensor* pages = plain(PyTuple_GET_ITEM(batch, 2), at::kInt);
+  if (!offsets || !lengths || !pages || offsets->dim() != 1 || lengths->dim() != 1 || pages->dim() != 2) return false;
+  const int64_t S = lengths->size(0);
+  if (offsets->size(0) != S + 1 || pages->size(0) != S) return false;
+  for (const at::Tensor* t : {v, ks, vs, offsets, lengths, pages})
+    if (t && t->get_device() != k->get_device()) return false;
+  p->k = k;
+  p->cache = nimble_cache{k->data_ptr(), v->data_ptr(), ks ? ks->data_ptr() : nullptr, vs ? vs->data_ptr() : nullptr, k->size(0), k->size(1),
+                          k->size(2), k->size(3), int8 ? NIMBLE_I8 : NIMBLE_BF16};
+  p->seqs = nimble_sequences{offsets->data_ptr(), lengths->data_ptr(), pages->data_ptr(), S, pages->size(1), rows};
+  return true;
+}
+
+// cache_write(cache, k, v, sequences, q or None, table or None, interleaved, out or None) -> q turned, True without q, or None.
+// A token of each of 64 sequences (torch products behind it not counted): WRITE_STEPS us a call through the steps, WRITE_US here.
+PyObject* cache_write(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 8 || !g_cache_write || modes_active() || !PyBool_Check(args[6])) Py_RETURN_NONE;
+  int64_t ks = 0, vs = 0, qs = 0;
+  const at::Tensor *k = rows_of(args[1], &ks), *v = rows_of(args[2], &vs), *q = nullptr, *table = nullptr, *given = nullptr;
+  Paged p;
+  if (!k || !v || k->sizes() != v->sizes() || !paged_of(args[0], args[3], k->size(0), &p)) Py_RETURN_NONE;
+  if (k->size(1) != p.cache.kv_heads || k->size(2) != p.cache.D) Py_RETURN_NONE;
+  if (args[4] != Py_None && (!(q = rows_of(args[4], &qs)) || q->size(0) != k->size(0) || q->size(2) != k->size(2))) Py_RETURN_NONE;
+  if (args[5] != Py_None && (!(table = plain(args[5], at::kFloat)) || table->dim() != 3 || table->size(2) != 2)) Py_RETURN_NONE;
+  if (args[7] != Py_None && (!q || !(given = plain(args[7], at::kBFloat16)) || given->sizes() != q->sizes())) Py_RETURN_NONE;
+  for (const at::Tensor* t : {k, v, q, table, given})
+    if (t && t->get_device() != p.k->get_device()) Py_RETURN_NONE;
+  void* stream;
+  const int here = current_stream_of(p.k->get_device(), &stream);
+  if (here < 0) return nullptr;
+  if (!here) Py_RETURN_NONE;
+  at::Tensor y;
+  if (given) y = *given;
+  else if (q) y = empty_like(*q, q->sizes(), at::kBFloat16);
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = g_cache_write(&p.cache, &p.seqs, k->data_ptr(), ks, v->data_ptr(), vs, q ? q->data_ptr() : nullptr, qs, q ? y.data_ptr() : nullptr,
+                     q ? q->size(1) : 0, table ? table->data_ptr() : nullptr, table ? table->size(0) : 0, table ? table->size(1) : 0,
+                     args[6] == Py_True, stream);
+  Py_END_ALLOW_THREADS
+  if (rc != NIMBLE_OK) Py_RETURN_NONE;
+  if (!q) Py_RETURN_TRUE;
+  if (given) {
+    Py_INCREF(args[7]);
+    return args[7];
+  }
+  return THPVariable_Wrap(std::move(y));
+  END_HANDLE_TH_ERRORS
+}
+
+// cache_read(cache, sequences, rows, out_dtype) -> (k, v) or None.
+PyObject* cache_read(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 4 || !g_cache_read || modes_active() || !PyLong_CheckExact(args[2]) || !PyLong_CheckExact(args[3])) Py_RETURN_NONE;
+  const long long rows = PyLong_AsLongLong(args[2]);
+  const long out_dtype = PyLong_AsLong(args[3]);
+  if (rows < 0 || (out_dtype != NIMBLE_BF16 && out_dtype != NIMBLE_F32)) {
+    PyErr_Clear();
+    Py_RETURN_NONE;
+  }
+  Paged p;
+  if (rows > (1ll << 24) || !paged_of(args[0], args[1], rows, &p)) Py_RETURN_NONE;
+  void* stream;
+  const int here = current_stream_of(p.k->get_device(), &stream);
+  if (here < 0) return nullptr;
+  if (!here) Py_RETURN_NONE;
+  const at::ScalarType type = out_dtype == NIMBLE_F32 ? at::kFloat : at::kBFloat16;
+  at::Tensor out[2];
+  for (at::Tensor& t : out) t = empty_like(*p.k, {rows, p.cache.kv_heads, p.cache.D}, type);
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = g_cache_read(&p.cache, &p.seqs, out[0].data_ptr(), out[1].data_ptr(), (int)out_dtype, stream);
+  Py_END_ALLOW_THREADS
+  if (rc != NIMBLE_OK) Py_RETURN_NONE;
+  PyObject* pair = PyTuple_New(2);
+  if (!pair) return nullptr;
+  for (int i = 0; i < 2; ++i) {
+    PyObject* t = THPVariable_Wrap(std::move(out[i]));
+    if (!t) {
+      Py_DECREF(pair);
+      return nullptr;
+    }
+    PyTuple_SET_ITEM(pair, i, t);
+  }
+  return pair;
+  END_HANDLE_TH_ERRORS
+}
+
+// paged_attention(q, cache, sequences, alpha, window, out or None) -> o or None, with a workspace of its own.  One token of one sequence of 777:
+// ATTN_STEPS us a call through the steps, ATTN_US here.
+PyObject* paged_attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 6 || !g_paged_attention || modes_active() || !PyFloat_CheckExact(args[3]) || !PyLong_CheckExact(args[4])) Py_RETURN_NONE;
+  int64_t qs = 0;
+  const at::Tensor *q = rows_of(args[0], &qs), *given = nullptr;
+  Paged p;
+  if (!q || !paged_of(args[1], args[2], q->size(0), &p) || q->size(2) != p.cache.D || q->get_device() != p.k->get_device()) Py_RETURN_NONE;
+  if (args[5] != Py_None && (!(given = plain(args[5], at::kBFloat16)) || given->sizes() != q->sizes() || given->get_device() != q->get_device())) Py_RETURN_NONE;
+  const long long window = PyLong_AsLongLong(args[4]);
+  nimble_paged_plan plan;
+  if (window < 0 || g_paged_plan(q->size(0), p.seqs.count, p.seqs.width, q->size(1), p.cache.kv_heads, p.cache.page, p.cache.D, p.cache.dtype,
+                                 window, &plan) != NIMBLE_OK) {
+    PyErr_Clear();
+    Py_RETURN_NONE;
+  }
+  void* stream;
+  const int here = current_stream_of(p.k->get_device(), &stream);
+  if (here < 0) return nullptr;
+  if (!here) Py_RETURN_NONE;
+  at::Tensor y = given ? *given : empty_like(*q, q->sizes(), at::kBFloat16), ws;
+  if (plan.workspace_bytes) ws = empty_like(*q, {(int64_t)plan.workspace_bytes}, at::kByte);
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = g_paged_attention(q->data_ptr(), qs, &p.cache, &p.seqs, y.data_ptr(), q->size(1), (float)PyFloat_AS_DOUBLE(args[3]), window,
+                         plan.workspace_bytes ? ws.data_ptr() : nullptr, plan.workspace_bytes, stream);
+  Py_END_ALLOW_THREADS
+  if (rc != NIMBLE_OK) Py_RETURN_NONE;
+  if (given) {
+    Py_INCREF(args[5]);
+    return args[5];
+  }
+  return THPVariable_Wrap(std::move(y));
+  END_HANDLE_TH_ERRORS
+}
+
 // lstm_sequence(xs, w_x, w_h, bias, h0, c0, max_polls) -> (h_seq, c_T, True) from the one-launch token loop; pre, the
 // inputs' share of the gates, where the loop gave up; or None.  The loop's launch waits for whatever the host does between it
 // and the projection's, and the pass ends with a wait: with these steps in Python / here (means over where the buffers
@@ -488,7 +684,26 @@ PyObject* bind_products(PyObject*, PyObject* args) {
   END_HANDLE_TH_ERRORS
 }
 
+// bind_paged(rotary, cache_write, cache_read, paged_attention_plan_of, paged_attention): the same for these, behind bind().
+PyObject* bind_paged(PyObject*, PyObject* args) {
+  HANDLE_TH_ERRORS
+  unsigned long long a[5];
+  if (!PyArg_ParseTuple(args, "KKKKK", &a[0], &a[1], &a[2], &a[3], &a[4])) return nullptr;
+  g_rotary = (decltype(g_rotary))a[0];
+  g_cache_write = (decltype(g_cache_write))a[1];
+  g_cache_read = (decltype(g_cache_read))a[2];
+  g_paged_plan = (decltype(g_paged_plan))a[3];
+  g_paged_attention = (decltype(g_paged_attention))a[4];
+  Py_RETURN_NONE;
+  END_HANDLE_TH_ERRORS
+}
+
 PyMethodDef kMethods[] = {
+    {"rotary", (PyCFunction)(void (*)(void))rotary, METH_FASTCALL, nullptr},
+    {"cache_write", (PyCFunction)(void (*)(void))cache_write, METH_FASTCALL, nullptr},
+    {"cache_read", (PyCFunction)(void (*)(void))cache_read, METH_FASTCALL, nullptr},
+    {"paged_attention", (PyCFunction)(void (*)(void))paged_attention, METH_FASTCALL, nullptr},
+    {"bind_paged", bind_paged, METH_VARARGS, nullptr},
     {"quantize_rows", (PyCFunction)(void (*)(void))quantize_rows, METH_FASTCALL, nullptr},
     {"product", (PyCFunction)(void (*)(void))product, METH_FASTCALL, nullptr},
     {"bind_products", bind_products, METH_VARARGS, nullptr},

@@ -22,7 +22,7 @@ static void launch_paged(const PagedArgs& g, const nimble_paged_plan& p, bool in
     else launch(paged_tokens_kernel<D, false>);
   }
   if (!p.parts) return;
-  auto join = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(p.join_grid[0], p.join_grid[1]), dim3(256), 0, stream, g); };
+  auto join = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(p.join_grid), dim3(256), 0, stream, g); };
   if (chunks) join(paged_join_kernel<128, D>);
   else join(paged_join_kernel<16, D>);
 }
@@ -65,6 +65,7 @@ int nimble_paged_attention_dyn(const void* q, int64_t q_stride, const nimble_cac
   if (p.parts) {
     g.slots = (int)p.slots;
     g.target_units = (int)(p.slots - 8) / 2;  // (see plan_paged)
+    g.join_rows = p.join_rows;
     g.part = (float*)workspace;
     g.stat = (float2*)(g.part + p.slots * p.rows * cache->D);
     g.items = (int*)(g.stat + p.slots * p.rows);

@@ -19,7 +19,7 @@ struct PagedArgs {
   float* part;         // [slots][rows][D] sums of parts, not divided
   float2* stat;        // [slots][rows] their largest score (base 2) and sum of probabilities
   int* items;          // [0]: tiles that were cut, then 8 words each
-  int slots, target_units;
+  int slots, target_units, join_rows;  // join_rows: the most rows of a tile
 };
 
 constexpr float kNothing = -3.0e38f;  // the reference of a row that has seen no key yet
@@ -235,51 +235,81 @@ __device__ __forceinline__ uint2 codes_to_bf16(uint32_t w) {
   return make_uint2(pack_bf16x2(a, b), pack_bf16x2(c, d));
 }
 
-// The parts of a tile joined: a workgroup a row, its waves sharing the parts.
+// ---------------------------------------------------------------------------
+// The parts of a row joined, in the order of the parts: o = sum_x 2^(ref_x - top) part_x / sum_x 2^(ref_x - top) sum_x.  A wave a row; where there
+// are fewer rows than workgroups a workgroup a row, whose waves take every fourth part.  A lane looks at one part's (ref, sum) and the wave at its
+// sums one part after the other, 8 loads at a time.
+// ---------------------------------------------------------------------------
 template <int ROWS, int D>
 __global__ void __launch_bounds__(256) paged_join_kernel(PagedArgs g) {
+  constexpr int P = D / 64;
+  typedef float Piece __attribute__((ext_vector_type(P)));
   __shared__ float2 wave_stat[4];
-  __shared__ float wave_sums[4][D];
-  const int item_i = blockIdx.x, row = blockIdx.y;
+  __shared__ Piece wave_sums[4][64];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int* item = g.items + (1 + item_i) * kPagedItemWords;
-  if (item_i >= g.items[0]) return;
-  const int slot = item[0], parts = item[1], step = item[7], tile = item[2], mm = tile * ROWS + row;
-  if (mm >= item[5] * g.group) return;
-  constexpr int P = D / 64;
-  float top = kNothing, total = 0.f, acc[P];
+  const long long count = (long long)g.items[0] * g.join_rows;
+  const bool together = count <= gridDim.x;
+  const int step = together ? 4 : 1;
+  for (long long at = together ? blockIdx.x : (long long)blockIdx.x * 4 + wave; at < count; at += together ? gridDim.x : 4ll * gridDim.x) {
+    const int* item = g.items + (1 + at / g.join_rows) * kPagedItemWords;
+    const int row = (int)(at % g.join_rows);
+    const int slot = item[0], parts = item[1], apart = item[7], mm = item[2] * ROWS + row;
+    if (mm >= item[5] * g.group) continue;  // (the same in the whole workgroup where its waves work together)
+    float top = kNothing, total = 0.f;
+    Piece acc{};
+    for (int x0 = together ? wave : 0; x0 < parts; x0 += 64 * step) {
+      const int x = x0 + lane * step;
+      const float2 st = x < parts ? g.stat[(long long)(slot + x * apart) * ROWS + row] : make_float2(kNothing, 0.f);
+      float next = fmaxf(top, st.x);
 #pragma unroll
-  for (int i = 0; i < P; ++i) acc[i] = 0.f;
-  for (int x = wave; x < parts; x += 4) {
-    const long long at = (long long)(slot + x * step) * ROWS + row;
-    const float2 st = g.stat[at];
-    float v[P];
+      for (int o = 32; o > 0; o >>= 1) next = fmaxf(next, __shfl_xor(next, o, 64));
+      const float back = __builtin_amdgcn_exp2f(top - next), scale = __builtin_amdgcn_exp2f(st.x - next);
+      float sum = st.y * scale;
 #pragma unroll
-    for (int i = 0; i < P; ++i) v[i] = g.part[at * D + i * 64 + lane];
-    const float next = fmaxf(top, st.x), back = __builtin_amdgcn_exp2f(top - next), scale = __builtin_amdgcn_exp2f(st.x - next);
-    total = total * back + st.y * scale;
+      for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+      total = total * back + sum;
+      acc *= back;
+      top = next;
+      const int n = (parts - x0 + step - 1) / step < 64 ? (parts - x0 + step - 1) / step : 64;
+      for (int y0 = 0; y0 < n; y0 += 8) {
+        Piece v[8];
 #pragma unroll
-    for (int i = 0; i < P; ++i) acc[i] = acc[i] * back + v[i] * scale;
-    top = next;
+        for (int y = 0; y < 8; ++y) {
+          const int part = x0 + (y0 + y < n ? y0 + y : n - 1) * step;
+          v[y] = *(const Piece*)(g.part + ((long long)(slot + part * apart) * ROWS + row) * D + lane * P);
+        }
+#pragma unroll
+        for (int y = 0; y < 8; ++y)
+          if (y0 + y < n) acc += v[y] * __shfl(scale, y0 + y, 64);
+      }
+    }
+    if (together) {
+      __syncthreads();
+      if (lane == 0) wave_stat[wave] = make_float2(top, total);
+      wave_sums[wave][lane] = acc;
+      __syncthreads();
+      if (wave > 0) continue;
+      float t = kNothing;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) t = fmaxf(t, wave_stat[w].x);
+      total = 0.f;
+      acc = Piece{};
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float scale = __builtin_amdgcn_exp2f(wave_stat[w].x - t);
+        total += wave_stat[w].y * scale;
+        acc += wave_sums[w][lane] * scale;
+      }
+    }
+    const int tok = mm / g.group;
+    const float inv = item[6] - item[5] + tok < 0 ? 0.f : 1.0f / total;
+    u16* o = g.o + ((long long)(item[4] + tok) * g.heads + item[3] * g.group + mm - tok * g.group) * D + lane * P;
+    if constexpr (P == 2)
+      *(uint32_t*)o = pack_bf16x2(acc[0] * inv, acc[1] * inv);
+    else
+      *o = f2bf(acc[0] * inv);
   }
-  if (lane == 0) wave_stat[wave] = make_float2(top, total);
-#pragma unroll
-  for (int i = 0; i < P; ++i) wave_sums[wave][i * 64 + lane] = acc[i];
-  __syncthreads();
-  if (threadIdx.x >= D) return;
-  float t = kNothing, all = 0.f, y = 0.f;
-#pragma unroll
-  for (int w = 0; w < 4; ++w) t = fmaxf(t, wave_stat[w].x);
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    const float scale = __builtin_amdgcn_exp2f(wave_stat[w].x - t);
-    all += wave_stat[w].y * scale;
-    y += wave_sums[w][threadIdx.x] * scale;
-  }
-  const int tok = mm / g.group;
-  const float inv = item[6] - item[5] + tok < 0 ? 0.f : 1.0f / all;
-  g.o[((long long)(item[4] + tok) * g.heads + item[3] * g.group + mm - tok * g.group) * D + threadIdx.x] = f2bf(y * inv);
 }
 
 }  // namespace nimble

@@ -14,7 +14,7 @@ namespace nimble {
 //   8 bits:  codes become bf16, which holds them exactly, behind the LDS reads; a key's scale multiplies its scores, a value's its
 //            probability.  A lane reads 16 codes of a key row where it reads 8 elements of bf16, so that the elements of a
 //            matrix instruction's k are taken from the row in another order, and those of q in the same.
-//   Loads:   direct global->LDS loads into the wave's own ring of S blocks, waited for by count: no barrier in the loop.  16 keys lie in one
+//   Loads:   direct global->LDS loads into the wave's own ring of two blocks, waited for by count: no barrier in the loop.  16 keys lie in one
 //            page, whose number is a scalar.  Chunk c of row r sits at c ^ swizzle(r).  Keys outside of what the tile sees repeat the
 //            nearest one that it does.
 // ---------------------------------------------------------------------------
@@ -29,7 +29,7 @@ __global__ void __launch_bounds__(256) paged_tokens_kernel(PagedArgs g) {
   constexpr int SCALES = I8 ? 256 : 0;           // 32 scales of keys, 32 of values
   constexpr int SLOT = 2 * TILE + SCALES;
   constexpr int S = 2;
-  constexpr int COUNT = 4 * LOADS + (I8 ? 1 : 0);  // loads of a block
+  constexpr int KL = 2 * LOADS + (I8 ? 1 : 0), VL = 2 * LOADS;  // loads of a block's keys (with the scales of both), of its values
   constexpr int RING = WAVES * S * SLOT, JOIN = WAVES * ROWS * D * 4;
   __shared__ __attribute__((aligned(256))) unsigned char lds[RING > JOIN ? RING : JOIN];
   __shared__ float2 stat[WAVES][ROWS];
@@ -83,43 +83,51 @@ __global__ void __launch_bounds__(256) paged_tokens_kernel(PagedArgs g) {
     page = page < g.cache.pages ? page : g.cache.pages - 1;
     return (((long long)page * g.cache.kv_heads + u.head) << g.cache.page_shift) + (key & slot_mask);
   };
-  auto issue = [&](int block, int slot) {
-    const uint32_t to = ring + slot * SLOT;
-    long long base[2];
-    int lo[2], hi[2];  // rows of the 16 that are loaded as they are
+  // Where a block's two times 16 keys are: rows of the cache, and which of each 16 are loaded as they are.
+  struct Place {
+    long long row[2];
+    int lo[2], hi[2];
+  };
+  auto place_of = [&](int block) {
+    Place p;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       int key = block * KEYS + t * 16;
       const int k0 = low & ~15, k1 = high & ~15;
       key = key < k0 ? k0 : key > k1 ? k1 : key;
-      base[t] = group_row(key);
-      lo[t] = low - key > 0 ? low - key : 0;
-      hi[t] = high - key < 15 ? high - key : 15;
+      p.row[t] = group_row(key);
+      p.lo[t] = low - key > 0 ? low - key : 0;
+      p.hi[t] = high - key < 15 ? high - key : 15;
     }
+    return p;
+  };
+  auto issue = [&](auto is_v, const Place& p, int slot) {
+    constexpr bool V = decltype(is_v)::value;
+    const uint32_t to = ring + slot * SLOT;
 #pragma unroll
-    for (int kv = 0; kv < 2; ++kv)
+    for (int t = 0; t < 2; ++t) {
+      const unsigned char* from = uniform_pointer((V ? g.cache.v : g.cache.k) + p.row[t] * RB);
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const unsigned char* from = uniform_pointer((kv ? g.cache.v : g.cache.k) + base[t] * RB);
-#pragma unroll
-        for (int n = 0; n < LOADS; ++n) {
-          uint32_t off = kv ? v_off[n] : k_off[n];
-          if (lo[t] > 0 || hi[t] < 15) {  // uniform
-            const int row = n * PER + load_row;
-            const int there = row < lo[t] ? lo[t] : row > hi[t] ? hi[t] : row;
-            off += (there - row) * RB;
-          }
-          dma16_so(off, from, to + kv * TILE + (t * LOADS + n) * 1024);
+      for (int n = 0; n < LOADS; ++n) {
+        uint32_t off = V ? v_off[n] : k_off[n];
+        if (p.lo[t] > 0 || p.hi[t] < 15) {  // uniform
+          const int row = n * PER + load_row;
+          const int there = row < p.lo[t] ? p.lo[t] : row > p.hi[t] ? p.hi[t] : row;
+          off += (there - row) * RB;
         }
+        dma16_so(off, from, to + V * TILE + (t * LOADS + n) * 1024);
       }
-    if (I8) {  // lane -> scale of a key (0..31) or a value (32..63)
+    }
+    if (I8 && !V) {  // lane -> scale of a key (0..31) or a value (32..63)
       const int t = (lane >> 4) & 1, row = lane & 15;
-      const int l0 = t ? lo[1] : lo[0], h0 = t ? hi[1] : hi[0];
+      const int l0 = t ? p.lo[1] : p.lo[0], h0 = t ? p.hi[1] : p.hi[0];
       const int there = row < l0 ? l0 : row > h0 ? h0 : row;
-      const float* from = (lane < 32 ? g.cache.k_scale : g.cache.v_scale) + (t ? base[1] : base[0]) + there;
+      const float* from = (lane < 32 ? g.cache.k_scale : g.cache.v_scale) + (t ? p.row[1] : p.row[0]) + there;
       dma4(from, to + 2 * TILE);
     }
   };
+  using K_TILE = std::false_type;
+  using V_TILE = std::true_type;
 
   f32x4 oacc[D / 16];
 #pragma unroll
@@ -127,14 +135,25 @@ __global__ void __launch_bounds__(256) paged_tokens_kernel(PagedArgs g) {
   float ref = kNothing, sum = 0.f;  // base 2; this lane's share of the sum
 
   const int mine = block1 - block0 > wave ? (block1 - block0 - wave + WAVES - 1) / WAVES : 0;
-  if (mine > 0) issue(block0 + wave, 0);
+  // Three halves of a block are under way beside the one in work: the values of block i + 1 are asked for ahead of block i's scores, the keys of
+  // block i + 2 behind them, when those of block i have been read.
+  Place next{};
+  if (mine > 0) {
+    const Place p = place_of(block0 + wave);
+    issue(K_TILE{}, p, 0);
+    issue(V_TILE{}, p, 0);
+    if (mine > 1) {
+      next = place_of(block0 + wave + WAVES);
+      issue(K_TILE{}, next, 1);
+    }
+  }
   for (int i = 0; i < mine; ++i) {
     const int block = block0 + wave + i * WAVES, slot = i & 1;
     if (i + 1 < mine) {
-      issue(block + WAVES, slot ^ 1);
-      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COUNT) : "memory");
+      issue(V_TILE{}, next, slot ^ 1);
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(KL + 2 * VL) : "memory");
     } else {
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(VL) : "memory");
     }
     const unsigned char* ks = lds + wave * S * SLOT + slot * SLOT;
     const uint32_t vs = ring + slot * SLOT + TILE;
@@ -161,6 +180,16 @@ __global__ void __launch_bounds__(256) paged_tokens_kernel(PagedArgs g) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) s[t][e] *= g.a2;
       }
+    }
+    float4 v_scale[2];
+    if (I8) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) v_scale[t] = *(const float4*)(ks + 2 * TILE + 128 + (t * 16 + h * 4) * 4);
+    }
+    if (i + 2 < mine) {
+      next = place_of(block + 2 * WAVES);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the keys and the scales have been read)
+      issue(K_TILE{}, next, slot);
     }
     const int key0 = block * KEYS;
     // (a block that every row of the tile sees whole needs no mask; rows past the last see nothing and are not stored)
@@ -198,7 +227,7 @@ __global__ void __launch_bounds__(256) paged_tokens_kernel(PagedArgs g) {
         sum += p[t][e];
       }
       if (I8) {
-        const float4 sc = *(const float4*)(ks + 2 * TILE + 128 + (t * 16 + h * 4) * 4);
+        const float4 sc = v_scale[t];
         p[t][0] *= sc.x, p[t][1] *= sc.y, p[t][2] *= sc.z, p[t][3] *= sc.w;
         if (edge) {
 #pragma unroll
@@ -209,6 +238,12 @@ __global__ void __launch_bounds__(256) paged_tokens_kernel(PagedArgs g) {
     }
     const bf16x8 pf = as_bf16x8(make_uint4(pack_bf16x2(p[0][0], p[0][1]), pack_bf16x2(p[0][2], p[0][3]), pack_bf16x2(p[1][0], p[1][1]),
                                            pack_bf16x2(p[1][2], p[1][3])));
+    if (i + 2 < mine)
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * KL + VL) : "memory");
+    else if (i + 1 < mine)
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(KL + VL) : "memory");
+    else
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
     for (int x = 0; x < D / 16; ++x) {
       bf16x8 vf;
@@ -227,7 +262,7 @@ __global__ void __launch_bounds__(256) paged_tokens_kernel(PagedArgs g) {
       }
       oacc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf, oacc[x], 0, 0, 0);
     }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the slot is refilled next)
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the values' slot is refilled next)
   }
   sum += __shfl_xor(sum, 16, 64);
   sum += __shfl_xor(sum, 32, 64);

@@ -23,6 +23,7 @@ class _StepsOnly:
     leaves every call to the steps, which give the same results, and says so on the first call on a GPU."""
     dense = attention = fused_attention = lstm_sequence = vm_run = set_workspace = staticmethod(lambda *a: None)
     quantize_rows = product = bind_products = staticmethod(lambda *a: None)
+    rotary = cache_write = cache_read = paged_attention = bind_paged = staticmethod(lambda *a: None)
 
     def __init__(self, why: ImportError):
         self.why = why
@@ -65,6 +66,9 @@ def _bind_host_calls(device) -> None:
     _host_calls.bind_products(*[ctypes.cast(getattr(lib, f), ctypes.c_void_p).value
                                 for f in ("nimble_quantize_rows_dyn", "nimble_dense_i8_dyn", "nimble_grouped_dense_dyn",
                                           "nimble_grouped_dense_i8_dyn")])
+    _host_calls.bind_paged(*[ctypes.cast(getattr(lib, f), ctypes.c_void_p).value
+                             for f in ("nimble_rotary_dyn", "nimble_cache_write_dyn", "nimble_cache_read_dyn", "nimble_paged_attention_plan_of",
+                                       "nimble_paged_attention_dyn")])
     _bound = True
 
 
@@ -424,6 +428,9 @@ def rotary(x: torch.Tensor, positions: torch.Tensor, table: torch.Tensor, interl
            out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Rotary positions: the first 2R elements of each head of x [T, H, D] (bf16, rows any stride apart) turned in pairs (i, i + R), or (2i, 2i + 1)
     where interleaved, by table[positions[t]] of [P, R, 2] (rotary_table); the rest copied.  positions [T] int64; out may be x."""
+    r = _host_calls.rotary(x, positions, table, interleaved, out)
+    if r is not None:
+        return r
     shape = nb.rotary_shape(tuple(x.shape), tuple(positions.shape), tuple(table.shape))
     with _together(x=x, positions=positions, table=table, out=out):
         y = out if out is not None else _alloc(shape, nb.BF16, x.device)
@@ -433,6 +440,8 @@ def rotary(x: torch.Tensor, positions: torch.Tensor, table: torch.Tensor, interl
         py, ys = _rows_ptr(y, "out")
         nb.nimble_rotary_dyn(px, xs, _ptr(positions, torch.int64, "positions"), _ptr(table, _F32, "table"), table.shape[0], py, ys, *shape,
                              table.shape[1], interleaved, _stream())
+    if not _bound:
+        _bind_host_calls(x.device)
     return y
 
 
@@ -441,6 +450,9 @@ def cache_write(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, sequences: 
     """Keys and values k, v [T, kv_heads, D] of a batch's rows into their places of the cache; with a table (rotary_table) the keys are
     turned by their positions first, and the queries q [T, heads, D] with them: returns these, contiguous (`out` may be q), or None without q.
     An 8-bit cache holds each token and head as quantize_rows does.  k, v and q may be parts of wider rows."""
+    r = _host_calls.cache_write(cache, k, v, sequences, q, table, interleaved, out)
+    if r is not None:
+        return None if r is True else r
     shape = nb.cache_write_shape(tuple(cache.k.shape), tuple(k.shape), tuple(v.shape), None if q is None else tuple(q.shape))
     if table is not None and (table.dim() != 3 or table.shape[2] != 2):
         raise nb.NimbleError(-3, f"cache_write: a table of {tuple(table.shape)}, (positions, pairs, 2) needed")
@@ -458,6 +470,8 @@ def cache_write(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, sequences: 
                                   _ptr(y, _BF, "out") if q is not None else 0, q.shape[1] if q is not None else 0,
                                   *((_ptr(table, _F32, "table"), table.shape[0], table.shape[1]) if table is not None else (0, 0, 0)),
                                   interleaved, _stream())
+    if not _bound:
+        _bind_host_calls(k.device)
     return y
 
 
@@ -465,12 +479,18 @@ def cache_read(cache: PagedCache, sequences: Sequences, rows: int, out_dtype: in
                out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """The keys and values of a batch's rows back out of the cache, each [rows, kv_heads, D] of out_dtype: the inverse of cache_write.  offsets that
     count each sequence's whole length read all of it.  Rows of no sequence are left as they were in `out`."""
+    if out is None:
+        r = _host_calls.cache_read(cache, sequences, rows, out_dtype)
+        if r is not None:
+            return r
     shape = nb.cache_read_shape(tuple(cache.k.shape), rows)
     ko, vo = out if out is not None else (None, None)
     with _together(cache_k=cache.k, cache_v=cache.v, k_scale=cache.k_scale, v_scale=cache.v_scale, k_out=ko, v_out=vo, **sequences._asdict()):
         c, s = _paged(cache, sequences, rows)
         ko, vo = (_output(t, shape, out_dtype, cache.k.device, "cache_read") for t in (ko, vo))
         nb.nimble_cache_read_dyn(c, s, _ptr(ko, _TORCH_DTYPE[out_dtype], "k_out"), _ptr(vo, _TORCH_DTYPE[out_dtype], "v_out"), out_dtype, _stream())
+    if not _bound:
+        _bind_host_calls(ko.device)
     return ko, vo
 
 
@@ -480,6 +500,10 @@ def paged_attention(q: torch.Tensor, cache: PagedCache, sequences: Sequences, al
     sequence, at position p, sees the keys max(0, p - window + 1) .. p (window = 0: all up to p); heads is a multiple of the cache's, whose
     heads / kv_heads query heads share keys.  alpha: 1 / sqrt(D) unless given.  A token of each sequence and chunks of many are served alike.
     workspace: of nb.paged_attention_plan's size, for one call at a time; by default a new one, so that calls may overlap."""
+    if workspace is None:
+        o = _host_calls.paged_attention(q, cache, sequences, alpha if alpha is not None else q.shape[-1] ** -0.5 if q.dim() == 3 else None, window, out)
+        if o is not None:
+            return o
     shape = nb.paged_attention_shape(tuple(q.shape), tuple(cache.k.shape))
     with _together(q=q, out=out, workspace=workspace, cache_k=cache.k, cache_v=cache.v, k_scale=cache.k_scale, v_scale=cache.v_scale,
                    **sequences._asdict()):
@@ -490,6 +514,8 @@ def paged_attention(q: torch.Tensor, cache: PagedCache, sequences: Sequences, al
             workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
         nb.nimble_paged_attention_dyn(*_rows_ptr(q, "q"), c, s, _ptr(y, _BF, "out"), shape[1], alpha if alpha is not None else shape[2] ** -0.5,
                                       window, workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream())
+    if not _bound:
+        _bind_host_calls(q.device)
     return y
 
 

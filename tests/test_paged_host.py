@@ -240,11 +240,11 @@ def test_grid_and_workspace_hold_every_batch():
         if not 0 < rows * group * kv_heads < 1 << 26:
             continue
         p = nb.paged_attention_plan(rows, S, width, group * kv_heads, kv_heads, page, D, rng.choice((nb.BF16, nb.I8)), window)
-        member = {0: (32, 512, 8), 1: (64, 512, 4)}[p.kernel]
+        member = {0: (32, (p.slots - 8) // 2, 8), 1: (64, (p.slots - 8) // 2, 4)}[p.kernel]
         units, slots, cut = _units(p, sizes, group, kv_heads, window, width * page, *member)
         assert units <= p.grid, (sizes, p)
         if p.parts:
-            assert slots <= p.slots and cut <= p.join_grid[0] and min(p.rows, max(n for _, n in sizes) * group) <= p.join_grid[1]
+            assert slots <= p.slots and cut <= p.slots // 2 and min(p.rows, max(n for _, n in sizes) * group) <= p.join_rows and p.join_grid
             assert p.workspace_bytes >= p.slots * p.rows * (D * 4 + 8) + (1 + cut) * 32
         else:
             assert slots == 0 and p.workspace_bytes == 0
