@@ -515,8 +515,7 @@ typedef struct nimble_paged_plan {
   int32_t kernel;           /* nimble_paged_kernel                                                     */
   int32_t rows;             /* rows of a tile                                                          */
   int32_t parts;            /* 1: sequences may be cut into parts, and a second launch joins them      */
-  int32_t join_rows;        /* the most rows of one tile that the second launch looks at               */
-  uint32_t grid, join_grid, block;
+  uint32_t grid, join_grid[2], block;
   int64_t slots;            /* parts that the workspace holds                                          */
   uint64_t workspace_bytes;
 } nimble_paged_plan;

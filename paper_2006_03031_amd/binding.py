@@ -57,8 +57,8 @@ class _CCache(ctypes.Structure):
 
 
 class _CPagedPlan(ctypes.Structure):
-    _fields_ = [("kernel", ctypes.c_int32), ("rows", ctypes.c_int32), ("parts", ctypes.c_int32), ("join_rows", ctypes.c_int32),
-                ("grid", ctypes.c_uint32), ("join_grid", ctypes.c_uint32), ("block", ctypes.c_uint32), ("slots", ctypes.c_int64),
+    _fields_ = [("kernel", ctypes.c_int32), ("rows", ctypes.c_int32), ("parts", ctypes.c_int32),
+                ("grid", ctypes.c_uint32), ("join_grid", ctypes.c_uint32 * 2), ("block", ctypes.c_uint32), ("slots", ctypes.c_int64),
                 ("workspace_bytes", ctypes.c_uint64)]
 
 
@@ -67,9 +67,8 @@ class PagedPlan:
     kernel: int
     rows: int
     parts: int
-    join_rows: int
     grid: int
-    join_grid: int
+    join_grid: Tuple[int, int]
     block: int
     slots: int
     workspace_bytes: int
@@ -471,7 +470,7 @@ def paged_attention_plan(rows: int, count: int, width: int, heads: int, kv_heads
                          window: int = 0) -> PagedPlan:
     c = _CPagedPlan()
     _check(load().nimble_paged_attention_plan_of(rows, count, width, heads, kv_heads, page, D, dtype, window, ctypes.byref(c)))
-    return PagedPlan(c.kernel, c.rows, c.parts, c.join_rows, c.grid, c.join_grid, c.block, c.slots, c.workspace_bytes)
+    return PagedPlan(c.kernel, c.rows, c.parts, c.grid, (c.join_grid[0], c.join_grid[1]), c.block, c.slots, c.workspace_bytes)
 
 
 # ---------------------------------------------------------------- device side

@@ -63,7 +63,7 @@ SequencesArgs sequences_args(const nimble_sequences& s) {
 struct PagedMember {
   int rows, block_keys, least_blocks;
 };
-static const PagedMember kPagedMembers[NIMBLE_PAGED_COUNT] = {{16, 32, 8}, {128, 64, 4}};
+static const PagedMember kPagedMembers[NIMBLE_PAGED_COUNT] = {{16, 32, 32}, {128, 64, 4}};
 // Workgroups that a compute unit holds at once, by their LDS (tokens) and registers: as many parts as fill the chip once are aimed at.
 static int paged_workgroups_per_cu(int kernel, int64_t D, int dtype) {
   if (kernel == NIMBLE_PAGED_CHUNKS) return 2;
@@ -92,13 +92,18 @@ static int plan_paged(int64_t rows, int64_t count, int64_t width, int64_t heads,
   const bool plenty = rows * group / m.rows * kv_heads >= 2 * target && keys <= 1024;
   out.parts = keys > (int64_t)m.block_keys * m.least_blocks && !plenty;
   if (tiles * kv_heads > kMostPagedGrid) return fail(NIMBLE_ERR_ARG, "more than 2^23 tiles");
-  out.grid = (uint32_t)(tiles * kv_heads + (out.parts ? target : 0));
   if (out.parts) {
+    // tokens: a span a workgroup, with two parts; chunks: a unit a workgroup, tiles and as many more as the cuts make
+    const bool spans = out.kernel == NIMBLE_PAGED_TOKENS;
+    out.grid = (uint32_t)(spans ? target : tiles * kv_heads + target);
     out.slots = 2 * target + 8;
-    out.join_rows = (int32_t)(rows * group < m.rows ? rows * group : m.rows);
-    const int64_t items = tiles * kv_heads < out.slots / 2 ? tiles * kv_heads : out.slots / 2, most = items * out.join_rows;
-    out.join_grid = (uint32_t)(most < 1024 ? most : 1024);  // (its workgroups go round)
-    out.workspace_bytes = (uint64_t)out.slots * m.rows * (D * 4 + 8) + (uint64_t)(1 + out.slots / 2) * kPagedItemWords * 4;
+    const int64_t most = rows * group < m.rows ? rows * group : m.rows;
+    out.join_grid[0] = (uint32_t)(spans ? target : tiles * kv_heads < target ? tiles * kv_heads : target);
+    const int64_t across = 2048 / out.join_grid[0] < 4 ? 4 : 2048 / out.join_grid[0];  // (few tiles: their rows side by side)
+    out.join_grid[1] = (uint32_t)(most < across ? most : across);
+    out.workspace_bytes = (uint64_t)out.slots * m.rows * (D * 4 + 8) + (uint64_t)(1 + target) * kPagedItemWords * 4;
+  } else {
+    out.grid = (uint32_t)(tiles * kv_heads);
   }
   *p = out;
   return NIMBLE_OK;

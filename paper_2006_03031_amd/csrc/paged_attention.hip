@@ -13,18 +13,18 @@ int check_rows(const void* p, int64_t stride, int64_t heads, int64_t D, const ch
 template <int D>
 static void launch_paged(const PagedArgs& g, const nimble_paged_plan& p, bool int8, hipStream_t stream) {
   auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(p.grid), dim3(p.block), 0, stream, g); };
-  const bool chunks = p.kernel == NIMBLE_PAGED_CHUNKS;
-  if (chunks) {
+  auto join = [&](auto kernel) {
+    if (p.parts) hipLaunchKernelGGL(kernel, dim3(p.join_grid[0], p.join_grid[1]), dim3(256), 0, stream, g);
+  };
+  if (p.kernel == NIMBLE_PAGED_CHUNKS) {
     if (int8) launch(paged_chunks_kernel<D, true>);
     else launch(paged_chunks_kernel<D, false>);
+    join(paged_join_kernel<128, D>);
   } else {
     if (int8) launch(paged_tokens_kernel<D, true>);
     else launch(paged_tokens_kernel<D, false>);
+    join(paged_join_kernel<16, D>);
   }
-  if (!p.parts) return;
-  auto join = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(p.join_grid), dim3(256), 0, stream, g); };
-  if (chunks) join(paged_join_kernel<128, D>);
-  else join(paged_join_kernel<16, D>);
 }
 
 }  // namespace nimble
@@ -65,7 +65,6 @@ int nimble_paged_attention_dyn(const void* q, int64_t q_stride, const nimble_cac
   if (p.parts) {
     g.slots = (int)p.slots;
     g.target_units = (int)(p.slots - 8) / 2;  // (see plan_paged)
-    g.join_rows = p.join_rows;
     g.part = (float*)workspace;
     g.stat = (float2*)(g.part + p.slots * p.rows * cache->D);
     g.items = (int*)(g.stat + p.slots * p.rows);

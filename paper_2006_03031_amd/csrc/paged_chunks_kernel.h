@@ -35,16 +35,20 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 4))
   const bool found = find_unit<ROWS, KEYS, LEAST>(g, blockIdx.x, u, items);
   if (g.slots && blockIdx.x == 0 && tid == 0) g.items[0] = found ? items : 0;
   if (!found) return;
-  if (u.parts > 1 && (u.slot >= g.slots || u.item >= g.slots / 2)) return;  // (not with offsets that keep to their description)
+  if (u.parts > 1 && (u.slot >= g.slots || u.item >= g.target_units)) return;  // (not with offsets that keep to their description)
   int low, high, block0, block1;
   unit_keys<ROWS, KEYS>(g, u, low, high, block0, block1);
   const int rows = u.seq.n * g.group, before = u.seq.length - u.seq.n;
 
   // this lane's row, and the blocks of the workgroup's that its wave's rows see: wave0 .. wave1 - 1
-  const int m0 = u.tile * ROWS + wave * 32, m = m0 + r32;
-  const int m_ld = m < rows ? m : rows - 1, token = m_ld / g.group;
+  const int m0 = u.tile * ROWS + wave * 32;
+  const int m = m0 + r32, m_ld = m < rows ? m : rows - 1, token = m_ld / g.group;
   const int pos = m < rows ? before + token : -1;
   const int first = g.window > 0 ? pos - g.window + 1 : 0;
+  const u16* q = g.q + (long long)(u.seq.first + token) * g.q_stride + (u.head * g.group + m_ld - token * g.group) * D;
+  bf16x8 qf[D / 16];
+#pragma unroll
+  for (int dd = 0; dd < D / 16; ++dd) qf[dd] = as_bf16x8(*(const uint4*)(q + dd * 16 + h * 8));
   int wave0 = block1, wave1 = block0, wave_least = -1, wave_high = -1;
   if (m0 < rows) {
     const int last = (m0 + 32 < rows ? m0 + 32 : rows) - 1;
@@ -58,11 +62,6 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 4))
   }
   wave0 = __builtin_amdgcn_readfirstlane(wave0);
   wave1 = __builtin_amdgcn_readfirstlane(wave1);
-
-  const u16* q = g.q + (long long)(u.seq.first + token) * g.q_stride + (u.head * g.group + m_ld - token * g.group) * D;
-  bf16x8 qf[D / 16];
-#pragma unroll
-  for (int dd = 0; dd < D / 16; ++dd) qf[dd] = as_bf16x8(*(const uint4*)(q + dd * 16 + h * 8));
 
   auto k_swizzle = [](int row) { return (row / (256 / RB)) & (CH < 16 ? CH - 1 : 15); };
   auto v_swizzle = [](int row) { return RB == 256 ? 4 * (row & 3) : 4 * ((row >> 1) & 1); };
@@ -146,7 +145,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 4))
   for (int t = 0; t < NT; ++t)
 #pragma unroll
     for (int e = 0; e < 16; ++e) oacc[t][e] = 0.f;
-  float ref = kNothing, sum0 = 0.f, sum1 = 0.f;  // bf16: in units of the scores; 8 bits: base 2
+  float ref = kNothing, sum0 = 0.f, sum1 = 0.f;  // ref: bf16 in units of the scores, 8 bits base 2
   const float a2 = I8 ? 1.0f : g.a2;
 
   const int i16 = lane & 15, dh = (lane >> 4) & 1;
@@ -157,20 +156,34 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 4))
   // chunk 2 dd + h of row 32 t + r: a row's first byte is a multiple of its length, so that the swizzle is one exclusive or
   typedef const __attribute__((address_space(3))) uint4* LdsPtr;
   const uint32_t k_at = ring + r32 * RB + (h ^ k_swizzle(r32)) * 16;
-  auto qk = [&](f32x16& s, int slot, int t, int dd) {
+  auto qk = [&](f32x16 (&s)[2], int slot, int dd) {
     uint32_t at = k_at + slot * TILE;
     asm volatile("" : "+v"(at));
-    const LdsPtr from = (LdsPtr)(uintptr_t)((at ^ (dd * 32)) + t * 32 * RB);
-    const bf16x8 kf = as_bf16x8(make_uint4(from->x, from->y, from->z, from->w));
     const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[dd], dd == 0 ? zero : s, 0, 0, 0);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const LdsPtr from = (LdsPtr)(uintptr_t)((at ^ (dd * 32)) + t * 32 * RB);
+      const bf16x8 kf = as_bf16x8(make_uint4(from->x, from->y, from->z, from->w));
+      s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[dd], dd == 0 ? zero : s[t], 0, 0, 0);
+    }
+  };
+  // Which of this lane's keys of a block its row sees: from `least` on `range` + 1, counted from the lane's first (one comparison each).
+  struct Seen {
+    unsigned least, range;
+    __device__ __forceinline__ bool operator()(int key) const { return (unsigned)key - least <= range; }
+  };
+  auto seen_of = [&](int key0) {
+    const int most = pos - key0 - h * 4, least = first - key0 - h * 4;
+    Seen seen{most < least ? 0x40000000u : (unsigned)least, most < least ? 0u : (unsigned)(most - least)};
+    asm volatile("" : "+v"(seen.least), "+v"(seen.range));  // (else the comparisons of both uses are kept in scalar registers)
+    return seen;
   };
   auto block = [&](int i) {
-    f32x16 s[2];
     const int slot = i & 1, key0 = i * KEYS;
     const float* scales = (const float*)(lds + 4 * TILE) + slot * 2 * KEYS;
+    f32x16 s[2];
 #pragma unroll
-    for (int dd = 0; dd < D / 16; ++dd) qk(s[0], slot, 0, dd), qk(s[1], slot, 1, dd);
+    for (int dd = 0; dd < D / 16; ++dd) qk(s, slot, dd);
     const bool edge = key0 + KEYS - 1 > wave_least || (g.window > 0 && key0 <= wave_high - g.window);
     if (I8) {
 #pragma unroll
@@ -181,15 +194,13 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 4))
           s[t][4 * b] *= sc.x, s[t][4 * b + 1] *= sc.y, s[t][4 * b + 2] *= sc.z, s[t][4 * b + 3] *= sc.w;
         }
     }
-    const int most = pos - key0 - h * 4, least = first - key0 - h * 4;  // of this lane's keys, counted from its first
     if (edge) {
+      const Seen seen = seen_of(key0);
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int key = t * 32 + (e >> 2) * 8 + (e & 3);
-          if (key > most || key < least) s[t][e] = -INFINITY;
-        }
+        for (int e = 0; e < 16; ++e)
+          if (!seen(t * 32 + (e >> 2) * 8 + (e & 3))) s[t][e] = -INFINITY;
     }
     float top = ref;
 #pragma unroll
@@ -212,34 +223,31 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 4))
     const uint32_t vs = ring + 2 * TILE + slot * TILE;
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {
+    for (int z = 0; z < 4; ++z) {
       float p[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float sx = s[x >> 1][(x & 1) * 8 + e];
+        const float sx = s[z >> 1][(z & 1) * 8 + e];
         p[e] = __builtin_amdgcn_exp2f(I8 ? sx + nm2 : fmaf(sx, a2, nm2));
         if (e & 1) sum1 += p[e]; else sum0 += p[e];
       }
       if (I8) {
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-          const float4 sc = *(const float4*)(scales + KEYS + x * 16 + b * 8 + h * 4);
+          const float4 sc = *(const float4*)(scales + KEYS + z * 16 + b * 8 + h * 4);
           p[4 * b] *= sc.x, p[4 * b + 1] *= sc.y, p[4 * b + 2] *= sc.z, p[4 * b + 3] *= sc.w;
         }
         if (edge) {
-          int most2 = most, least2 = least;
-          asm volatile("" : "+v"(most2), "+v"(least2));  // (else 32 comparisons are kept in scalar registers)
+          const Seen seen = seen_of(key0);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const int key = x * 16 + (e >> 2) * 8 + (e & 3);
-            if (key > most2 || key < least2) p[e] = 0.f;  // (its scale may be NaN)
-          }
+          for (int e = 0; e < 8; ++e)
+            if (!seen(z * 16 + (e >> 2) * 8 + (e & 3))) p[e] = 0.f;  // (its scale may be NaN)
         }
       }
       const bf16x8 pf = as_bf16x8(make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7])));
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        const uint32_t at = vs + v_off[t] + x * 16 * RB;
+        const uint32_t at = vs + v_off[t] + z * 16 * RB;
         const uint2 lo = lds_read_tr16(at), hi = lds_read_tr16(at + 8 * RB);
         oacc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(make_uint4(lo.x, lo.y, hi.x, hi.y)), pf, oacc[t], 0, 0, 0);
       }
@@ -277,11 +285,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 4))
       if (i >= wave0 && i < wave1) block(i);
     }
   }
-  float sum = sum0 + sum1;
-  sum += __shfl_xor(sum, 32, 64);
-  const float ref2 = ref > kNothing ? ref * a2 : kNothing;
-
-  if (u.parts > 1 && u.part == 0 && tid == 0) put_item(g, u);
+  if (u.parts > 1 && u.part == 0 && tid == 0) put_item(g, u, u.item, u.parts, u.slot, u.slot + g.cache.kv_heads, g.cache.kv_heads);
   if (m0 >= rows) return;
   if (!I8) {
     bool odd = false;
@@ -295,15 +299,17 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 4))
       return;
     }
   }
+  float sum = sum0 + sum1;
+  sum += __shfl_xor(sum, 32, 64);
   if (m >= rows) return;
-  if (u.parts > 1) {
+  if (u.slot >= 0) {
     const long long to = (long long)u.slot * ROWS + wave * 32 + r32;
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int b = 0; b < 4; ++b)
         *(float4*)(g.part + to * D + t * 32 + b * 8 + h * 4) = make_float4(oacc[t][4 * b], oacc[t][4 * b + 1], oacc[t][4 * b + 2], oacc[t][4 * b + 3]);
-    if (h == 0) g.stat[to] = make_float2(ref2, sum);
+    if (h == 0) g.stat[to] = make_float2(ref > kNothing ? ref * a2 : kNothing, sum);
     return;
   }
   const float inv = pos < 0 ? 0.f : 1.0f / sum;

@@ -18,8 +18,8 @@ struct PagedArgs {
   float a2;            // alpha log2 e
   float* part;         // [slots][rows][D] sums of parts, not divided
   float2* stat;        // [slots][rows] their largest score (base 2) and sum of probabilities
-  int* items;          // [0]: tiles that were cut, then 8 words each
-  int slots, target_units, join_rows;  // join_rows: the most rows of a tile
+  int* items;          // [0]: tiles that may have been cut, then kPagedItemWords each, from the second entry on
+  int slots, target_units;
 };
 
 constexpr float kNothing = -3.0e38f;  // the reference of a row that has seen no key yet
@@ -36,8 +36,31 @@ struct PagedUnit {
   Sequence seq;
   int s, head, tile, tiles;
   int part, parts;
-  int slot, item;  // in the workspace, where parts > 1
+  int slot, item;  // in the workspace; slot -1: the tile was not cut
 };
+
+// Inclusive sums over the 64 lanes, in registers.
+template <typename T>
+__device__ __forceinline__ T wave_scan(T x) {
+  auto step = [&](auto ctrl, auto rows) {
+    constexpr int C = decltype(ctrl)::value, R = decltype(rows)::value;
+    unsigned w[sizeof(T) / 4];
+    __builtin_memcpy(w, &x, sizeof x);
+#pragma unroll
+    for (unsigned& y : w) y = (unsigned)__builtin_amdgcn_update_dpp(0, (int)y, C, R, 0xf, false);
+    T y;
+    __builtin_memcpy(&y, w, sizeof y);
+    x += y;
+  };
+  using std::integral_constant;
+  step(integral_constant<int, 0x111>{}, integral_constant<int, 0xf>{});  // from 1, 2, 4 and 8 lanes below in a row of 16
+  step(integral_constant<int, 0x112>{}, integral_constant<int, 0xf>{});
+  step(integral_constant<int, 0x114>{}, integral_constant<int, 0xf>{});
+  step(integral_constant<int, 0x118>{}, integral_constant<int, 0xf>{});
+  step(integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{});  // the last of rows 0 and 2 to rows 1 and 3
+  step(integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{});  // the last of row 1 to rows 2 and 3
+  return x;
+}
 
 template <int ROWS, int KEYS>
 __device__ __forceinline__ void tile_work(const PagedArgs& g, const Sequence& q, int& tiles, int& blocks) {
@@ -47,7 +70,8 @@ __device__ __forceinline__ void tile_work(const PagedArgs& g, const Sequence& q,
   blocks = tiles ? (keys + KEYS - 1) / KEYS : 0;
 }
 
-// The most blocks of one part.  The same in every lane of every wave of a call.
+// The blocks of one part, give or take half as many: a tile is cut into as many parts as comes closest.  (Never more than that: 512 tiles of 224 to
+// 256 blocks, of which half were cut, took 550 us, one and a half rounds; whole WHOLE_US.)  The same in every lane of every wave of a call.
 template <int ROWS, int KEYS, int LEAST>
 __device__ __forceinline__ int part_blocks(const PagedArgs& g) {
   const int lane = threadIdx.x & 63;
@@ -60,8 +84,7 @@ __device__ __forceinline__ int part_blocks(const PagedArgs& g) {
       total += (float)tiles * (float)blocks;
     }
   }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o, 64);
+  total = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(wave_scan(total)), 63));
   const float most = ceilf(total * (float)g.cache.kv_heads / (float)g.target_units) + 1.0f;
   return most < (float)LEAST ? LEAST : most > 1.0e9f ? 1000000000 : (int)most;
 }
@@ -82,14 +105,9 @@ __device__ __forceinline__ bool find_unit(const PagedArgs& g, unsigned unit, Pag
       q = sequence_of(g.seqs, s, g.cache.page_shift);
       tile_work<ROWS, KEYS>(g, q, tiles, blocks);
     }
-    const int parts = blocks > most ? (blocks + most - 1) / most : 1;
+    const int parts = (int)(((unsigned)blocks + (unsigned)most / 2) / (unsigned)most) > 1 ? (int)(((unsigned)blocks + (unsigned)most / 2) / (unsigned)most) : 1;
     const unsigned mine = (unsigned)tiles * parts, mine_cut = parts > 1 ? mine : 0, tiles_cut = parts > 1 ? tiles : 0;
-    unsigned a = mine, b = mine_cut, c = tiles_cut;  // inclusive sums
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const unsigned ua = __shfl_up(a, o, 64), ub = __shfl_up(b, o, 64), uc = __shfl_up(c, o, 64);
-      if (lane >= o) a += ua, b += ub, c += uc;
-    }
+    const unsigned a = wave_scan(mine), b = wave_scan(mine_cut), c = wave_scan(tiles_cut);
     const unsigned long long here = __ballot(units + a > want);
     if (!found && here) {
       const int l = __ffsll((unsigned long long)here) - 1;
@@ -105,7 +123,7 @@ __device__ __forceinline__ bool find_unit(const PagedArgs& g, unsigned unit, Pag
       const int back = rest / u.parts;
       u.tile = u.tiles - 1 - back;
       u.part = rest - back * u.parts;
-      u.slot = (int)((cut_units + (unsigned)of((int)(b - mine_cut)) + rest) * G + u.head);
+      u.slot = u.parts == 1 ? -1 : (int)((cut_units + (unsigned)of((int)(b - mine_cut)) + rest) * G + u.head);
       u.item = (int)((cut_tiles + (unsigned)of((int)(c - tiles_cut)) + back) * G + u.head);
       found = true;
     }
@@ -137,6 +155,112 @@ __device__ __forceinline__ void unit_keys(const PagedArgs& g, const PagedUnit& u
   const int b0 = low / KEYS, nb = high / KEYS + 1 - b0, q = nb / u.parts, r = nb - q * u.parts;  // (the first r parts have one more)
   block0 = __builtin_amdgcn_readfirstlane(b0 + u.part * q + (u.part < r ? u.part : r));
   block1 = __builtin_amdgcn_readfirstlane(block0 + q + (u.part < r ? 1 : 0));
+}
+
+// ---------------------------------------------------------------------------
+// The other way to share the work, for few rows, where a tile is one sequence's keys and what counts is that every workgroup has the same
+// number of them: the blocks of all tiles in a row, one sequence after the other, cut into spans of equal length, one a workgroup.  A span may
+// end one tile, hold several and begin another.  A workgroup leaves at most two parts: of the tile that another one began (slot 2 w) and of
+// the one that it begins (slot 2 w + 1); the second launch finds a cut tile by the workgroup that began it.
+//   A tile counts as many blocks as the longest of its sequence, rounded up to LEAST, so that spans of that length, where there is little to do,
+// do not cross tiles; a share of them is that share of the blocks that it has.
+//   (64 sequences of up to 8192 keys, uneven, as tiles cut into equal parts of at most a 512th of all: 144 us, 1.5 rounds of workgroups; in
+// spans SPAN_US.)
+// ---------------------------------------------------------------------------
+template <int ROWS, int KEYS, int LEAST>
+struct SpanWalk {
+  typedef unsigned long long u64;
+  const PagedArgs& g;
+  int base;                // this lane's sequence is base + lane
+  Sequence q;
+  int tiles, blocks;
+  u64 ahead, upto;         // blocks of the sequences ahead of these 64, and up to this lane's with them
+  u64 at, end, per;        // what is left of the span, and its length
+  bool none;               // the span is empty
+
+  static __device__ __forceinline__ u64 lane_value(u64 x, int l) {
+    return ((u64)(unsigned)__builtin_amdgcn_readlane((int)(x >> 32), l) << 32) | (unsigned)__builtin_amdgcn_readlane((int)(unsigned)x, l);
+  }
+  __device__ __forceinline__ u64 look(int s) {
+    q = Sequence{0, 0, 0};
+    tiles = blocks = 0;
+    if (s >= g.seqs.count) return 0;
+    q = sequence_of(g.seqs, s, g.cache.page_shift);
+    tile_work<ROWS, KEYS>(g, q, tiles, blocks);
+    blocks = g.slots ? (blocks + LEAST - 1) / LEAST * LEAST : blocks > 0;  // (without a workspace a tile counts once, and so does a span)
+    if (blocks == 0 && tiles) blocks = g.slots ? LEAST : 1;                // rows that see nothing
+    return (u64)tiles * (unsigned)blocks * (unsigned)g.cache.kv_heads;
+  }
+  __device__ __forceinline__ void load(int b) {
+    const int lane = threadIdx.x & 63;
+    base = b;
+    upto = ahead + wave_scan(look(b + lane));
+  }
+  __device__ __forceinline__ SpanWalk(const PagedArgs& args, unsigned w) : g(args) {
+    const int lane = threadIdx.x & 63;
+    u64 total = 0;
+    ahead = 0;
+    if (g.seqs.count > 64) {
+      for (int b = 0; b < g.seqs.count; b += 64) total += look(b + lane);
+      total = lane_value(wave_scan(total), 63);
+      load(0);
+    } else {
+      load(0);
+      total = lane_value(upto, 63);
+    }
+    per = 1;
+    if (g.slots) {
+      const unsigned spans = (unsigned)g.target_units;
+      per = total >> 31 ? (total + spans - 1) / spans : ((unsigned)total + spans - 1) / spans;
+      if (per < LEAST) per = LEAST;
+    }
+    at = (u64)w * per;
+    end = at + per < total ? at + per : total;
+    none = at >= total;
+  }
+  // The tile that the rest of the span begins with: x0 .. x1 - 1 of its u.parts = blocks.  tile_at: where the tile begins.
+  __device__ __forceinline__ void next(PagedUnit& u, int& x0, int& x1, u64& tile_at) {
+    while (at >= lane_value(upto, 63)) {
+      ahead = lane_value(upto, 63);
+      load(base + 64);
+    }
+    const int l = __ffsll(__ballot(upto > at)) - 1;
+    auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
+    u.s = base + l;
+    u.seq.first = of(q.first);
+    u.seq.n = of(q.n);
+    u.seq.length = of(q.length);
+    u.tiles = of(tiles);
+    u.parts = of(blocks);
+    const u64 first = lane_value(upto, l) - (u64)u.tiles * (unsigned)u.parts * (unsigned)g.cache.kv_heads, in = at - first;
+    const u64 which = in >> 32 ? in / (unsigned)u.parts : (unsigned)in / (unsigned)u.parts;
+    tile_at = first + which * (unsigned)u.parts;
+    u.tile = (int)((unsigned)which / (unsigned)g.cache.kv_heads);   // (tiles * heads are fewer than 2^23)
+    u.head = (int)((unsigned)which - (unsigned)u.tile * (unsigned)g.cache.kv_heads);
+    x0 = (int)(at - tile_at);
+    x1 = end - tile_at < (u64)u.parts ? (int)(end - tile_at) : u.parts;
+    at = tile_at + x1;
+  }
+  // The workgroup whose span holds block x.
+  __device__ __forceinline__ unsigned owner(u64 x) const { return (unsigned)(x >> 32 || per >> 32 ? x / per : (unsigned)x / (unsigned)per); }
+};
+
+// The blocks of a span's share of a tile.
+template <int ROWS, int KEYS>
+__device__ __forceinline__ void share_keys(const PagedArgs& g, const PagedUnit& u, int x0, int x1, int& low, int& high, int& block0, int& block1) {
+  PagedUnit all = u;
+  all.part = 0;
+  all.parts = 1;
+  unit_keys<ROWS, KEYS>(g, all, low, high, block0, block1);
+  const unsigned nb = block1 - block0;
+  auto share = [&](int x) {
+    if (x == u.parts) return (int)nb;
+    const unsigned long long t = (unsigned long long)nb * (unsigned)x;
+    return (int)(t >> 32 ? t / (unsigned)u.parts : (unsigned)t / (unsigned)u.parts);
+  };
+  const int b0 = block0;
+  block0 = __builtin_amdgcn_readfirstlane(b0 + share(x0));
+  block1 = __builtin_amdgcn_readfirstlane(b0 + share(x1));
 }
 
 // A pointer that is the same in all lanes, in scalar registers.
@@ -197,7 +321,7 @@ __device__ __forceinline__ void careful_row(const PagedArgs& g, const PagedUnit&
       for (int i = 0; i < P; ++i) acc[i] = fmaf(px, bf2f(((const u16*)g.cache.v)[rx * D + i * 64 + lane]), acc[i]);
     }
   }
-  if (u.parts > 1) {
+  if (u.slot >= 0) {
     const long long to = (long long)u.slot * ROWS + m - u.tile * ROWS;
 #pragma unroll
     for (int i = 0; i < P; ++i) g.part[to * D + i * 64 + lane] = acc[i];
@@ -210,11 +334,11 @@ __device__ __forceinline__ void careful_row(const PagedArgs& g, const PagedUnit&
   for (int i = 0; i < P; ++i) o[i * 64 + lane] = f2bf(acc[i] * inv);
 }
 
-// What the second launch has to know of a tile that was cut.
-__device__ __forceinline__ void put_item(const PagedArgs& g, const PagedUnit& u) {
-  int* item = g.items + (1 + u.item) * kPagedItemWords;
-  item[0] = u.slot, item[1] = u.parts, item[2] = u.tile, item[3] = u.head;
-  item[4] = u.seq.first, item[5] = u.seq.n, item[6] = u.seq.length, item[7] = g.cache.kv_heads;  // (slots of a tile's parts are kv_heads apart)
+// What the second launch has to know of a tile that was cut: its first part's slot, the second's, and how far apart those behind it are.
+__device__ __forceinline__ void put_item(const PagedArgs& g, const PagedUnit& u, int which, int parts, int slot, int second, int apart) {
+  int* item = g.items + (1 + which) * kPagedItemWords;
+  item[0] = parts, item[1] = slot, item[2] = second, item[3] = apart;
+  item[4] = u.tile, item[5] = u.head, item[6] = u.seq.first, item[7] = u.seq.n, item[8] = u.seq.length;
 }
 
 __device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
@@ -236,79 +360,83 @@ __device__ __forceinline__ uint2 codes_to_bf16(uint32_t w) {
 }
 
 // ---------------------------------------------------------------------------
-// The parts of a row joined, in the order of the parts: o = sum_x 2^(ref_x - top) part_x / sum_x 2^(ref_x - top) sum_x.  A wave a row; where there
-// are fewer rows than workgroups a workgroup a row, whose waves take every fourth part.  A lane looks at one part's (ref, sum) and the wave at its
+// The parts of a row joined, in the order of the parts: o = sum_x 2^(ref_x - top) part_x / sum_x 2^(ref_x - top) sum_x.  A wave a row; with more
+// than 8 parts a workgroup a row, whose waves take every fourth part.  A lane looks at one part's (ref, sum) and the wave at its
 // sums one part after the other, 8 loads at a time.
 // ---------------------------------------------------------------------------
 template <int ROWS, int D>
 __global__ void __launch_bounds__(256) paged_join_kernel(PagedArgs g) {
-  constexpr int P = D / 64;
+  constexpr int P = D / 64, MANY = 8;
   typedef float Piece __attribute__((ext_vector_type(P)));
   __shared__ float2 wave_stat[4];
   __shared__ Piece wave_sums[4][64];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const long long count = (long long)g.items[0] * g.join_rows;
-  const bool together = count <= gridDim.x;
-  const int step = together ? 4 : 1;
-  for (long long at = together ? blockIdx.x : (long long)blockIdx.x * 4 + wave; at < count; at += together ? gridDim.x : 4ll * gridDim.x) {
-    const int* item = g.items + (1 + at / g.join_rows) * kPagedItemWords;
-    const int row = (int)(at % g.join_rows);
-    const int slot = item[0], parts = item[1], apart = item[7], mm = item[2] * ROWS + row;
-    if (mm >= item[5] * g.group) continue;  // (the same in the whole workgroup where its waves work together)
-    float top = kNothing, total = 0.f;
-    Piece acc{};
-    for (int x0 = together ? wave : 0; x0 < parts; x0 += 64 * step) {
-      const int x = x0 + lane * step;
-      const float2 st = x < parts ? g.stat[(long long)(slot + x * apart) * ROWS + row] : make_float2(kNothing, 0.f);
-      float next = fmaxf(top, st.x);
-#pragma unroll
-      for (int o = 32; o > 0; o >>= 1) next = fmaxf(next, __shfl_xor(next, o, 64));
-      const float back = __builtin_amdgcn_exp2f(top - next), scale = __builtin_amdgcn_exp2f(st.x - next);
-      float sum = st.y * scale;
-#pragma unroll
-      for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
-      total = total * back + sum;
-      acc *= back;
-      top = next;
-      const int n = (parts - x0 + step - 1) / step < 64 ? (parts - x0 + step - 1) / step : 64;
-      for (int y0 = 0; y0 < n; y0 += 8) {
+  const int count = g.items[0];
+  for (int i = blockIdx.x; i < count; i += gridDim.x) {
+    const int* item = g.items + (1 + i) * kPagedItemWords;
+    const int parts = item[0], slot = item[1], second = item[2], apart = item[3], tile = item[4], head = item[5];
+    if (parts < 2) continue;
+    const int left = item[7] * g.group - tile * ROWS, rows = left < ROWS ? left : ROWS;
+    const bool together = parts > MANY;
+    const int step = together ? 4 : 1;
+    for (int row = blockIdx.y + (together ? 0 : wave * gridDim.y); row < rows; row += together ? gridDim.y : 4 * gridDim.y) {
+      float top = kNothing, total = 0.f;
+      Piece acc{};
+      auto place = [&](int x) { return (long long)(x ? second + (x - 1) * apart : slot) * ROWS + row; };
+      for (int x0 = together ? wave : 0; x0 < parts; x0 += 64 * step) {
+        const int x = x0 + lane * step;
+        const float2 st = x < parts ? g.stat[place(x)] : make_float2(kNothing, 0.f);
+        const int n = (parts - x0 + step - 1) / step < 64 ? (parts - x0 + step - 1) / step : 64;
         Piece v[8];
+        auto load = [&](int y0) {
 #pragma unroll
-        for (int y = 0; y < 8; ++y) {
-          const int part = x0 + (y0 + y < n ? y0 + y : n - 1) * step;
-          v[y] = *(const Piece*)(g.part + ((long long)(slot + part * apart) * ROWS + row) * D + lane * P);
+          for (int y = 0; y < 8; ++y) v[y] = *(const Piece*)(g.part + place(x0 + (y0 + y < n ? y0 + y : n - 1) * step) * D + lane * P);
+        };
+        load(0);
+        float next = fmaxf(top, st.x);
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) next = fmaxf(next, __shfl_xor(next, o, 64));
+        const float back = __builtin_amdgcn_exp2f(top - next), scale = __builtin_amdgcn_exp2f(st.x - next);
+        float sum = st.y * scale;
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+        total = total * back + sum;
+        acc *= back;
+        top = next;
+        for (int y0 = 0; y0 < n; y0 += 8) {
+          if (y0) load(y0);
+#pragma unroll
+          for (int y = 0; y < 8; ++y)
+            if (y0 + y < n) acc += v[y] * __shfl(scale, y0 + y, 64);
         }
-#pragma unroll
-        for (int y = 0; y < 8; ++y)
-          if (y0 + y < n) acc += v[y] * __shfl(scale, y0 + y, 64);
       }
-    }
-    if (together) {
-      __syncthreads();
-      if (lane == 0) wave_stat[wave] = make_float2(top, total);
-      wave_sums[wave][lane] = acc;
-      __syncthreads();
-      if (wave > 0) continue;
-      float t = kNothing;
+      if (together) {
+        __syncthreads();
+        if (lane == 0) wave_stat[wave] = make_float2(top, total);
+        wave_sums[wave][lane] = acc;
+        __syncthreads();
+        if (wave > 0) continue;
+        float t = kNothing;
 #pragma unroll
-      for (int w = 0; w < 4; ++w) t = fmaxf(t, wave_stat[w].x);
-      total = 0.f;
-      acc = Piece{};
+        for (int w = 0; w < 4; ++w) t = fmaxf(t, wave_stat[w].x);
+        total = 0.f;
+        acc = Piece{};
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const float scale = __builtin_amdgcn_exp2f(wave_stat[w].x - t);
-        total += wave_stat[w].y * scale;
-        acc += wave_sums[w][lane] * scale;
+        for (int w = 0; w < 4; ++w) {
+          const float scale = __builtin_amdgcn_exp2f(wave_stat[w].x - t);
+          total += wave_stat[w].y * scale;
+          acc += wave_sums[w][lane] * scale;
+        }
       }
+      const int mm = tile * ROWS + row, tok = mm / g.group;
+      const float inv = item[8] - item[7] + tok < 0 ? 0.f : 1.0f / total;
+      u16* o = g.o + ((long long)(item[6] + tok) * g.heads + head * g.group + mm - tok * g.group) * D + lane * P;
+      if constexpr (P == 2)
+        *(uint32_t*)o = pack_bf16x2(acc[0] * inv, acc[1] * inv);
+      else
+        *o = f2bf(acc[0] * inv);
     }
-    const int tok = mm / g.group;
-    const float inv = item[6] - item[5] + tok < 0 ? 0.f : 1.0f / total;
-    u16* o = g.o + ((long long)(item[4] + tok) * g.heads + item[3] * g.group + mm - tok * g.group) * D + lane * P;
-    if constexpr (P == 2)
-      *(uint32_t*)o = pack_bf16x2(acc[0] * inv, acc[1] * inv);
-    else
-      *o = f2bf(acc[0] * inv);
   }
 }
 

@@ -14,13 +14,14 @@ namespace nimble {
 //   8 bits:  codes become bf16, which holds them exactly, behind the LDS reads; a key's scale multiplies its scores, a value's its
 //            probability.  A lane reads 16 codes of a key row where it reads 8 elements of bf16, so that the elements of a
 //            matrix instruction's k are taken from the row in another order, and those of q in the same.
+//   Work:    a workgroup walks its span of all tiles' blocks (SpanWalk).
 //   Loads:   direct global->LDS loads into the wave's own ring of two blocks, waited for by count: no barrier in the loop.  16 keys lie in one
 //            page, whose number is a scalar.  Chunk c of row r sits at c ^ swizzle(r).  Keys outside of what the tile sees repeat the
 //            nearest one that it does.
 // ---------------------------------------------------------------------------
 template <int D, bool I8>
 __global__ void __launch_bounds__(256) paged_tokens_kernel(PagedArgs g) {
-  constexpr int ROWS = 16, KEYS = 32, LEAST = 8, WAVES = 4;
+  constexpr int ROWS = 16, KEYS = 32, LEAST = 32, WAVES = 4;
   constexpr int RB = D * (I8 ? 1 : 2);           // bytes of a key row
   constexpr int CH = RB / 16;                    // its chunks
   constexpr int PER = 1024 / RB;                 // rows of one load
@@ -38,14 +39,23 @@ __global__ void __launch_bounds__(256) paged_tokens_kernel(PagedArgs g) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r16 = lane & 15, h = lane >> 4;
+  SpanWalk<ROWS, KEYS, LEAST> walk(g, blockIdx.x);
+  if (g.slots && tid == 0) {
+    if (blockIdx.x == 0) g.items[0] = (int)gridDim.x;
+    g.items[(1 + blockIdx.x) * kPagedItemWords] = 0;
+  }
+  if (walk.none) return;
+  for (bool again = true; again; again = walk.at < walk.end) {
   PagedUnit u;
-  int items;
-  const bool found = find_unit<ROWS, KEYS, LEAST>(g, blockIdx.x, u, items);
-  if (g.slots && blockIdx.x == 0 && tid == 0) g.items[0] = found ? items : 0;
-  if (!found) return;
-  if (u.parts > 1 && (u.slot >= g.slots || u.item >= g.slots / 2)) return;  // (not with offsets that keep to their description)
-  int low, high, block0, block1;
-  unit_keys<ROWS, KEYS>(g, u, low, high, block0, block1);
+  int x0, x1, low, high, block0, block1;
+  unsigned long long tile_at;
+  walk.next(u, x0, x1, tile_at);
+  u.slot = x0 == 0 && x1 == u.parts ? -1 : 2 * (int)blockIdx.x + (x0 == 0);
+  share_keys<ROWS, KEYS>(g, u, x0, x1, low, high, block0, block1);
+  if (x0 == 0 && x1 < u.parts && tid == 0) {
+    const int last = (int)walk.owner(tile_at + u.parts - 1);
+    put_item(g, u, (int)blockIdx.x, last - (int)blockIdx.x + 1, u.slot, 2 * ((int)blockIdx.x + 1), 2);
+  }
 
   // this lane's row
   const int m = u.tile * ROWS + r16, rows = u.seq.n * g.group;
@@ -209,8 +219,12 @@ __global__ void __launch_bounds__(256) paged_tokens_kernel(PagedArgs g) {
     float top = ref;
 #pragma unroll
     for (int e = 0; e < 4; ++e) top = fmaxf(fmaxf(top, s[0][e]), s[1][e]);
-    top = fmaxf(top, __shfl_xor(top, 16, 64));
-    top = fmaxf(top, __shfl_xor(top, 32, 64));
+    {  // of the row's four quarters
+      const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+      top = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+      const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+      top = fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+    }
     if (__any(top > ref)) {
       const float back = __builtin_amdgcn_exp2f(ref - top);
       sum *= back;
@@ -299,32 +313,34 @@ __global__ void __launch_bounds__(256) paged_tokens_kernel(PagedArgs g) {
     mine_stat[i] = make_float2(top, total);
     odd |= not_finite(acc[i].x) | not_finite(acc[i].y) | not_finite(acc[i].z) | not_finite(acc[i].w);
   }
+  bool careful = false;
   if (!I8) {
     if (__any(odd) && lane == 0) poisoned = 1;
     __syncthreads();
-    if (poisoned) {
-      if (u.parts > 1 && u.part == 0 && tid == 0) put_item(g, u);
-      for (int row = wave; row < ROWS; row += WAVES)
-        if (u.tile * ROWS + row < rows) careful_row<ROWS, D>(g, u, u.tile * ROWS + row, block0 * KEYS, block1 * KEYS);
-      return;
+    careful = poisoned;
+  }
+  if (careful) {
+    for (int row = wave; row < ROWS; row += WAVES)
+      if (u.tile * ROWS + row < rows) careful_row<ROWS, D>(g, u, u.tile * ROWS + row, block0 * KEYS, block1 * KEYS);
+  } else {
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+      const int at = i * 256 + tid, row = at / (D / 4), c = at % (D / 4);
+      const int mm = u.tile * ROWS + row;
+      if (mm >= rows) continue;
+      if (u.slot >= 0) {
+        const long long to = (long long)u.slot * ROWS + row;
+        *(float4*)(g.part + to * D + c * 4) = acc[i];
+        if (c == 0) g.stat[to] = mine_stat[i];
+        continue;
+      }
+      const int tok = mm / g.group;
+      const float inv = u.seq.length - u.seq.n + tok < 0 ? 0.f : 1.0f / mine_stat[i].y;
+      u16* o = g.o + ((long long)(u.seq.first + tok) * g.heads + u.head * g.group + mm - tok * g.group) * D + c * 4;
+      *(uint2*)o = make_uint2(pack_bf16x2(acc[i].x * inv, acc[i].y * inv), pack_bf16x2(acc[i].z * inv, acc[i].w * inv));
     }
   }
-  if (u.parts > 1 && u.part == 0 && tid == 0) put_item(g, u);
-#pragma unroll
-  for (int i = 0; i < PIECES; ++i) {
-    const int at = i * 256 + tid, row = at / (D / 4), c = at % (D / 4);
-    const int mm = u.tile * ROWS + row;
-    if (mm >= rows) continue;
-    if (u.parts > 1) {
-      const long long to = (long long)u.slot * ROWS + row;
-      *(float4*)(g.part + to * D + c * 4) = acc[i];
-      if (c == 0) g.stat[to] = mine_stat[i];
-      continue;
-    }
-    const int tok = mm / g.group;
-    const float inv = u.seq.length - u.seq.n + tok < 0 ? 0.f : 1.0f / mine_stat[i].y;
-    u16* o = g.o + ((long long)(u.seq.first + tok) * g.heads + u.head * g.group + mm - tok * g.group) * D + c * 4;
-    *(uint2*)o = make_uint2(pack_bf16x2(acc[i].x * inv, acc[i].y * inv), pack_bf16x2(acc[i].z * inv, acc[i].w * inv));
+  __syncthreads();  // (the ring is filled again)
   }
 }
 

@@ -198,28 +198,49 @@ def _f32(x):
     return ctypes.c_float(x).value
 
 
-def _units(p, sizes, group, kv_heads, window, width_keys, block_keys, target, least):
-    """(units, slots, cut tiles) that the kernels make of a batch, as they work them out: totals in f32."""
-    work = []
-    total = 0.0
+def _tiles(p, sizes, group, window, width_keys, block_keys):
     for old, n in sizes:
         tiles = -(-n * group // p.rows)
         keys = min(old + n, width_keys)
         if window and window + p.rows < keys:
             keys = window + p.rows
-        blocks = -(-keys // block_keys) if tiles else 0
-        work.append((tiles, blocks))
+        yield tiles, -(-keys // block_keys) if tiles else 0
+
+
+def _check_parts(p, sizes, group, kv_heads, window, width_keys, target):
+    """The units that the chunks' kernel makes of a batch, as it works them out: totals in f32."""
+    work = list(_tiles(p, sizes, group, window, width_keys, 64))
+    total = 0.0
+    for tiles, blocks in work:
         total = _f32(total + _f32(tiles * blocks))
-    most = 1 << 30
-    if p.parts:
-        most = min(max(least, math.ceil(_f32(_f32(total * kv_heads) / target)) + 1), 1 << 30)
+    most = min(max(4, math.ceil(_f32(_f32(total * kv_heads) / target)) + 1), 1 << 30) if p.parts else 1 << 30
     units = slots = cut = 0
     for tiles, blocks in work:
-        parts = -(-blocks // most) if blocks > most else 1
+        parts = max(1, (blocks + most // 2) // most)
         units += tiles * parts
         if parts > 1:
             slots, cut = slots + tiles * parts, cut + tiles
-    return units * kv_heads, slots * kv_heads, cut * kv_heads
+    assert units * kv_heads <= p.grid and slots * kv_heads <= p.slots and cut * kv_heads <= target
+    return slots > 0
+
+
+def _check_spans(p, sizes, group, kv_heads, window, width_keys, target):
+    """The spans of the tokens' kernel: every block has a workgroup, every part a slot, and every cut tile is found by its first."""
+    ends, at = [], 0
+    for tiles, blocks in _tiles(p, sizes, group, window, width_keys, 32):
+        blocks = (max(1, -(-blocks // 32)) * 32 if p.parts else 1) if tiles else 0
+        for _ in range(tiles * kv_heads):
+            ends.append((at, at + blocks))
+            at += blocks
+    per = max(32, -(-at // target)) if p.parts else 1
+    assert -(-at // per) <= p.grid
+    begun = set()
+    for first, end in ends:
+        a, b = first // per, (end - 1) // per
+        if a != b:
+            assert p.parts and a not in begun and 2 * b + 1 < p.slots
+            begun.add(a)
+    return bool(begun)
 
 
 def test_grid_and_workspace_hold_every_batch():
@@ -237,16 +258,15 @@ def test_grid_and_workspace_hold_every_batch():
         width = -(-max(o + n for o, n in sizes) // page) + rng.randint(0, 3)
         window = rng.choice((0, 0, 1, 100, 5000))
         D = rng.choice((64, 128))
-        if not 0 < rows * group * kv_heads < 1 << 26:
+        if not 0 < rows * group * kv_heads < 1 << 20:
             continue
         p = nb.paged_attention_plan(rows, S, width, group * kv_heads, kv_heads, page, D, rng.choice((nb.BF16, nb.I8)), window)
-        member = {0: (32, (p.slots - 8) // 2, 8), 1: (64, (p.slots - 8) // 2, 4)}[p.kernel]
-        units, slots, cut = _units(p, sizes, group, kv_heads, window, width * page, *member)
-        assert units <= p.grid, (sizes, p)
+        target = (p.slots - 8) // 2 if p.parts else 0
+        cut = (_check_spans, _check_parts)[p.kernel](p, sizes, group, kv_heads, window, width * page, target)
         if p.parts:
-            assert slots <= p.slots and cut <= p.slots // 2 and min(p.rows, max(n for _, n in sizes) * group) <= p.join_rows and p.join_grid
-            assert p.workspace_bytes >= p.slots * p.rows * (D * 4 + 8) + (1 + cut) * 32
+            assert p.join_grid[0] and 1 <= p.join_grid[1] <= p.rows
+            assert p.workspace_bytes >= p.slots * p.rows * (D * 4 + 8) + (1 + target) * 48
         else:
-            assert slots == 0 and p.workspace_bytes == 0
-        seen.add((p.kernel, p.parts, slots > 0))
-    assert (0, 1, True) in seen and (0, 0, False) in seen
+            assert not cut and p.workspace_bytes == 0
+        seen.add((p.kernel, p.parts, cut))
+    assert seen >= {(0, 1, True), (0, 1, False), (0, 0, False), (1, 1, True), (1, 1, False), (1, 0, False)}
