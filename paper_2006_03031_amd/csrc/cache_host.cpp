@@ -59,16 +59,19 @@ SequencesArgs sequences_args(const nimble_sequences& s) {
 }
 
 // ------------------------------------------------------------------------------------------------ attention
-// Rows of a tile, keys of a block, the least number of blocks that is worth a part of its own.
+// Rows of a tile, and the keys up to which nothing is cut: the second launch costs more than a longer walk saves.
 struct PagedMember {
-  int rows, block_keys, least_blocks;
+  int rows, least_keys;
 };
-static const PagedMember kPagedMembers[NIMBLE_PAGED_COUNT] = {{16, 32, 32}, {128, 64, 4}};
+static const PagedMember kPagedMembers[NIMBLE_PAGED_COUNT] = {{16, 1024}, {128, 256}};
+constexpr int64_t kStepKeys = 256;   // of the tokens' spans
 // Workgroups that a compute unit holds at once, by their LDS (tokens) and registers: as many parts as fill the chip once are aimed at.
 static int paged_workgroups_per_cu(int kernel, int64_t D, int dtype) {
   if (kernel == NIMBLE_PAGED_CHUNKS) return 2;
-  return (D == 128 ? 1 : 2) * (dtype == NIMBLE_I8 ? 2 : 1);
+  return D == 64 && dtype == NIMBLE_I8 ? 2 : 1;
 }
+// Waves of a workgroup: eight, or four where the LDS holds no more.
+static int paged_waves(int kernel, int64_t D, int dtype) { return kernel == NIMBLE_PAGED_CHUNKS || (D == 128 && dtype == NIMBLE_BF16) ? 4 : 8; }
 
 static int plan_paged(int64_t rows, int64_t count, int64_t width, int64_t heads, int64_t kv_heads, int64_t page, int64_t D, int dtype,
                       int64_t window, nimble_paged_plan* p) {
@@ -86,12 +89,14 @@ static int plan_paged(int64_t rows, int64_t count, int64_t width, int64_t heads,
   int64_t keys = width * page;
   if (window > 0 && window + m.rows < keys) keys = window + m.rows;
   out.rows = m.rows;
-  out.block = 256;
+  out.block = 64u * (unsigned)paged_waves(out.kernel, D, dtype);
   // Nothing is cut where tiles alone fill the chip twice and none can take long: the second launch is saved.
   const int64_t target = (int64_t)kComputeUnits * paged_workgroups_per_cu(out.kernel, D, dtype);
   const bool plenty = rows * group / m.rows * kv_heads >= 2 * target && keys <= 1024;
-  out.parts = keys > (int64_t)m.block_keys * m.least_blocks && !plenty;
+  out.parts = keys > m.least_keys && !plenty;
   if (tiles * kv_heads > kMostPagedGrid) return fail(NIMBLE_ERR_ARG, "more than 2^23 tiles");
+  if (tiles * kv_heads > ((1ll << 31) - 1) / (ceil_div(keys, kStepKeys) + 1))
+    return fail(NIMBLE_ERR_ARG, "%lld tiles of %lld keys", (long long)(tiles * kv_heads), (long long)keys);
   if (out.parts) {
     // tokens: a span a workgroup, with two parts; chunks: a unit a workgroup, tiles and as many more as the cuts make
     const bool spans = out.kernel == NIMBLE_PAGED_TOKENS;

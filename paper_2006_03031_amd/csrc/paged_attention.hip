@@ -21,8 +21,9 @@ static void launch_paged(const PagedArgs& g, const nimble_paged_plan& p, bool in
     else launch(paged_chunks_kernel<D, false>);
     join(paged_join_kernel<128, D>);
   } else {
-    if (int8) launch(paged_tokens_kernel<D, true>);
-    else launch(paged_tokens_kernel<D, false>);
+    constexpr int kWide = D == 128 ? 4 : 8;  // (of bf16; as in plan_paged)
+    if (int8) launch(paged_tokens_kernel<D, true, 8>);
+    else launch(paged_tokens_kernel<D, false, kWide>);
     join(paged_join_kernel<16, D>);
   }
 }
@@ -62,6 +63,7 @@ int nimble_paged_attention_dyn(const void* q, int64_t q_stride, const nimble_cac
   g.window = (int)(window < kMostPositions ? window : 0);  // (2^30 and beyond: all)
   g.a2 = alpha * 1.4426950408889634f;
   if (!std::isfinite(g.a2)) return fail(NIMBLE_ERR_ARG, "paged_attention: alpha = %g is too large", (double)alpha);
+  g.once = p.kernel == NIMBLE_PAGED_TOKENS && seqs->rows * g.group <= p.rows * seqs->count;
   if (p.parts) {
     g.slots = (int)p.slots;
     g.target_units = (int)(p.slots - 8) / 2;  // (see plan_paged)

@@ -20,6 +20,7 @@ struct PagedArgs {
   float2* stat;        // [slots][rows] their largest score (base 2) and sum of probabilities
   int* items;          // [0]: tiles that may have been cut, then kPagedItemWords each, from the second entry on
   int slots, target_units;
+  int once;            // keys and values are loaded past the caches
 };
 
 constexpr float kNothing = -3.0e38f;  // the reference of a row that has seen no key yet
@@ -162,64 +163,56 @@ __device__ __forceinline__ void unit_keys(const PagedArgs& g, const PagedUnit& u
 // number of them: the blocks of all tiles in a row, one sequence after the other, cut into spans of equal length, one a workgroup.  A span may
 // end one tile, hold several and begin another.  A workgroup leaves at most two parts: of the tile that another one began (slot 2 w) and of
 // the one that it begins (slot 2 w + 1); the second launch finds a cut tile by the workgroup that began it.
-//   A tile counts as many blocks as the longest of its sequence, rounded up to LEAST, so that spans of that length, where there is little to do,
-// do not cross tiles; a share of them is that share of the blocks that it has.
-//   (64 sequences of up to 8192 keys, uneven, as tiles cut into equal parts of at most a 512th of all: 144 us, 1.5 rounds of workgroups; in
-// spans SPAN_US.)
+//   Lengths are counted in steps of STEP blocks, a tile as many as the longest of its sequence; a share of them is that share of the blocks that
+// the tile has.  (64 sequences of up to 8192 keys, uneven, as tiles cut into equal parts of at most a 512th of all: 144 us, 1.5 rounds
+// of workgroups; in spans 121.)
 // ---------------------------------------------------------------------------
-template <int ROWS, int KEYS, int LEAST>
+template <int ROWS, int KEYS, int STEP>
 struct SpanWalk {
-  typedef unsigned long long u64;
   const PagedArgs& g;
   int base;                // this lane's sequence is base + lane
   Sequence q;
-  int tiles, blocks;
-  u64 ahead, upto;         // blocks of the sequences ahead of these 64, and up to this lane's with them
-  u64 at, end, per;        // what is left of the span, and its length
+  int tiles, steps;
+  unsigned ahead, upto;    // steps of the sequences ahead of these 64, and up to this lane's with them
+  unsigned at, end, per;   // what is left of the span, and its length
   bool none;               // the span is empty
 
-  static __device__ __forceinline__ u64 lane_value(u64 x, int l) {
-    return ((u64)(unsigned)__builtin_amdgcn_readlane((int)(x >> 32), l) << 32) | (unsigned)__builtin_amdgcn_readlane((int)(unsigned)x, l);
-  }
-  __device__ __forceinline__ u64 look(int s) {
+  static __device__ __forceinline__ unsigned lane_value(unsigned x, int l) { return (unsigned)__builtin_amdgcn_readlane((int)x, l); }
+  __device__ __forceinline__ unsigned look(int s) {
     q = Sequence{0, 0, 0};
-    tiles = blocks = 0;
+    tiles = steps = 0;
     if (s >= g.seqs.count) return 0;
     q = sequence_of(g.seqs, s, g.cache.page_shift);
+    int blocks;
     tile_work<ROWS, KEYS>(g, q, tiles, blocks);
-    blocks = g.slots ? (blocks + LEAST - 1) / LEAST * LEAST : blocks > 0;  // (without a workspace a tile counts once, and so does a span)
-    if (blocks == 0 && tiles) blocks = g.slots ? LEAST : 1;                // rows that see nothing
-    return (u64)tiles * (unsigned)blocks * (unsigned)g.cache.kv_heads;
+    steps = (blocks + STEP - 1) / STEP;
+    if (steps == 0 || !g.slots) steps = tiles > 0;  // rows that see nothing; without a workspace a tile is a step and so is a span
+    return (unsigned)tiles * (unsigned)steps * (unsigned)g.cache.kv_heads;  // (all of them fewer than 2^31: checked by the host)
   }
   __device__ __forceinline__ void load(int b) {
-    const int lane = threadIdx.x & 63;
     base = b;
-    upto = ahead + wave_scan(look(b + lane));
+    upto = ahead + wave_scan(look(b + (threadIdx.x & 63)));
   }
   __device__ __forceinline__ SpanWalk(const PagedArgs& args, unsigned w) : g(args) {
-    const int lane = threadIdx.x & 63;
-    u64 total = 0;
+    unsigned total = 0;
     ahead = 0;
     if (g.seqs.count > 64) {
-      for (int b = 0; b < g.seqs.count; b += 64) total += look(b + lane);
+      for (int b = 0; b < g.seqs.count; b += 64) total += look(b + (threadIdx.x & 63));
       total = lane_value(wave_scan(total), 63);
       load(0);
     } else {
       load(0);
       total = lane_value(upto, 63);
     }
-    per = 1;
-    if (g.slots) {
-      const unsigned spans = (unsigned)g.target_units;
-      per = total >> 31 ? (total + spans - 1) / spans : ((unsigned)total + spans - 1) / spans;
-      if (per < LEAST) per = LEAST;
-    }
-    at = (u64)w * per;
-    end = at + per < total ? at + per : total;
-    none = at >= total;
+    per = g.slots ? (total + (unsigned)g.target_units - 1) / (unsigned)g.target_units : 1;
+    if (per == 0) per = 1;
+    const unsigned long long from = (unsigned long long)w * per;
+    none = from >= total;
+    at = none ? total : (unsigned)from;
+    end = total - at < per ? total : at + per;
   }
-  // The tile that the rest of the span begins with: x0 .. x1 - 1 of its u.parts = blocks.  tile_at: where the tile begins.
-  __device__ __forceinline__ void next(PagedUnit& u, int& x0, int& x1, u64& tile_at) {
+  // The tile that the rest of the span begins with: steps x0 .. x1 - 1 of its u.parts.  tile_at: where the tile begins.
+  __device__ __forceinline__ void next(PagedUnit& u, unsigned& x0, unsigned& x1, unsigned& tile_at) {
     while (at >= lane_value(upto, 63)) {
       ahead = lane_value(upto, 63);
       load(base + 64);
@@ -231,36 +224,34 @@ struct SpanWalk {
     u.seq.n = of(q.n);
     u.seq.length = of(q.length);
     u.tiles = of(tiles);
-    u.parts = of(blocks);
-    const u64 first = lane_value(upto, l) - (u64)u.tiles * (unsigned)u.parts * (unsigned)g.cache.kv_heads, in = at - first;
-    const u64 which = in >> 32 ? in / (unsigned)u.parts : (unsigned)in / (unsigned)u.parts;
+    u.parts = of(steps);
+    const unsigned G = (unsigned)g.cache.kv_heads;
+    const unsigned first = lane_value(upto, l) - (unsigned)u.tiles * (unsigned)u.parts * G;
+    const unsigned which = (at - first) / (unsigned)u.parts;
     tile_at = first + which * (unsigned)u.parts;
-    u.tile = (int)((unsigned)which / (unsigned)g.cache.kv_heads);   // (tiles * heads are fewer than 2^23)
-    u.head = (int)((unsigned)which - (unsigned)u.tile * (unsigned)g.cache.kv_heads);
-    x0 = (int)(at - tile_at);
-    x1 = end - tile_at < (u64)u.parts ? (int)(end - tile_at) : u.parts;
+    u.tile = (int)(which / G);
+    u.head = (int)(which - (unsigned)u.tile * G);
+    x0 = at - tile_at;
+    x1 = end - tile_at < (unsigned)u.parts ? end - tile_at : (unsigned)u.parts;
     at = tile_at + x1;
   }
-  // The workgroup whose span holds block x.
-  __device__ __forceinline__ unsigned owner(u64 x) const { return (unsigned)(x >> 32 || per >> 32 ? x / per : (unsigned)x / (unsigned)per); }
+  // The workgroup whose span holds step x.
+  __device__ __forceinline__ unsigned owner(unsigned x) const { return x / per; }
 };
 
 // The blocks of a span's share of a tile.
 template <int ROWS, int KEYS>
-__device__ __forceinline__ void share_keys(const PagedArgs& g, const PagedUnit& u, int x0, int x1, int& low, int& high, int& block0, int& block1) {
+__device__ __forceinline__ void share_keys(const PagedArgs& g, const PagedUnit& u, unsigned x0, unsigned x1, int& low, int& high, int& block0, int& block1) {
   PagedUnit all = u;
   all.part = 0;
   all.parts = 1;
   unit_keys<ROWS, KEYS>(g, all, low, high, block0, block1);
-  const unsigned nb = block1 - block0;
-  auto share = [&](int x) {
-    if (x == u.parts) return (int)nb;
-    const unsigned long long t = (unsigned long long)nb * (unsigned)x;
-    return (int)(t >> 32 ? t / (unsigned)u.parts : (unsigned)t / (unsigned)u.parts);
-  };
+  if (x0 == 0 && x1 == (unsigned)u.parts) return;
+  const unsigned nb = block1 - block0;                      // below 2^26, and steps below 2^23
+  const unsigned q = nb / (unsigned)u.parts, r = nb - q * (unsigned)u.parts;   // (the first r steps have one block more)
   const int b0 = block0;
-  block0 = __builtin_amdgcn_readfirstlane(b0 + share(x0));
-  block1 = __builtin_amdgcn_readfirstlane(b0 + share(x1));
+  block0 = __builtin_amdgcn_readfirstlane(b0 + (int)(x0 * q + (x0 < r ? x0 : r)));
+  block1 = __builtin_amdgcn_readfirstlane(b0 + (int)(x1 * q + (x1 < r ? x1 : r)));
 }
 
 // A pointer that is the same in all lanes, in scalar registers.

@@ -6,7 +6,7 @@
 namespace nimble {
 
 // ---------------------------------------------------------------------------
-// Few rows: 16 of a (sequence, head) per workgroup, four waves that each take every fourth block of 32 keys and meet at the end.
+// Few rows: 16 of a (sequence, head) per workgroup, WAVES waves that each take every WAVES-th block of 32 keys and meet at the end.
 //   scores:  MFMA 16x16x32, 16 keys on the A side, the 16 rows on the B side: lane (r, h) = (lane & 15, lane >> 4) holds, for row r, keys
 //            16 t + 4 h + (0..3) of tile t = 0, 1.
 //   P.V:     the 8 k slots of h are defined as the keys it holds, 4 of either tile, so that P stays in its lane; the values come out of
@@ -19,9 +19,9 @@ namespace nimble {
 //            page, whose number is a scalar.  Chunk c of row r sits at c ^ swizzle(r).  Keys outside of what the tile sees repeat the
 //            nearest one that it does.
 // ---------------------------------------------------------------------------
-template <int D, bool I8>
-__global__ void __launch_bounds__(256) paged_tokens_kernel(PagedArgs g) {
-  constexpr int ROWS = 16, KEYS = 32, LEAST = 32, WAVES = 4;
+template <int D, bool I8, int WAVES>
+__global__ void __launch_bounds__(WAVES * 64) paged_tokens_kernel(PagedArgs g) {
+  constexpr int ROWS = 16, KEYS = 32, STEP = 8, T = WAVES * 64;
   constexpr int RB = D * (I8 ? 1 : 2);           // bytes of a key row
   constexpr int CH = RB / 16;                    // its chunks
   constexpr int PER = 1024 / RB;                 // rows of one load
@@ -39,7 +39,7 @@ __global__ void __launch_bounds__(256) paged_tokens_kernel(PagedArgs g) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r16 = lane & 15, h = lane >> 4;
-  SpanWalk<ROWS, KEYS, LEAST> walk(g, blockIdx.x);
+  SpanWalk<ROWS, KEYS, STEP> walk(g, blockIdx.x);
   if (g.slots && tid == 0) {
     if (blockIdx.x == 0) g.items[0] = (int)gridDim.x;
     g.items[(1 + blockIdx.x) * kPagedItemWords] = 0;
@@ -47,12 +47,12 @@ __global__ void __launch_bounds__(256) paged_tokens_kernel(PagedArgs g) {
   if (walk.none) return;
   for (bool again = true; again; again = walk.at < walk.end) {
   PagedUnit u;
-  int x0, x1, low, high, block0, block1;
-  unsigned long long tile_at;
+  int low, high, block0, block1;
+  unsigned x0, x1, tile_at;
   walk.next(u, x0, x1, tile_at);
-  u.slot = x0 == 0 && x1 == u.parts ? -1 : 2 * (int)blockIdx.x + (x0 == 0);
+  u.slot = x0 == 0 && x1 == (unsigned)u.parts ? -1 : 2 * (int)blockIdx.x + (x0 == 0);
   share_keys<ROWS, KEYS>(g, u, x0, x1, low, high, block0, block1);
-  if (x0 == 0 && x1 < u.parts && tid == 0) {
+  if (x0 == 0 && x1 < (unsigned)u.parts && tid == 0) {
     const int last = (int)walk.owner(tile_at + u.parts - 1);
     put_item(g, u, (int)blockIdx.x, last - (int)blockIdx.x + 1, u.slot, 2 * ((int)blockIdx.x + 1), 2);
   }
@@ -83,13 +83,21 @@ __global__ void __launch_bounds__(256) paged_tokens_kernel(PagedArgs g) {
     v_off[n] = row * RB + (load_chunk_ ^ v_swizzle(row)) * 16;
   }
   const uint32_t ring = __builtin_amdgcn_readfirstlane(lds_addr_of(lds) + wave * S * SLOT);
-  // (through the scalar cache: a vector load here would be waited for, and with it all that are under way)
-  typedef const __attribute__((address_space(4))) int* ScalarTable;
-  const ScalarTable table = (ScalarTable)(uintptr_t)(g.seqs.pages + (long long)u.s * g.seqs.width);
+  const int* table = g.seqs.pages + (long long)u.s * g.seqs.width;
   const int slot_mask = (1 << g.cache.page_shift) - 1;
-  // the first of the 16 keys' rows, counted in rows of the cache
-  auto group_row = [&](int key) {
-    unsigned page = (unsigned)table[key >> g.cache.page_shift];
+  const int k0 = low & ~15, k1 = high & ~15;
+  auto held_to = [&](int key) { return key < k0 ? k0 : key > k1 ? k1 : key; };
+  // The pages of the wave's next 64 blocks: lane l holds that of keys 16 (l & 1) .. + 15 of its blocks l / 2 and 32 + l / 2.  (Looked up block by block
+  // through the scalar cache a block of 777 keys of 64 took 0.77 us, with the pages at hand AT_HAND.)
+  int pages0 = 0, pages1 = 0;
+  auto page_at = [&](int i) { return table[held_to((block0 + wave + i * WAVES) * KEYS + (lane & 1) * 16) >> g.cache.page_shift]; };
+  auto look_up = [&](int first) {  // from the wave's block `first` on
+    pages0 = page_at(first + (lane >> 1));
+    pages1 = page_at(first + 32 + (lane >> 1));
+  };
+  // the first of 16 keys' rows, counted in rows of the cache
+  auto group_row = [&](int i, int t, int key) {
+    unsigned page = (unsigned)__builtin_amdgcn_readlane(i & 32 ? pages1 : pages0, (i & 31) * 2 + t);
     page = page < g.cache.pages ? page : g.cache.pages - 1;
     return (((long long)page * g.cache.kv_heads + u.head) << g.cache.page_shift) + (key & slot_mask);
   };
@@ -98,14 +106,13 @@ __global__ void __launch_bounds__(256) paged_tokens_kernel(PagedArgs g) {
     long long row[2];
     int lo[2], hi[2];
   };
-  auto place_of = [&](int block) {
+  auto place_of = [&](int i) {  // of the wave's block i
+    if (i && (i & 63) == 0) look_up(i);
     Place p;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      int key = block * KEYS + t * 16;
-      const int k0 = low & ~15, k1 = high & ~15;
-      key = key < k0 ? k0 : key > k1 ? k1 : key;
-      p.row[t] = group_row(key);
+      const int key = held_to((block0 + wave + i * WAVES) * KEYS + t * 16);
+      p.row[t] = group_row(i, t, key);
       p.lo[t] = low - key > 0 ? low - key : 0;
       p.hi[t] = high - key < 15 ? high - key : 15;
     }
@@ -117,15 +124,18 @@ __global__ void __launch_bounds__(256) paged_tokens_kernel(PagedArgs g) {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       const unsigned char* from = uniform_pointer((V ? g.cache.v : g.cache.k) + p.row[t] * RB);
+      const bool whole = p.lo[t] == 0 && p.hi[t] == 15;
 #pragma unroll
       for (int n = 0; n < LOADS; ++n) {
         uint32_t off = V ? v_off[n] : k_off[n];
-        if (p.lo[t] > 0 || p.hi[t] < 15) {  // uniform
+        if (!whole) {
           const int row = n * PER + load_row;
           const int there = row < p.lo[t] ? p.lo[t] : row > p.hi[t] ? p.hi[t] : row;
           off += (there - row) * RB;
         }
-        dma16_so(off, from, to + V * TILE + (t * LOADS + n) * 1024);
+        const uint32_t at = to + V * TILE + (t * LOADS + n) * 1024;
+        if (g.once) dma16_so_once(off, from, at);
+        else dma16_so(off, from, at);
       }
     }
     if (I8 && !V) {  // lane -> scale of a key (0..31) or a value (32..63)
@@ -142,18 +152,19 @@ __global__ void __launch_bounds__(256) paged_tokens_kernel(PagedArgs g) {
   f32x4 oacc[D / 16];
 #pragma unroll
   for (int i = 0; i < D / 16; ++i) oacc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float ref = kNothing, sum = 0.f;  // base 2; this lane's share of the sum
+  float ref = kNothing, sum = 0.f;  // in units of the scores; this lane's share of the sum
 
   const int mine = block1 - block0 > wave ? (block1 - block0 - wave + WAVES - 1) / WAVES : 0;
   // Three halves of a block are under way beside the one in work: the values of block i + 1 are asked for ahead of block i's scores, the keys of
   // block i + 2 behind them, when those of block i have been read.
   Place next{};
   if (mine > 0) {
-    const Place p = place_of(block0 + wave);
+    look_up(0);
+    const Place p = place_of(0);
     issue(K_TILE{}, p, 0);
     issue(V_TILE{}, p, 0);
     if (mine > 1) {
-      next = place_of(block0 + wave + WAVES);
+      next = place_of(1);
       issue(K_TILE{}, next, 1);
     }
   }
@@ -185,19 +196,16 @@ __global__ void __launch_bounds__(256) paged_tokens_kernel(PagedArgs g) {
       }
       if (I8) {
         const float4 sc = *(const float4*)(ks + 2 * TILE + (t * 16 + h * 4) * 4);
-        s[t][0] *= sc.x * g.a2, s[t][1] *= sc.y * g.a2, s[t][2] *= sc.z * g.a2, s[t][3] *= sc.w * g.a2;
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s[t][e] *= g.a2;
+        s[t][0] *= sc.x, s[t][1] *= sc.y, s[t][2] *= sc.z, s[t][3] *= sc.w;
       }
     }
-    float4 v_scale[2];
+    f32x4 v_scale[2];
     if (I8) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t) v_scale[t] = *(const float4*)(ks + 2 * TILE + 128 + (t * 16 + h * 4) * 4);
+      for (int t = 0; t < 2; ++t) v_scale[t] = *(const f32x4*)(ks + 2 * TILE + 128 + (t * 16 + h * 4) * 4);
     }
     if (i + 2 < mine) {
-      next = place_of(block + 2 * WAVES);
+      next = place_of(i + 2);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the keys and the scales have been read)
       issue(K_TILE{}, next, slot);
     }
@@ -205,15 +213,15 @@ __global__ void __launch_bounds__(256) paged_tokens_kernel(PagedArgs g) {
     // (a block that every row of the tile sees whole needs no mask; rows past the last see nothing and are not stored)
     const int least = u.seq.length - u.seq.n + u.tile * ROWS / g.group;
     const bool edge = key0 + KEYS - 1 > least || (g.window > 0 && key0 <= high - g.window);
-    bool seen[2][4];
     if (edge) {
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int key = key0 + t * 16 + h * 4 + e;
-          seen[t][e] = key <= pos && key >= first;
-          if (!seen[t][e]) s[t][e] = -INFINITY;
+          if (key <= pos && key >= first) continue;
+          s[t][e] = -INFINITY;
+          if (I8) v_scale[t][e] = 0.f;  // (it may be NaN)
         }
     }
     float top = ref;
@@ -226,28 +234,21 @@ __global__ void __launch_bounds__(256) paged_tokens_kernel(PagedArgs g) {
       top = fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
     }
     if (__any(top > ref)) {
-      const float back = __builtin_amdgcn_exp2f(ref - top);
+      const float back = __builtin_amdgcn_exp2f((ref - top) * g.a2);
       sum *= back;
 #pragma unroll
       for (int x = 0; x < D / 16; ++x) oacc[x] *= back;
       ref = top;
     }
+    const float nm2 = ref > kNothing ? -ref * g.a2 : 0.f;  // (a row that has seen nothing: its scores are minus infinity)
     float p[2][4];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        p[t][e] = __builtin_amdgcn_exp2f(s[t][e] - ref);
+        p[t][e] = __builtin_amdgcn_exp2f(fmaf(s[t][e], g.a2, nm2));
         sum += p[t][e];
-      }
-      if (I8) {
-        const float4 sc = v_scale[t];
-        p[t][0] *= sc.x, p[t][1] *= sc.y, p[t][2] *= sc.z, p[t][3] *= sc.w;
-        if (edge) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (!seen[t][e]) p[t][e] = 0.f;  // (its scale may be NaN)
-        }
+        if (I8) p[t][e] *= v_scale[t][e];
       }
     }
     const bf16x8 pf = as_bf16x8(make_uint4(pack_bf16x2(p[0][0], p[0][1]), pack_bf16x2(p[0][2], p[0][3]), pack_bf16x2(p[1][0], p[1][1]),
@@ -285,18 +286,18 @@ __global__ void __launch_bounds__(256) paged_tokens_kernel(PagedArgs g) {
   float* sums = (float*)lds;
   if (tid == 0) poisoned = 0;
   __syncthreads();
-  if (h == 0) stat[wave][r16] = make_float2(ref, sum);
+  if (h == 0) stat[wave][r16] = make_float2(ref > kNothing ? ref * g.a2 : kNothing, sum);
 #pragma unroll
   for (int x = 0; x < D / 16; ++x)
     *(f32x4*)(sums + (wave * ROWS + r16) * D + (((x * 4 + h) ^ r16) * 4)) = oacc[x];  // (16-byte pieces spread over the banks)
   __syncthreads();
-  constexpr int PIECES = ROWS * D / 4 / 256;
+  constexpr int PIECES = (ROWS * D / 4 + T - 1) / T;
   float4 acc[PIECES];
   float2 mine_stat[PIECES];
   bool odd = false;
 #pragma unroll
   for (int i = 0; i < PIECES; ++i) {
-    const int at = i * 256 + tid, row = at / (D / 4), c = at % (D / 4);
+    const int at = i * T + tid, row = at / (D / 4) % ROWS, c = at % (D / 4);
     float top = kNothing;
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) top = fmaxf(top, stat[w][row].x);
@@ -325,9 +326,9 @@ __global__ void __launch_bounds__(256) paged_tokens_kernel(PagedArgs g) {
   } else {
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
-      const int at = i * 256 + tid, row = at / (D / 4), c = at % (D / 4);
+      const int at = i * T + tid, row = at / (D / 4), c = at % (D / 4);
       const int mm = u.tile * ROWS + row;
-      if (mm >= rows) continue;
+      if (row >= ROWS || mm >= rows) continue;
       if (u.slot >= 0) {
         const long long to = (long long)u.slot * ROWS + row;
         *(float4*)(g.part + to * D + c * 4) = acc[i];

@@ -225,14 +225,15 @@ def _check_parts(p, sizes, group, kv_heads, window, width_keys, target):
 
 
 def _check_spans(p, sizes, group, kv_heads, window, width_keys, target):
-    """The spans of the tokens' kernel: every block has a workgroup, every part a slot, and every cut tile is found by its first."""
+    """The spans of the tokens' kernel: every step has a workgroup, every part a slot, and every cut tile is found by its first."""
     ends, at = [], 0
     for tiles, blocks in _tiles(p, sizes, group, window, width_keys, 32):
-        blocks = (max(1, -(-blocks // 32)) * 32 if p.parts else 1) if tiles else 0
+        steps = (max(1, -(-blocks // 8)) if p.parts else 1) if tiles else 0
         for _ in range(tiles * kv_heads):
-            ends.append((at, at + blocks))
-            at += blocks
-    per = max(32, -(-at // target)) if p.parts else 1
+            ends.append((at, at + steps))
+            at += steps
+    assert at < 1 << 31
+    per = max(1, -(-at // target)) if p.parts else 1
     assert -(-at // per) <= p.grid
     begun = set()
     for first, end in ends:
