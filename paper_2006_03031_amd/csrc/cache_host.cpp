@@ -65,13 +65,18 @@ struct PagedMember {
 };
 static const PagedMember kPagedMembers[NIMBLE_PAGED_COUNT] = {{16, 1024}, {128, 256}};
 constexpr int64_t kStepKeys = 256;   // of the tokens' spans
-// Workgroups that a compute unit holds at once, by their LDS (tokens) and registers: as many parts as fill the chip once are aimed at.
-static int paged_workgroups_per_cu(int kernel, int64_t D, int dtype) {
-  if (kernel == NIMBLE_PAGED_CHUNKS) return 2;
-  return D == 64 && dtype == NIMBLE_I8 ? 2 : 1;
+// Waves of a workgroup, and workgroups that a compute unit holds at once, by their LDS (tokens) and registers: as many parts as fill the chip once
+// are aimed at.  Tokens: four waves where workgroups share a compute unit, so that one loads while another joins its waves' sums and goes over to
+// the next tile (64 tokens over up to 8192 keys in 8 bits, spans of two tiles: eight waves 114 us, twice four 106); eight where tiles are few and short and the
+// walk over one is what takes its time (one token over 777 keys of 64: four 10.4, eight 7.8).  Of bf16 heads of 128 the LDS holds four waves.
+struct PagedWaves {
+  int waves, per_cu;
+};
+static PagedWaves paged_waves(int kernel, int64_t D, int dtype, bool lone) {
+  if (kernel == NIMBLE_PAGED_CHUNKS) return {4, 2};
+  const int four = (D == 128 ? 1 : 2) * (dtype == NIMBLE_I8 ? 2 : 1);
+  return lone && four > 1 ? PagedWaves{8, four / 2} : PagedWaves{4, four};
 }
-// Waves of a workgroup: eight, or four where the LDS holds no more.
-static int paged_waves(int kernel, int64_t D, int dtype) { return kernel == NIMBLE_PAGED_CHUNKS || (D == 128 && dtype == NIMBLE_BF16) ? 4 : 8; }
 
 static int plan_paged(int64_t rows, int64_t count, int64_t width, int64_t heads, int64_t kv_heads, int64_t page, int64_t D, int dtype,
                       int64_t window, nimble_paged_plan* p) {
@@ -89,9 +94,10 @@ static int plan_paged(int64_t rows, int64_t count, int64_t width, int64_t heads,
   int64_t keys = width * page;
   if (window > 0 && window + m.rows < keys) keys = window + m.rows;
   out.rows = m.rows;
-  out.block = 64u * (unsigned)paged_waves(out.kernel, D, dtype);
   // Nothing is cut where tiles alone fill the chip twice and none can take long: the second launch is saved.
-  const int64_t target = (int64_t)kComputeUnits * paged_workgroups_per_cu(out.kernel, D, dtype);
+  const PagedWaves w = paged_waves(out.kernel, D, dtype, keys <= m.least_keys && tiles * kv_heads <= kComputeUnits);
+  const int64_t target = (int64_t)kComputeUnits * w.per_cu;
+  out.block = 64u * (unsigned)w.waves;
   const bool plenty = rows * group / m.rows * kv_heads >= 2 * target && keys <= 1024;
   out.parts = keys > m.least_keys && !plenty;
   if (tiles * kv_heads > kMostPagedGrid) return fail(NIMBLE_ERR_ARG, "more than 2^23 tiles");

@@ -21,9 +21,12 @@ static void launch_paged(const PagedArgs& g, const nimble_paged_plan& p, bool in
     else launch(paged_chunks_kernel<D, false>);
     join(paged_join_kernel<128, D>);
   } else {
-    constexpr int kWide = D == 128 ? 4 : 8;  // (of bf16; as in plan_paged)
-    if (int8) launch(paged_tokens_kernel<D, true, 8>);
-    else launch(paged_tokens_kernel<D, false, kWide>);
+    constexpr int kWide = D == 128 ? 4 : 8;  // (of bf16: what the LDS holds)
+    const bool wide = p.block == 512;
+    if (int8 && wide) launch(paged_tokens_kernel<D, true, 8>);
+    else if (int8) launch(paged_tokens_kernel<D, true, 4>);
+    else if (wide) launch(paged_tokens_kernel<D, false, kWide>);
+    else launch(paged_tokens_kernel<D, false, 4>);
     join(paged_join_kernel<16, D>);
   }
 }
@@ -63,7 +66,11 @@ int nimble_paged_attention_dyn(const void* q, int64_t q_stride, const nimble_cac
   g.window = (int)(window < kMostPositions ? window : 0);  // (2^30 and beyond: all)
   g.a2 = alpha * 1.4426950408889634f;
   if (!std::isfinite(g.a2)) return fail(NIMBLE_ERR_ARG, "paged_attention: alpha = %g is too large", (double)alpha);
-  g.once = p.kernel == NIMBLE_PAGED_TOKENS && seqs->rows * g.group <= p.rows * seqs->count;
+  // Past the caches where each key is read by one workgroup and the page table has room for more than 8 MB: what a layer finds in memory, other
+  // layers' caches having been there in between, comes sooner (32 MB 16.7 -> 15.4 us, 256 MB 56.3 -> 49.8), what it finds in the memory-side
+  // cache, alone over and over, later (128 MB 33.6 -> 33.0, 34.3 -> 37.3, 256 MB 50.3 -> 53); a short sequence of one token 7.8 -> 8.6.
+  g.once = p.kernel == NIMBLE_PAGED_TOKENS && seqs->rows * g.group <= p.rows * seqs->count &&
+           (double)seqs->count * seqs->width * cache->page * cache->kv_heads * cache->D * (cache->dtype == NIMBLE_I8 ? 2 : 4) > 8e6;
   if (p.parts) {
     g.slots = (int)p.slots;
     g.target_units = (int)(p.slots - 8) / 2;  // (see plan_paged)

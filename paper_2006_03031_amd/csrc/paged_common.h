@@ -363,71 +363,72 @@ __global__ void __launch_bounds__(256) paged_join_kernel(PagedArgs g) {
   __shared__ Piece wave_sums[4][64];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int count = g.items[0];
-  for (int i = blockIdx.x; i < count; i += gridDim.x) {
-    const int* item = g.items + (1 + i) * kPagedItemWords;
-    const int parts = item[0], slot = item[1], second = item[2], apart = item[3], tile = item[4], head = item[5];
-    if (parts < 2) continue;
-    const int left = item[7] * g.group - tile * ROWS, rows = left < ROWS ? left : ROWS;
-    const bool together = parts > MANY;
-    const int step = together ? 4 : 1;
-    for (int row = blockIdx.y + (together ? 0 : wave * gridDim.y); row < rows; row += together ? gridDim.y : 4 * gridDim.y) {
-      float top = kNothing, total = 0.f;
-      Piece acc{};
-      auto place = [&](int x) { return (long long)(x ? second + (x - 1) * apart : slot) * ROWS + row; };
-      for (int x0 = together ? wave : 0; x0 < parts; x0 += 64 * step) {
-        const int x = x0 + lane * step;
-        const float2 st = x < parts ? g.stat[place(x)] : make_float2(kNothing, 0.f);
-        const int n = (parts - x0 + step - 1) / step < 64 ? (parts - x0 + step - 1) / step : 64;
-        Piece v[8];
-        auto load = [&](int y0) {
+  // (the grid is as long as the table of tiles can be; an entry is read with the number of entries, not behind it)
+  const int* entry = g.items + (1 + blockIdx.x) * kPagedItemWords;
+  int item[9], count = g.items[0];
 #pragma unroll
-          for (int y = 0; y < 8; ++y) v[y] = *(const Piece*)(g.part + place(x0 + (y0 + y < n ? y0 + y : n - 1) * step) * D + lane * P);
-        };
-        load(0);
-        float next = fmaxf(top, st.x);
+  for (int x = 0; x < 9; ++x) item[x] = entry[x];
+  const int parts = item[0], slot = item[1], second = item[2], apart = item[3], tile = item[4], head = item[5];
+  if ((int)blockIdx.x >= count || parts < 2) return;
+  const int left = item[7] * g.group - tile * ROWS, rows = left < ROWS ? left : ROWS;
+  const bool together = parts > MANY;
+  const int step = together ? 4 : 1;
+  for (int row = blockIdx.y + (together ? 0 : wave * gridDim.y); row < rows; row += together ? gridDim.y : 4 * gridDim.y) {
+    float top = kNothing, total = 0.f;
+    Piece acc{};
+    auto place = [&](int x) { return (long long)(x ? second + (x - 1) * apart : slot) * ROWS + row; };
+    for (int x0 = together ? wave : 0; x0 < parts; x0 += 64 * step) {
+      const int x = x0 + lane * step;
+      const float2 st = x < parts ? g.stat[place(x)] : make_float2(kNothing, 0.f);
+      const int n = (parts - x0 + step - 1) / step < 64 ? (parts - x0 + step - 1) / step : 64;
+      Piece v[8];
+      auto load = [&](int y0) {
 #pragma unroll
-        for (int o = 32; o > 0; o >>= 1) next = fmaxf(next, __shfl_xor(next, o, 64));
-        const float back = __builtin_amdgcn_exp2f(top - next), scale = __builtin_amdgcn_exp2f(st.x - next);
-        float sum = st.y * scale;
+        for (int y = 0; y < 8; ++y) v[y] = *(const Piece*)(g.part + place(x0 + (y0 + y < n ? y0 + y : n - 1) * step) * D + lane * P);
+      };
+      load(0);
+      float next = fmaxf(top, st.x);
 #pragma unroll
-        for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
-        total = total * back + sum;
-        acc *= back;
-        top = next;
-        for (int y0 = 0; y0 < n; y0 += 8) {
-          if (y0) load(y0);
+      for (int o = 32; o > 0; o >>= 1) next = fmaxf(next, __shfl_xor(next, o, 64));
+      const float back = __builtin_amdgcn_exp2f(top - next), scale = __builtin_amdgcn_exp2f(st.x - next);
+      float sum = st.y * scale;
 #pragma unroll
-          for (int y = 0; y < 8; ++y)
-            if (y0 + y < n) acc += v[y] * __shfl(scale, y0 + y, 64);
-        }
+      for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+      total = total * back + sum;
+      acc *= back;
+      top = next;
+      for (int y0 = 0; y0 < n; y0 += 8) {
+        if (y0) load(y0);
+#pragma unroll
+        for (int y = 0; y < 8; ++y)
+          if (y0 + y < n) acc += v[y] * __shfl(scale, y0 + y, 64);
       }
-      if (together) {
-        __syncthreads();
-        if (lane == 0) wave_stat[wave] = make_float2(top, total);
-        wave_sums[wave][lane] = acc;
-        __syncthreads();
-        if (wave > 0) continue;
-        float t = kNothing;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) t = fmaxf(t, wave_stat[w].x);
-        total = 0.f;
-        acc = Piece{};
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const float scale = __builtin_amdgcn_exp2f(wave_stat[w].x - t);
-          total += wave_stat[w].y * scale;
-          acc += wave_sums[w][lane] * scale;
-        }
-      }
-      const int mm = tile * ROWS + row, tok = mm / g.group;
-      const float inv = item[8] - item[7] + tok < 0 ? 0.f : 1.0f / total;
-      u16* o = g.o + ((long long)(item[6] + tok) * g.heads + head * g.group + mm - tok * g.group) * D + lane * P;
-      if constexpr (P == 2)
-        *(uint32_t*)o = pack_bf16x2(acc[0] * inv, acc[1] * inv);
-      else
-        *o = f2bf(acc[0] * inv);
     }
+    if (together) {
+      __syncthreads();
+      if (lane == 0) wave_stat[wave] = make_float2(top, total);
+      wave_sums[wave][lane] = acc;
+      __syncthreads();
+      if (wave > 0) continue;
+      float t = kNothing;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) t = fmaxf(t, wave_stat[w].x);
+      total = 0.f;
+      acc = Piece{};
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float scale = __builtin_amdgcn_exp2f(wave_stat[w].x - t);
+        total += wave_stat[w].y * scale;
+        acc += wave_sums[w][lane] * scale;
+      }
+    }
+    const int mm = tile * ROWS + row, tok = mm / g.group;
+    const float inv = item[8] - item[7] + tok < 0 ? 0.f : 1.0f / total;
+    u16* o = g.o + ((long long)(item[6] + tok) * g.heads + head * g.group + mm - tok * g.group) * D + lane * P;
+    if constexpr (P == 2)
+      *(uint32_t*)o = pack_bf16x2(acc[0] * inv, acc[1] * inv);
+    else
+      *o = f2bf(acc[0] * inv);
   }
 }
 
