@@ -59,11 +59,9 @@ SequencesArgs sequences_args(const nimble_sequences& s) {
 }
 
 // ------------------------------------------------------------------------------------------------ attention
-// Rows of a tile, and the keys up to which nothing is cut: the second launch costs more than a longer walk saves.
-struct PagedMember {
-  int rows, least_keys;
-};
-static const PagedMember kPagedMembers[NIMBLE_PAGED_COUNT] = {{16, 1024}, {128, 256}};
+constexpr int kPagedRows[NIMBLE_PAGED_COUNT] = {16, 128};
+// Up to so many keys nothing is cut: the second launch costs more than a longer walk saves (one token over 777 keys of 64: 10.4 us cut, then 7.8).
+constexpr int64_t kUncutKeys = 1024;
 constexpr int64_t kStepKeys = 256;   // of the tokens' spans
 // Waves of a workgroup, and workgroups that a compute unit holds at once, by their LDS (tokens) and registers: as many parts as fill the chip once
 // are aimed at.  Tokens: four waves where workgroups share a compute unit, so that one loads while another joins its waves' sums and goes over to
@@ -72,10 +70,24 @@ constexpr int64_t kStepKeys = 256;   // of the tokens' spans
 struct PagedWaves {
   int waves, per_cu;
 };
+static int four_waves_per_cu(int64_t D, int dtype) { return (D == 128 ? 1 : 2) * (dtype == NIMBLE_I8 ? 2 : 1); }
 static PagedWaves paged_waves(int kernel, int64_t D, int dtype, bool lone) {
   if (kernel == NIMBLE_PAGED_CHUNKS) return {4, 2};
-  const int four = (D == 128 ? 1 : 2) * (dtype == NIMBLE_I8 ? 2 : 1);
+  const int four = four_waves_per_cu(D, dtype);
   return lone && four > 1 ? PagedWaves{8, four / 2} : PagedWaves{4, four};
+}
+
+// Which kernel.  16 rows a workgroup for up to 16 rows a sequence, and for more where nothing is cut and its tiles are about as many as the chip holds;
+// else 128.  Microseconds, 16 / 128 rows a workgroup (graph replays; rows: of a sequence and a head of the cache):
+//   bf16, heads of 64, 16 of the cache:  1 sequence, 128 rows over 628 keys 8.8 / 13.9, 512 over 1012 16 / 17; 16, 64 over 564 23 / 24, 128 over 628 42 / 35,
+//     1 sequence, 32 rows over 4032 25 / 13, 128 over 4128 27 / 20, over 30128 145 / 39
+//   bf16, 128, 8:  1, 128 over 532 14.5 / 18.6; 4, 15.5 / 20.4; 16, 53 / 34; 1, 32 over 4008 23 / 15, over 30008 51 / 33
+//   int8, 64, 16:  16, 128 over 628 30 / 38; 4, 32 over 4032 26 / 26, over 30032 97 / 112, 128 over 4128 59 / 38
+//   int8, 128, 8:  16, 128 over 532 31 / 35; 4, 32 over 4008 25 / 23, over 30008 94 / 82, 128 over 30032 274 / 108
+static int paged_kernel(int64_t rows, int64_t live, int64_t kv_heads, int64_t D, int dtype, int64_t keys) {
+  if (keys <= kUncutKeys && (rows / kPagedRows[0] + live) * kv_heads <= kComputeUnits * 3 / 2 * four_waves_per_cu(D, dtype)) return NIMBLE_PAGED_TOKENS;
+  const int64_t few = dtype == NIMBLE_I8 && keys > kUncutKeys ? 32 : 16;  // (128 rows share what it takes to make bf16 of the codes)
+  return rows > few * live ? NIMBLE_PAGED_CHUNKS : NIMBLE_PAGED_TOKENS;
 }
 
 static int plan_paged(int64_t rows, int64_t count, int64_t width, int64_t heads, int64_t kv_heads, int64_t page, int64_t D, int dtype,
@@ -87,19 +99,17 @@ static int plan_paged(int64_t rows, int64_t count, int64_t width, int64_t heads,
   if (window < 0) return fail(NIMBLE_ERR_ARG, "negative window");
   nimble_paged_plan out{};
   const int64_t group = heads / kv_heads, live = count < rows ? count : rows;
-  out.kernel = rows * group > 32 * live ? NIMBLE_PAGED_CHUNKS : NIMBLE_PAGED_TOKENS;
-  const PagedMember& m = kPagedMembers[out.kernel];
-  const int64_t tiles = rows * group / m.rows + live;   // a sequence adds at most one that is not full
-  // the keys that a tile can see
-  int64_t keys = width * page;
-  if (window > 0 && window + m.rows < keys) keys = window + m.rows;
-  out.rows = m.rows;
-  // Nothing is cut where tiles alone fill the chip twice and none can take long: the second launch is saved.
-  const PagedWaves w = paged_waves(out.kernel, D, dtype, keys <= m.least_keys && tiles * kv_heads <= kComputeUnits);
+  auto seen = [&](int64_t tile_rows) {  // the most keys that a tile can see
+    const int64_t all = width * page;
+    return window > 0 && window + tile_rows < all ? window + tile_rows : all;
+  };
+  out.kernel = paged_kernel(rows * group, live, kv_heads, D, dtype, seen(kPagedRows[0]));
+  out.rows = kPagedRows[out.kernel];
+  const int64_t tiles = rows * group / out.rows + live, keys = seen(out.rows);   // a sequence adds at most one tile that is not full
+  out.parts = keys > kUncutKeys;
+  const PagedWaves w = paged_waves(out.kernel, D, dtype, !out.parts && tiles * kv_heads <= kComputeUnits);
   const int64_t target = (int64_t)kComputeUnits * w.per_cu;
   out.block = 64u * (unsigned)w.waves;
-  const bool plenty = rows * group / m.rows * kv_heads >= 2 * target && keys <= 1024;
-  out.parts = keys > m.least_keys && !plenty;
   if (tiles * kv_heads > kMostPagedGrid) return fail(NIMBLE_ERR_ARG, "more than 2^23 tiles");
   if (tiles * kv_heads > ((1ll << 31) - 1) / (ceil_div(keys, kStepKeys) + 1))
     return fail(NIMBLE_ERR_ARG, "%lld tiles of %lld keys", (long long)(tiles * kv_heads), (long long)keys);
@@ -108,11 +118,11 @@ static int plan_paged(int64_t rows, int64_t count, int64_t width, int64_t heads,
     const bool spans = out.kernel == NIMBLE_PAGED_TOKENS;
     out.grid = (uint32_t)(spans ? target : tiles * kv_heads + target);
     out.slots = 2 * target + 8;
-    const int64_t most = rows * group < m.rows ? rows * group : m.rows;
+    const int64_t most = rows * group < out.rows ? rows * group : out.rows;
     out.join_grid[0] = (uint32_t)(spans ? target : tiles * kv_heads < target ? tiles * kv_heads : target);
     const int64_t across = 2048 / out.join_grid[0] < 4 ? 4 : 2048 / out.join_grid[0];  // (few tiles: their rows side by side)
     out.join_grid[1] = (uint32_t)(most < across ? most : across);
-    out.workspace_bytes = (uint64_t)out.slots * m.rows * (D * 4 + 8) + (uint64_t)(1 + target) * kPagedItemWords * 4;
+    out.workspace_bytes = (uint64_t)out.slots * out.rows * (D * 4 + 8) + (uint64_t)(1 + target) * kPagedItemWords * 4;
   } else {
     out.grid = (uint32_t)(tiles * kv_heads);
   }

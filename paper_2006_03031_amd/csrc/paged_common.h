@@ -352,7 +352,7 @@ __device__ __forceinline__ uint2 codes_to_bf16(uint32_t w) {
 
 // ---------------------------------------------------------------------------
 // The parts of a row joined, in the order of the parts: o = sum_x 2^(ref_x - top) part_x / sum_x 2^(ref_x - top) sum_x.  A wave a row; with more
-// than 8 parts a workgroup a row, whose waves take every fourth part.  A lane looks at one part's (ref, sum) and the wave at its
+// than 8 parts, and rows few enough that each has a workgroup, a workgroup a row, whose waves take every fourth part.  A lane looks at one part's (ref, sum) and the wave at its
 // sums one part after the other, 8 loads at a time.
 // ---------------------------------------------------------------------------
 template <int ROWS, int D>
@@ -371,7 +371,7 @@ __global__ void __launch_bounds__(256) paged_join_kernel(PagedArgs g) {
   const int parts = item[0], slot = item[1], second = item[2], apart = item[3], tile = item[4], head = item[5];
   if ((int)blockIdx.x >= count || parts < 2) return;
   const int left = item[7] * g.group - tile * ROWS, rows = left < ROWS ? left : ROWS;
-  const bool together = parts > MANY;
+  const bool together = parts > MANY && rows <= (int)gridDim.y;
   const int step = together ? 4 : 1;
   for (int row = blockIdx.y + (together ? 0 : wave * gridDim.y); row < rows; row += together ? gridDim.y : 4 * gridDim.y) {
     float top = kNothing, total = 0.f;
