@@ -30,10 +30,12 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 4))
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r32 = lane & 31, h = lane >> 5;
 
+  __shared__ int unit[kUnitWords];
+  if (wave == 0) find_unit<ROWS, KEYS, LEAST>(g, blockIdx.x, unit);
+  __syncthreads();
   PagedUnit u;
-  int items;
-  const bool found = find_unit<ROWS, KEYS, LEAST>(g, blockIdx.x, u, items);
-  if (g.slots && blockIdx.x == 0 && tid == 0) g.items[0] = found ? items : 0;
+  const bool found = take_unit(unit, u);
+  if (g.slots && blockIdx.x == 0 && tid == 0) g.items[0] = unit[11];
   if (!found) return;
   if (u.parts > 1 && (u.slot >= g.slots || u.item >= g.target_units)) return;  // (not with offsets that keep to their description)
   int low, high, block0, block1;

@@ -29,13 +29,13 @@ constexpr float kNothing = -3.0e38f;  // the reference of a row that has seen no
 // What a workgroup does: a tile of ROWS rows of one sequence and one head of the cache, or a part of the keys that it sees.
 // The rows of a (sequence, head) are its tokens times the query heads that share the head, row = token * group + query head: all of them
 // meet the same keys.  Only the device knows the lengths, so it is the device that cuts: the key blocks of all tiles together, divided by
-// the units that fill the chip, are the most that one part takes, and a tile that has more is cut into equal parts.  Every wave works
+// the units that fill the chip, are what one part takes, and a tile that has more is cut into equal parts.  Every workgroup works
 // this out for itself from all lengths, 64 sequences a step.  Heavy tiles of a sequence come first, the heads of the cache innermost: their
 // workgroups go to the XCDs in turn, so that the tiles which read one head's keys share an L2.
 // ---------------------------------------------------------------------------
 struct PagedUnit {
   Sequence seq;
-  int s, head, tile, tiles;
+  int s, head, tile, tiles;  // tiles: of the sequence (SpanWalk only)
   int part, parts;
   int slot, item;  // in the workspace; slot -1: the tile was not cut
 };
@@ -61,6 +61,21 @@ __device__ __forceinline__ T wave_scan(T x) {
   step(integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{});  // the last of rows 0 and 2 to rows 1 and 3
   step(integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{});  // the last of row 1 to rows 2 and 3
   return x;
+}
+
+__device__ __forceinline__ int wave_max(int x) {  // of values from 0 on
+  auto step = [&](auto ctrl, auto rows) {
+    const int y = __builtin_amdgcn_update_dpp(0, x, decltype(ctrl)::value, decltype(rows)::value, 0xf, false);
+    x = y > x ? y : x;
+  };
+  using std::integral_constant;
+  step(integral_constant<int, 0x111>{}, integral_constant<int, 0xf>{});
+  step(integral_constant<int, 0x112>{}, integral_constant<int, 0xf>{});
+  step(integral_constant<int, 0x114>{}, integral_constant<int, 0xf>{});
+  step(integral_constant<int, 0x118>{}, integral_constant<int, 0xf>{});
+  step(integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{});
+  step(integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{});
+  return __builtin_amdgcn_readlane(x, 63);
 }
 
 template <int ROWS, int KEYS>
@@ -90,12 +105,15 @@ __device__ __forceinline__ int part_blocks(const PagedArgs& g) {
   return most < (float)LEAST ? LEAST : most > 1.0e9f ? 1000000000 : (int)most;
 }
 
+// One wave finds the workgroup's unit (four at once take four times as long) and leaves it in `shared`, kUnitWords words of LDS; behind a barrier
+// take_unit reads it, and the number of tiles that are cut (the last word, where unit = 0).
+constexpr int kUnitWords = 12;
 template <int ROWS, int KEYS, int LEAST>
-__device__ __forceinline__ bool find_unit(const PagedArgs& g, unsigned unit, PagedUnit& u, int& items) {
+__device__ __forceinline__ void find_unit(const PagedArgs& g, unsigned unit, int* shared) {
   const int lane = threadIdx.x & 63, G = g.cache.kv_heads;
   const int most = g.slots ? part_blocks<ROWS, KEYS, LEAST>(g) : 1000000000;
   const unsigned want = unit / G;
-  u.head = (int)(unit - want * G);
+  const int head = (int)(unit - want * G);
   unsigned units = 0, cut_units = 0, cut_tiles = 0;  // of the sequences ahead
   bool found = false;
   for (int base = 0; base < g.seqs.count && (!found || unit == 0); base += 64) {
@@ -106,34 +124,63 @@ __device__ __forceinline__ bool find_unit(const PagedArgs& g, unsigned unit, Pag
       q = sequence_of(g.seqs, s, g.cache.page_shift);
       tile_work<ROWS, KEYS>(g, q, tiles, blocks);
     }
-    const int parts = (int)(((unsigned)blocks + (unsigned)most / 2) / (unsigned)most) > 1 ? (int)(((unsigned)blocks + (unsigned)most / 2) / (unsigned)most) : 1;
-    const unsigned mine = (unsigned)tiles * parts, mine_cut = parts > 1 ? mine : 0, tiles_cut = parts > 1 ? tiles : 0;
-    const unsigned a = wave_scan(mine), b = wave_scan(mine_cut), c = wave_scan(tiles_cut);
-    const unsigned long long here = __ballot(units + a > want);
-    if (!found && here) {
-      const int l = __ffsll((unsigned long long)here) - 1;
-      auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
-      const unsigned before = units + (unsigned)of((int)(a - mine));
-      u.s = base + l;
-      u.seq.first = of(q.first);
-      u.seq.n = of(q.n);
-      u.seq.length = of(q.length);
-      u.tiles = of(tiles);
-      u.parts = of(parts);
-      const int rest = (int)(want - before);
-      const int back = rest / u.parts;
-      u.tile = u.tiles - 1 - back;
-      u.part = rest - back * u.parts;
-      u.slot = u.parts == 1 ? -1 : (int)((cut_units + (unsigned)of((int)(b - mine_cut)) + rest) * G + u.head);
-      u.item = (int)((cut_tiles + (unsigned)of((int)(c - tiles_cut)) + back) * G + u.head);
-      found = true;
+    int parts = 1;
+    unsigned b = 0, c = 0;
+    if (g.slots) {
+      const unsigned p = ((unsigned)blocks + (unsigned)most / 2) / (unsigned)most;
+      parts = p > 1 ? (int)p : 1;
     }
-    units += (unsigned)__builtin_amdgcn_readlane((int)a, 63);
-    cut_units += (unsigned)__builtin_amdgcn_readlane((int)b, 63);
-    cut_tiles += (unsigned)__builtin_amdgcn_readlane((int)c, 63);
+    const unsigned mine = (unsigned)tiles * parts, mine_cut = parts > 1 ? mine : 0, tiles_cut = parts > 1 ? tiles : 0;
+    if (g.slots) b = wave_scan(mine_cut), c = wave_scan(tiles_cut);
+    // of these 64 sequences the long ones first, in four classes: what begins last should not take longest
+    const int longest = wave_max(blocks);
+    unsigned start = units;
+#pragma unroll
+    for (int k = 3; k >= 0; --k) {
+      const bool in = (k == 0 || blocks * 4ll > (long long)longest * k) && (k == 3 || blocks * 4ll <= (long long)longest * (k + 1));
+      const unsigned upto = wave_scan(in ? mine : 0u);
+      if (in) start = units + upto - mine;
+      units += (unsigned)__builtin_amdgcn_readlane((int)upto, 63);
+    }
+    const bool here = mine > 0 && want >= start && want - start < mine;
+    if (!found && __any(here)) {
+      found = true;
+      if (here) {
+        const int rest = (int)(want - start), back = rest / parts;
+        shared[0] = 1;
+        shared[1] = s;
+        shared[2] = q.first;
+        shared[3] = q.n;
+        shared[4] = q.length;
+        shared[5] = tiles - 1 - back;
+        shared[6] = rest - back * parts;
+        shared[7] = parts;
+        shared[8] = parts == 1 ? -1 : (int)((cut_units + b - mine_cut + rest) * G + head);
+        shared[9] = (int)((cut_tiles + c - tiles_cut + back) * G + head);
+        shared[10] = head;
+      }
+    }
+    if (g.slots) {
+      cut_units += (unsigned)__builtin_amdgcn_readlane((int)b, 63);
+      cut_tiles += (unsigned)__builtin_amdgcn_readlane((int)c, 63);
+    }
   }
-  items = (int)cut_tiles * G;  // (of all sequences where unit = 0, which looks at all)
-  return found;
+  if (lane == 0) {
+    if (!found) shared[0] = 0;
+    shared[11] = (int)cut_tiles * G;
+  }
+}
+__device__ __forceinline__ bool take_unit(const int* shared, PagedUnit& u) {
+  auto word = [&](int i) { return __builtin_amdgcn_readfirstlane(shared[i]); };
+  u.s = word(1);
+  u.seq = Sequence{word(2), word(3), word(4)};
+  u.tile = word(5);
+  u.part = word(6);
+  u.parts = word(7);
+  u.slot = word(8);
+  u.item = word(9);
+  u.head = word(10);
+  return word(0) != 0;
 }
 
 // The keys of a tile, and of one part of it, in blocks.
