@@ -27,9 +27,15 @@ int check_rows(const void* p, int64_t stride, int64_t heads, int64_t D, const ch
   return NIMBLE_OK;
 }
 
+// Rows of a workgroup: as many as leave each compute unit `groups` of them.
+static int rows_each(int64_t rows, int groups) {
+  const int64_t n = rows / (groups * kComputeUnits);
+  return (int)(n < 1 ? 1 : n > kMostPlaces ? kMostPlaces : n);
+}
+
 template <int D, bool INTERLEAVED>
 static void launch_write(const CacheWriteArgs& g, bool int8, hipStream_t stream) {
-  const dim3 grid((unsigned)g.seqs.rows), block(256);
+  const dim3 grid((unsigned)ceil_div(g.seqs.rows, g.rows_each)), block(256);
   if (int8)
     hipLaunchKernelGGL((cache_write_kernel<D, true, INTERLEAVED>), grid, block, 0, stream, g);
   else
@@ -38,7 +44,7 @@ static void launch_write(const CacheWriteArgs& g, bool int8, hipStream_t stream)
 
 template <int D>
 static void launch_read(const CacheReadArgs& g, bool int8, bool f32, hipStream_t stream) {
-  const dim3 grid((unsigned)g.seqs.rows), block(256);
+  const dim3 grid((unsigned)ceil_div(g.seqs.rows, g.rows_each)), block(256);
   auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, g); };
   if (int8) {
     if (f32) launch(cache_read_kernel<D, true, true>);
@@ -136,6 +142,7 @@ int nimble_cache_write_dyn(const nimble_cache* cache, const nimble_sequences* se
   g.table_rows = table_rows;
   g.heads = (int)heads;
   g.R = g.table ? (int)R : 0;
+  g.rows_each = rows_each(seqs->rows, 16);
   const bool int8 = cache->dtype == NIMBLE_I8;
   if (D == 64) {
     if (interleaved) launch_write<64, true>(g, int8, (hipStream_t)stream);
@@ -156,7 +163,7 @@ int nimble_cache_read_dyn(const nimble_cache* cache, const nimble_sequences* seq
   if (seqs->rows == 0 || seqs->count == 0) return NIMBLE_OK;
   if (!k_out || !v_out) return fail(NIMBLE_ERR_NULL, "null tensor pointer");
   if (misaligned(k_out) || misaligned(v_out)) return fail(NIMBLE_ERR_ALIGN, "device pointers must be 16-byte aligned");
-  const CacheReadArgs g{cache_args(*cache), sequences_args(*seqs), k_out, v_out};
+  const CacheReadArgs g{cache_args(*cache), sequences_args(*seqs), k_out, v_out, rows_each(seqs->rows, 16)};
   if (cache->D == 64)
     launch_read<64>(g, cache->dtype == NIMBLE_I8, out_dtype == NIMBLE_F32, (hipStream_t)stream);
   else
