@@ -136,6 +136,112 @@ def test_what_a_row_does_not_see_has_no_part(old, bad):
     assert bool((got[5, :2][:, keep] - want[5, :2][:, keep]).abs().le(bound[5, :2][:, keep]).all())
 
 
+def _plan(batch, H, G, D, int8=False, window=0):
+    import paper_2006_03031_amd as nb
+    return nb.paged_attention_plan(batch.rows, len(batch.sizes), batch.pages.shape[1], H, G, batch.page, D, nb.I8 if int8 else nb.BF16, window)
+
+
+CHUNKS = [[(0, 300), (0, 1), (1200, 129), (0, 0), (64, 64)], [(0, 128), (0, 127)], [(2000, 200)], [(0, 700), (30, 90), (-50, 150), (-40, 40)]]
+
+
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("window", [0, 1, 70, 128, 1500])
+@pytest.mark.parametrize("H,G,D", [(2, 1, 64), (3, 1, 128), (4, 4, 64)])
+@pytest.mark.parametrize("sizes", range(len(CHUNKS)))
+def test_many_rows(sizes, H, G, D, window, int8):
+    """128 rows a workgroup: tiles and waves that are partly or not at all filled, rows at positions below 0, a sequence without tokens."""
+    batch = Batch(CHUNKS[sizes], 32, ahead=1, behind=2, extra_columns=40)
+    assert _plan(batch, H, G, D, int8, window).kernel == (1 if not 0 < window <= 1000 else 0)
+    cache, q = pu.random_cache(batch, G, D, int8), _q(batch, H, D)
+    out = torch.full((batch.rows, H, D), 7.0, dtype=BF)
+    got = _run(q, cache, batch, window=window, out=out)
+    _check(got, q, cache, batch, window)
+    assert bool((got[:1] == 7).all()) and bool((got[-2:] == 7).all())
+    low = torch.tensor([r for _, r, p in batch.each() if p < 0], dtype=torch.int64)
+    assert bool((got.cpu()[low] == 0).all())
+
+
+@pytest.mark.parametrize("bad", [math.inf, math.nan])
+@pytest.mark.parametrize("old", [0, 1500])
+def test_many_rows_and_what_they_do_not_see(old, bad):
+    """An infinite or NaN key and value among the new ones: rows ahead of it are as without it, rows behind it are not finite where it counts."""
+    batch = Batch([(old, 180), (old, 150)], 16, extra_columns=80)
+    assert _plan(batch, 4, 2, 64).kernel == 1
+    cache, q = pu.random_cache(batch, 2, 64, False), _q(batch, 4, 64)
+    want, bound = pu.attention(q, cache, batch)
+    page, slot = batch.slots(0, torch.tensor([old + 100]))
+    cache[1][page, 0, slot, 5] = bad
+    cache[0][page, 1, slot, 5] = bad
+    got = _run(q, cache, batch).double().cpu()
+    clean = list(range(100)) + list(range(180, 330))
+    assert bool((got[clean] - want[clean]).abs().le(bound[clean]).all())
+    seen = got[100:180]
+    assert not bool(seen[:, :2, 5].isfinite().any()) and bool(seen[:, :2, :5].isfinite().all())
+    # the other head's scores: NaN, or plus or minus infinity by the query's sign, which leaves its weights NaN or 0
+    if math.isnan(bad):
+        assert bool(seen[:, 2:].isnan().all())
+
+
+def test_many_rows_and_nan_scales_of_hidden_keys():
+    batch = Batch([(1100, 200)], 16)
+    assert _plan(batch, 2, 1, 64, True).kernel == 1
+    cache, q = pu.random_cache(batch, 1, 64, True), _q(batch, 2, 64)
+    want, bound = pu.attention(q, cache, batch)
+    page, slot = batch.slots(0, torch.tensor([1100 + 150]))
+    cache[2][page, 0, slot] = math.nan
+    cache[3][page, 0, slot] = math.nan
+    got = _run(q, cache, batch).double().cpu()
+    assert bool((got[:150] - want[:150]).abs().le(bound[:150]).all()) and bool(got[150:].isnan().all())
+
+
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("count,waves", [(1, 8), (300, 4)])
+def test_the_tokens_workgroups(count, waves, D, int8):
+    """Eight waves for few short tiles, four for many (and for bf16 heads of 128)."""
+    batch = Batch([(700 - i, 1) for i in range(count)], 32)
+    p = _plan(batch, 8, 4, D, int8)
+    assert p.kernel == 0 and p.block == 64 * (4 if D == 128 and not int8 else waves)
+    cache, q = pu.random_cache(batch, 4, D, int8), _q(batch, 8, D)
+    got = _run(q, cache, batch)
+    few = Batch(batch.sizes, 32)
+    few.sizes = batch.sizes[:5]
+    _check(got, q, cache, few)
+
+
+@pytest.mark.parametrize("int8,D", [(False, 128), (True, 64)])
+def test_walks_of_more_than_64_blocks_a_wave(int8, D):
+    """Sequences so long that a wave looks its pages up more than once; the reference in 64 bits on the GPU."""
+    from paper_2006_03031_amd import runtime as rt
+    G, page, lengths = 16, 64, (150001, 149000) if int8 else (90001, 80000)
+    W = -(-max(lengths) // page)
+    shape = (2 * W, G, page, D)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    if int8:
+        cache = rt.PagedCache(*(torch.randint(-127, 128, shape, dtype=torch.int8, device="cuda", generator=g) for _ in "kv"),
+                              *(torch.rand(shape[:3], device="cuda", generator=g) * 0.02 for _ in "kv"))
+    else:
+        cache = rt.PagedCache(*(torch.randn(shape, device="cuda", generator=g, dtype=BF) for _ in "kv"))
+    pages = torch.randperm(2 * W, device="cuda", generator=g).to(torch.int32).view(2, W)
+    q = torch.randn(2, G, D, device="cuda", generator=g, dtype=BF)
+    seqs = rt.Sequences(torch.arange(3, device="cuda"), torch.tensor(lengths, device="cuda"), pages)
+    got = rt.paged_attention(q, cache, seqs).double()
+    half = pu.half_step(BF)
+    for s, L in enumerate(lengths):
+        j = torch.arange(L, device="cuda")
+        for h in (0, 7, 15):
+            at = pages[s].long()[j // page], h, j % page
+            k, v = cache.k[at].double(), cache.v[at].double()
+            if int8:
+                k, v = k * cache.k_scale[at].double()[:, None], v * cache.v_scale[at].double()[:, None]
+            terms = k * q[s, h].double()
+            w = torch.softmax(terms.sum(1) * D ** -0.5, 0)
+            want = (w[:, None] * v).sum(0)
+            off = (D + 4) * 2.0 ** -24 * D ** -0.5 * float(terms.abs().sum(1).max())
+            bound = half * want.abs() + (half + 2 * off + 2.0 ** -18) * (w[:, None] * v.abs()).sum(0)
+            assert bool(((got[s, h] - want).abs() <= bound).all()), (s, h)
+
+
 def test_pages_ahead_of_the_window_may_be_gone():
     batch = Batch([(500, 3)], 16)
     cache, q = pu.random_cache(batch, 2, 64, False), _q(batch, 4, 64)

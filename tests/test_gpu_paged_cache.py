@@ -269,6 +269,52 @@ def test_rows_find_their_sequence_among_many(count):
 
 
 @pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("count,most", [(40, 500), (70, 300), (64, 2300)])
+def test_workgroups_of_several_rows(count, most, int8):
+    """Batches of so many rows that a workgroup takes 2 to 16 of them: rows of several sequences, of none, and without a place beside each other."""
+    import paper_2006_03031_amd as nb
+    from paper_2006_03031_amd import runtime as rt
+    g = torch.Generator().manual_seed(count)
+    new = torch.randint(0, most, (count,), generator=g).tolist()
+    batch = Batch([(0, n) for n in new], 64, ahead=5, behind=11)
+    assert batch.rows > 8192
+    batch.pages[3, 1] = -1                                    # rows 64 .. 127 of one sequence are dropped
+    assert new[3] > 70
+    cache = pu.to_gpu(pu.random_cache(batch, 1, 64, int8))
+    before = [None if t is None else t.clone() for t in cache]
+    k, v, q = (torch.randn(batch.rows, n, 64, generator=g).to(BF).cuda() for n in (1, 1, 3))
+    seqs = batch.on_gpu()
+    out = torch.full_like(q, 9.0)
+    table = pu.angles(most, 32).float().cuda()
+    rt.cache_write(cache, k, v, seqs, q=q, table=table, out=out)
+    positions = torch.zeros(batch.rows, dtype=torch.int64)
+    mine = torch.zeros(batch.rows, dtype=torch.bool)
+    placed = mine.clone()
+    for s, row, p in batch.each():
+        positions[row], mine[row], placed[row] = p, True, int(batch.pages[s, p // 64]) >= 0
+    want_q, want_k = (rt.rotary(t, positions.cuda(), table) for t in (q, k))
+    mine, placed = mine.cuda(), placed.cuda()
+    assert torch.equal(out[mine], want_q[mine]) and bool((out[~mine] == 9).all())
+    filled = tuple(torch.full((batch.rows, 1, 64), 9.0, dtype=BF, device="cuda") for _ in "kv")
+    got_k, got_v = rt.cache_read(cache, seqs, batch.rows, out=filled)
+    assert bool((got_k[~placed] == 9).all()) and bool((got_v[~placed] == 9).all())
+    if int8:
+        # half a step of the code, and the roundings of the scale, the product and the bf16 result
+        for got, want in ((got_k, want_k), (got_v, v)):
+            top = want[placed].float().abs().amax(-1, keepdim=True)
+            assert bool(((got - want)[placed].float().abs() <= top * (0.5 / 127 + 3 * pu.half_step(BF))).all())
+    else:
+        assert torch.equal(got_k[placed], want_k[placed]) and torch.equal(got_v[placed], v[placed])
+    used = torch.zeros(batch.count, 64, dtype=torch.bool)
+    for s, _, p in batch.each():
+        if int(batch.pages[s, p // 64]) >= 0:
+            used[int(batch.pages[s, p // 64]), p % 64] = True
+    for a, b in zip(cache, before):
+        if a is not None:
+            assert torch.equal(a[:, 0].cpu()[~used], b[:, 0].cpu()[~used])
+
+
+@pytest.mark.parametrize("int8", [False, True])
 @pytest.mark.parametrize("window", [0, 20])
 def test_a_decoder_layer_in_chunks_is_the_layer_at_once(int8, window):
     """A prompt through dense, cache_write and paged_attention as one batch, and the same tokens a few at a time, at the end one by one as
