@@ -23,7 +23,7 @@ struct CacheArgs {
 
 // A launch is of fewer than 2^32 threads.
 constexpr int64_t kMostPagedGrid = 1 << 23;
-// Sequences are looked for 64 by 64 (PagedUnit), positions and rows are 32-bit numbers.
+// Sequences are looked for 64 by 64 (SpanWalk, find_unit), positions and rows are 32-bit numbers.
 constexpr int64_t kMostSequences = 1 << 16, kMostPositions = 1ll << 30, kMostRows = 1ll << 24;
 constexpr int kPagedItemWords = 12;
 

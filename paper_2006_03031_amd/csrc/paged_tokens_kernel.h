@@ -18,6 +18,10 @@ namespace nimble {
 //   Loads:   direct global->LDS loads into the wave's own ring of two blocks, waited for by count: no barrier in the loop.  16 keys lie in one
 //            page, whose number is a scalar.  Chunk c of row r sits at c ^ swizzle(r).  Keys outside of what the tile sees repeat the
 //            nearest one that it does.
+//   Bound by memory where the cache is large: one token over 131001 keys, 8 heads of 128 in bf16, 88.5 us, 537 MB at 6.06 TB/s, of which 5.1 are the second
+// launch (a kernel that only reads reaches 6.4 to 6.5); 64 tokens over up to 8192 keys in 8 bits 108 us, 563 MB at 5.2 TB/s: two tiles a workgroup, whose
+// beginnings and ends nothing hides.  One token over 777 keys, 16 heads of 64: 8.5 us, a launch, three loads one behind the other for the unit,
+// the wave's three blocks and the meeting of eight waves.
 // ---------------------------------------------------------------------------
 template <int D, bool I8, int WAVES>
 __global__ void __launch_bounds__(WAVES * 64) paged_tokens_kernel(PagedArgs g) {
@@ -88,7 +92,7 @@ __global__ void __launch_bounds__(WAVES * 64) paged_tokens_kernel(PagedArgs g) {
   const int k0 = low & ~15, k1 = high & ~15;
   auto held_to = [&](int key) { return key < k0 ? k0 : key > k1 ? k1 : key; };
   // The pages of the wave's next 64 blocks: lane l holds that of keys 16 (l & 1) .. + 15 of its blocks l / 2 and 32 + l / 2.  (Looked up block by block
-  // through the scalar cache a block of 777 keys of 64 took 0.77 us, with the pages at hand AT_HAND.)
+  // through the scalar cache a block of a wave took 0.77 us of one token over 777 keys of 64, most of it waiting for its page.)
   int pages0 = 0, pages1 = 0;
   auto page_at = [&](int i) { return table[held_to((block0 + wave + i * WAVES) * KEYS + (lane & 1) * 16) >> g.cache.page_shift]; };
   auto look_up = [&](int first) {  // from the wave's block `first` on

@@ -501,7 +501,7 @@ def paged_attention(q: torch.Tensor, cache: PagedCache, sequences: Sequences, al
     heads / kv_heads query heads share keys.  alpha: 1 / sqrt(D) unless given.  A token of each sequence and chunks of many are served alike.
     workspace: of nb.paged_attention_plan's size, for one call at a time; by default a new one, so that calls may overlap."""
     if workspace is None:
-        o = _host_calls.paged_attention(q, cache, sequences, alpha if alpha is not None else q.shape[-1] ** -0.5 if q.dim() == 3 else None, window, out)
+        o = _host_calls.paged_attention(q, cache, sequences, alpha if alpha is not None else q.shape[2] ** -0.5 if q.dim() == 3 and q.shape[2] else None, window, out)
         if o is not None:
             return o
     shape = nb.paged_attention_shape(tuple(q.shape), tuple(cache.k.shape))

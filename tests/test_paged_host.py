@@ -271,3 +271,12 @@ def test_grid_and_workspace_hold_every_batch():
             assert not cut and p.workspace_bytes == 0
         seen.add((p.kernel, p.parts, cut))
     assert seen >= {(0, 1, True), (0, 1, False), (0, 0, False), (1, 1, True), (1, 1, False), (1, 0, False)}
+
+
+def test_queries_without_elements_are_refused_by_their_shape():
+    from paper_2006_03031_amd import runtime as rt
+    k = torch.zeros(CACHE, dtype=torch.bfloat16)
+    batch = rt.Sequences(torch.zeros(2, dtype=torch.int64), torch.zeros(1, dtype=torch.int64), torch.zeros((1, 3), dtype=torch.int32))
+    for shape in ((7, 4, 0), (7, 4, 32), (7, 3, 64), (7, 256)):
+        with pytest.raises(nb.NimbleError):
+            rt.paged_attention(torch.zeros(shape, dtype=torch.bfloat16), rt.PagedCache(k, k), batch)
