@@ -497,8 +497,9 @@ int nimble_cache_read_dyn(const nimble_cache* cache, const nimble_sequences* seq
 /* Attention of the rows over the cache, their own keys and values included (write them first):
  *   o[r,h] = sum_j softmax_j(alpha q[r,h].k[j,h/(H/G)]) v[j,h/(H/G)] over the positions max(0, p-window+1) <= j <= p of r's sequence,
  * p the position of r; window = 0: all j <= p.  A row that sees nothing (p < 0) gives zeros.  q [rows,H,D] bf16, o [rows,H,D] bf16
- * contiguous; H a multiple of G; alpha > 0 and finite, window >= 0.  Scores, softmax and sums in f32, the probabilities (times the
- * values' scales) rounded to bf16 before the product with v.  What a row does not see has no part in its result, whatever it holds.
+ * contiguous; H a multiple of G; alpha > 0 and finite, window >= 0.  Scores, softmax and sums in f32; the probabilities (times the
+ * values' scales) enter the product with v rounded to bf16 where there are many rows, and as a sum of two bf16, 2^-16 off at most, where
+ * there are few (which is which: nimble_paged_attention_plan_of).  What a row does not see has no part in its result, whatever it holds.
  * Long sequences are cut on the device, by the lengths, and joined by a second launch; the result depends on the lengths of all
  * sequences of the call, but not on the run.
  * workspace: nimble_paged_attention_plan_of's workspace_bytes, used by one call at a time; nothing in it carries over. */

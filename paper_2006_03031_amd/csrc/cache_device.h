@@ -38,6 +38,9 @@ __device__ __forceinline__ int sequence_at(const SequencesArgs& g, int t) {
   return base < g.count && g.offsets[base] <= t ? base : -1;
 }
 
+// One of two neighbouring bf16.
+__device__ __forceinline__ float of_pair(uint32_t w, int i) { return __uint_as_float(i ? w & 0xffff0000u : w << 16); }
+
 // Row of the cache that holds position p of sequence s: (page * heads + head) * page size + slot, or -1.
 __device__ __forceinline__ long long cache_row(const CacheArgs& c, const SequencesArgs& g, int s, int p) {
   const int column = p >> c.page_shift;

@@ -61,8 +61,6 @@ __global__ void __launch_bounds__(256)
 //   Bound by memory: 8177 rows of 32 heads of 128 in 26.2 us, 136 MB at 5.2 TB/s, what a copy of 1 GiB reaches; one row of 16 heads 1.6, a launch and two
 // loads one behind the other.  (Loads or stores past the caches were slower.)
 // ---------------------------------------------------------------------------
-__device__ __forceinline__ float of_pair(uint32_t w, int i) { return __uint_as_float(i ? w & 0xffff0000u : w << 16); }
-
 struct Chunk {  // 8 bf16
   uint32_t w[4];
   __device__ __forceinline__ float value(int i) const { return of_pair(w[i >> 1], i & 1); }

@@ -63,12 +63,15 @@ def values(cache, which):
     return x if scale is None else x * scale.double()[..., None]
 
 
-def attention(q, cache, batch, window=0, alpha=None):
+def attention(q, cache, batch, window=0, alpha=None, weight_step=None):
     """(o, bound): the formula in 64 bits, and how far the kernel may be off in each element: half a step of bf16 for the result, another,
     relative to sum_j w_j |v_j|, for the probabilities' rounding, and for the weights' own errors twice those of the scores, whose D products
     are added in f32, and 2^-18 for exp2, the running sums and the joins.  exp2 of less than -126, and a probability below 2^-126 once it is
-    rounded to bf16, may be taken as 0, a weight of at most 2^-126 either time (the weights' sum is at least about 1): 2^-125 sum_j |v_j|."""
+    rounded to bf16, may be taken as 0, a weight of at most 2^-126 either time (the weights' sum is at least about 1): 2^-125 sum_j |v_j|.
+    weight_step: what the probabilities' rounding may take instead; in two bf16 it is half a step of half a step, and what the second loses
+    below 2^-126 at most 2^-125 too."""
     T, H, D = q.shape
+    weight_step = half_step(BF) if weight_step is None else weight_step
     G = cache[0].shape[1]
     alpha = D ** -0.5 if alpha is None else alpha
     k_all, v_all = values(cache, 0), values(cache, 1)
@@ -87,8 +90,8 @@ def attention(q, cache, batch, window=0, alpha=None):
             vh = v[:, h // (H // G)]
             o[row, h] = w @ vh
             scores_off = (D + 4) * 2.0 ** -24 * alpha * float(terms.abs().sum(1).max())
-            bound[row, h] = half_step(BF) * o[row, h].abs() + (half_step(BF) + 2 * scores_off + 2.0 ** -18) * (w @ vh.abs()) + \
-                2.0 ** -125 * vh.abs().sum(0)
+            bound[row, h] = half_step(BF) * o[row, h].abs() + (weight_step + 2 * scores_off + 2.0 ** -18) * (w @ vh.abs()) + \
+                2.0 ** -124 * vh.abs().sum(0)
     return o, bound
 
 

@@ -20,8 +20,8 @@ def _run(q, cache, batch, **kw):
     return rt.paged_attention(q.cuda(), pu.to_gpu(cache), batch.on_gpu(), **kw)
 
 
-def _check(got, q, cache, batch, window=0, alpha=None):
-    want, bound = pu.attention(q, cache, batch, window, alpha)
+def _check(got, q, cache, batch, window=0, alpha=None, weight_step=None):
+    want, bound = pu.attention(q, cache, batch, window, alpha, weight_step)
     got = got.double().cpu()
     rows = [r for _, r, _ in batch.each()]
     off = ((got - want).abs() - bound)[rows]
@@ -47,6 +47,15 @@ def test_formula(sizes, H, G, D, int8):
     batch = Batch(SIZES[sizes], 16)
     cache, q = pu.random_cache(batch, G, D, int8), _q(batch, H, D)
     _check(_run(q, cache, batch), q, cache, batch)
+
+
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("sizes", ["short", "ragged", "long"])
+def test_probabilities_of_few_rows_are_kept_in_two_parts(sizes, D, int8):
+    batch = Batch(SIZES[sizes] if sizes != "long" else [(5000, 1), (12, 1), (2100, 1)], 32)
+    cache, q = pu.random_cache(batch, 2, D, int8, seed=7), _q(batch, 4, D, seed=8)
+    _check(_run(q, cache, batch), q, cache, batch, weight_step=pu.half_step(BF) ** 2)
 
 
 @pytest.mark.parametrize("int8", [False, True])
