@@ -332,9 +332,16 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 4))
 #pragma unroll
   for (int t = 0; t < NT; ++t)
 #pragma unroll
-    for (int b = 0; b < 4; ++b)
-      *(uint2*)(o + t * 32 + b * 8 + h * 4) = make_uint2(pack_bf16x2(oacc[t][4 * b] * inv, oacc[t][4 * b + 1] * inv),
-                                                         pack_bf16x2(oacc[t][4 * b + 2] * inv, oacc[t][4 * b + 3] * inv));
+    for (int b = 0; b < 4; b += 2) {  // (the two lanes of a row exchange, for whole 16 bytes a lane: 32 prompts of up to 512 rows 22.0 -> 21.5 us)
+      uint32_t w[2][2];
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int y = 0; y < 2; ++y) w[x][y] = pack_bf16x2(oacc[t][4 * (b + x) + 2 * y] * inv, oacc[t][4 * (b + x) + 2 * y + 1] * inv);
+      const auto s0 = __builtin_amdgcn_permlane32_swap(w[0][0], w[1][0], false, false);
+      const auto s1 = __builtin_amdgcn_permlane32_swap(w[0][1], w[1][1], false, false);
+      *(uint4*)(o + t * 32 + (b + h) * 8) = make_uint4(s0[0], s1[0], s0[1], s1[1]);
+    }
 }
 
 }  // namespace nimble
