@@ -12,6 +12,17 @@ struct SequencesArgs {
   const int* pages;
   int count, width, rows;
 };
+// x / d for x < 2^30 and d <= 2^16 as (2 x magic / 2^32) >> shift: shift = floor(log2 d), magic = ceil(2^(31 + shift) / d), whose excess e = magic d - 2^(31 + shift)
+// is at most d - 1 < 2^(shift + 1), so that x e < 2^(31 + shift), which is less than what a quotient can be off by.
+struct Divisor {
+  unsigned magic, shift;
+};
+inline Divisor divisor_of(int64_t d) {
+  unsigned shift = 0;
+  while ((d >> shift) > 1) ++shift;
+  return Divisor{(unsigned)(((1ull << (31 + shift)) + (uint64_t)d - 1) / (uint64_t)d), shift};
+}
+
 struct CacheArgs {
   unsigned char* k;
   unsigned char* v;

@@ -63,6 +63,8 @@ int nimble_paged_attention_dyn(const void* q, int64_t q_stride, const nimble_cac
   g.q_stride = q_stride;
   g.heads = (int)heads;
   g.group = (int)(heads / cache->kv_heads);
+  g.by_group = divisor_of(g.group);
+  g.by_heads = divisor_of(cache->kv_heads);
   g.window = (int)(window < kMostPositions ? window : 0);  // (2^30 and beyond: all)
   g.a2 = alpha * 1.4426950408889634f;
   if (!std::isfinite(g.a2)) return fail(NIMBLE_ERR_ARG, "paged_attention: alpha = %g is too large", (double)alpha);

@@ -15,13 +15,18 @@ namespace nimble {
 //   bf16:    direct global->LDS loads.  Chunk c of key row r sits at c ^ k_swizzle(r), of value row r at c ^ v_swizzle(r).
 //   8 bits:  codes go through registers, where they become bf16, which holds them exactly, once for the workgroup; a key's scale multiplies its
 //            scores, a value's its probability.
-//   Bound by the matrix products and by what the chip draws: 2048 tokens over 16384 keys, 32 heads of 128 over 8, 521 us, 989 TFLOP/s with random numbers; with
-// zeros, at a higher clock, 416 us, 1239 (the library's product of 8192^3 with random numbers 1307 to 1354).  Of LDS reads it needs as
-// much time as of matrix instructions (32 rows a wave).  Tried and slower: scores of block i + 1 ahead of the probabilities of block i (521, or spilled),
-// 64 rows a wave (868: accumulators move to and fro), eight waves over 256 rows in two phases (537).  32 prompts of up to 512, 16 heads of 64: 22.8 us.
+//   Bound by the matrix products and by what the chip draws: 2048 tokens over 16384 keys, 32 heads of 128 over 8, 502 to 516 us, 1000 to 1026 TFLOP/s with random numbers;
+// with zeros, at a higher clock, 398 us, 1296 (the library's product of 8192^3 with random numbers 1307 to 1354).  Of LDS reads it needs as
+// much time as of matrix instructions (32 rows a wave).  Tried and slower: scores of block i + 1 ahead of the probabilities of block i (no gain, or spilled),
+// 64 rows a wave (868: accumulators move to and fro), eight waves over 256 rows in two phases (537 where this took 521),
+// the sum of the probabilities by a matrix instruction with ones (+ 5 %), a copy of the loop without masks (+ 9 %).  32 prompts of up to 512, 16 heads of 64:
+// 20.8 us, 69 MB at 3.3 TB/s: 1280 tiles of 1 to 8 blocks, of which 1024 are under way at once; a tile spends 1.3 us in finding itself and 1.7 to 2.9 until its
+// first keys are there.
 // ---------------------------------------------------------------------------
+// (Heads of 64 in 8 bits: three waves a SIMD, with registers for what is converted; 2048 tokens over 16384 keys 439 us, two to four 466, four 684.  Of
+// bf16 four: 32 prompts of up to 512 rows 20.7 us, three 22.2, two 25.5.)
 template <int D, bool I8>
-__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 4))) paged_chunks_kernel(PagedArgs g) {
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(I8 && D == 64 ? 3 : 2, I8 && D == 64 ? 3 : 4))) paged_chunks_kernel(PagedArgs g) {
   constexpr int ROWS = 128, KEYS = 64, LEAST = 4;
   constexpr int RB = 2 * D, CH = RB / 16;             // bytes and chunks of a row in LDS
   constexpr int TILE = KEYS * RB;
@@ -48,7 +53,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 4))
 
   // this lane's row, and the blocks of the workgroup's that its wave's rows see: wave0 .. wave1 - 1
   const int m0 = u.tile * ROWS + wave * 32;
-  const int m = m0 + r32, m_ld = m < rows ? m : rows - 1, token = m_ld / g.group;
+  const int m = m0 + r32, m_ld = m < rows ? m : rows - 1, token = divided(m_ld, g.by_group);
   const int pos = m < rows ? before + token : -1;
   const int first = g.window > 0 ? pos - g.window + 1 : 0;
   const u16* q = g.q + (long long)(u.seq.first + token) * g.q_stride + (u.head * g.group + m_ld - token * g.group) * D;
@@ -58,8 +63,8 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 4))
   int wave0 = block1, wave1 = block0, wave_least = -1, wave_high = -1;
   if (m0 < rows) {
     const int last = (m0 + 32 < rows ? m0 + 32 : rows) - 1;
-    wave_least = __builtin_amdgcn_readfirstlane(before + m0 / g.group);
-    wave_high = __builtin_amdgcn_readfirstlane(before + last / g.group);
+    wave_least = __builtin_amdgcn_readfirstlane(before + divided(m0, g.by_group));
+    wave_high = __builtin_amdgcn_readfirstlane(before + divided(last, g.by_group));
     int wave_low = g.window > 0 ? wave_least - g.window + 1 : 0;
     if (wave_low < 0) wave_low = 0;
     wave0 = wave_low / KEYS > block0 ? wave_low / KEYS : block0;

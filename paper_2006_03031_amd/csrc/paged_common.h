@@ -14,6 +14,7 @@ struct PagedArgs {
   uint16_t* o;
   long long q_stride;
   int heads, group;    // query heads, and those that share a key head
+  Divisor by_group, by_heads;  // by `group`, by the heads of the cache
   int window;          // 0: none
   float a2;            // alpha log2 e
   float* part;         // [slots][rows][D] sums of parts, not divided
@@ -22,6 +23,9 @@ struct PagedArgs {
   int slots, target_units;
   int once;            // keys and values are loaded past the caches
 };
+
+// (A division is some 25 instructions, 0.05 us where a workgroup begins, one behind the other.)
+__device__ __forceinline__ int divided(int x, const Divisor& d) { return (int)(__umulhi(2u * (unsigned)x, d.magic) >> d.shift); }
 
 constexpr float kNothing = -3.0e38f;  // the reference of a row that has seen no key yet
 
@@ -112,7 +116,7 @@ template <int ROWS, int KEYS, int LEAST>
 __device__ __forceinline__ void find_unit(const PagedArgs& g, unsigned unit, int* shared) {
   const int lane = threadIdx.x & 63, G = g.cache.kv_heads;
   const int most = g.slots ? part_blocks<ROWS, KEYS, LEAST>(g) : 1000000000;
-  const unsigned want = unit / G;
+  const unsigned want = (unsigned)divided((int)unit, g.by_heads);
   const int head = (int)(unit - want * G);
   unsigned units = 0, cut_units = 0, cut_tiles = 0;  // of the sequences ahead
   bool found = false;
@@ -146,7 +150,7 @@ __device__ __forceinline__ void find_unit(const PagedArgs& g, unsigned unit, int
     if (!found && __any(here)) {
       found = true;
       if (here) {
-        const int rest = (int)(want - start), back = rest / parts;
+        const int rest = (int)(want - start), back = parts == 1 ? rest : rest / parts;
         shared[0] = 1;
         shared[1] = s;
         shared[2] = q.first;
@@ -188,10 +192,10 @@ template <int ROWS, int KEYS>
 __device__ __forceinline__ void unit_keys(const PagedArgs& g, const PagedUnit& u, int& low, int& high, int& block0, int& block1) {
   const int m0 = u.tile * ROWS, rows = u.seq.n * g.group, m1 = (m0 + ROWS < rows ? m0 + ROWS : rows) - 1;
   const int before = u.seq.length - u.seq.n;
-  high = before + m1 / g.group;                                             // the last key that a row of the tile sees
+  high = before + divided(m1, g.by_group);                                             // the last key that a row of the tile sees
   low = 0;
   if (g.window > 0) {
-    low = before + m0 / g.group - g.window + 1;                             // and the first
+    low = before + divided(m0, g.by_group) - g.window + 1;                             // and the first
     if (low < 0) low = 0;
   }
   low = __builtin_amdgcn_readfirstlane(low);
@@ -200,7 +204,13 @@ __device__ __forceinline__ void unit_keys(const PagedArgs& g, const PagedUnit& u
     block0 = block1 = 0;
     return;
   }
-  const int b0 = low / KEYS, nb = high / KEYS + 1 - b0, q = nb / u.parts, r = nb - q * u.parts;  // (the first r parts have one more)
+  const int b0 = low / KEYS, nb = high / KEYS + 1 - b0;
+  if (u.parts == 1) {
+    block0 = b0;
+    block1 = b0 + nb;
+    return;
+  }
+  const int q = nb / u.parts, r = nb - q * u.parts;  // (the first r parts have one more)
   block0 = __builtin_amdgcn_readfirstlane(b0 + u.part * q + (u.part < r ? u.part : r));
   block1 = __builtin_amdgcn_readfirstlane(block0 + q + (u.part < r ? 1 : 0));
 }
@@ -274,9 +284,9 @@ struct SpanWalk {
     u.parts = of(steps);
     const unsigned G = (unsigned)g.cache.kv_heads;
     const unsigned first = lane_value(upto, l) - (unsigned)u.tiles * (unsigned)u.parts * G;
-    const unsigned which = (at - first) / (unsigned)u.parts;
+    const unsigned which = u.parts == 1 ? at - first : (at - first) / (unsigned)u.parts;
     tile_at = first + which * (unsigned)u.parts;
-    u.tile = (int)(which / G);
+    u.tile = divided((int)which, g.by_heads);
     u.head = (int)(which - (unsigned)u.tile * G);
     x0 = at - tile_at;
     x1 = end - tile_at < (unsigned)u.parts ? end - tile_at : (unsigned)u.parts;
@@ -315,7 +325,7 @@ template <int ROWS, int D>
 __device__ __forceinline__ void careful_row(const PagedArgs& g, const PagedUnit& u, int m, int key0, int key1) {
   constexpr int P = D / 64;
   const int lane = threadIdx.x & 63;
-  const int token = m / g.group;
+  const int token = divided(m, g.by_group);
   const int p = u.seq.length - u.seq.n + token;
   int first = g.window > 0 ? p - g.window + 1 : 0, last = p;
   if (first < key0) first = key0;
@@ -470,7 +480,7 @@ __global__ void __launch_bounds__(256) paged_join_kernel(PagedArgs g) {
         acc += wave_sums[w][lane] * scale;
       }
     }
-    const int mm = tile * ROWS + row, tok = mm / g.group;
+    const int mm = tile * ROWS + row, tok = divided(mm, g.by_group);
     const float inv = item[8] - item[7] + tok < 0 ? 0.f : 1.0f / total;
     u16* o = g.o + ((long long)(item[6] + tok) * g.heads + head * g.group + mm - tok * g.group) * D + lane * P;
     if constexpr (P == 2)

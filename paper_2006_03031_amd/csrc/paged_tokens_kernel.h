@@ -18,13 +18,15 @@ namespace nimble {
 //   Loads:   direct global->LDS loads into the wave's own ring of two blocks, waited for by count: no barrier in the loop.  16 keys lie in one
 //            page, whose number is a scalar.  Chunk c of row r sits at c ^ swizzle(r).  Keys outside of what the tile sees repeat the
 //            nearest one that it does.
-//   Bound by memory where the cache is large: one token over 131001 keys, 8 heads of 128 in bf16, 88.5 us, 537 MB at 6.06 TB/s, of which 5.1 are the second
-// launch (a kernel that only reads reaches 6.4 to 6.5); 64 tokens over up to 8192 keys in 8 bits 108 us, 563 MB at 5.2 TB/s: two tiles a workgroup, whose
-// beginnings and ends nothing hides.  One token over 777 keys, 16 heads of 64: 8.5 us, a launch, three loads one behind the other for the unit,
+//   Bound by memory where the cache is large: one token over 131001 keys, 8 heads of 128 in bf16, 87.4 us, 537 MB at 6.1 TB/s, of which 5.1 are the second
+// launch (a kernel that only reads reaches 6.4 to 6.5); 64 tokens over up to 8192 keys in 8 bits 101 us, 563 MB at 5.6 TB/s: two tiles a workgroup, whose
+// beginnings and ends nothing hides.  One token over 777 keys, 16 heads of 64: 8.4 us, a launch, three loads one behind the other for the unit,
 // the wave's three blocks and the meeting of eight waves.
 // ---------------------------------------------------------------------------
+// (As many waves a SIMD as the LDS holds: with fewer the spans, one for each, go in two rounds.  64 tokens over 4096 keys, 16 heads of 64 in 8 bits, with three
+// of four 121 us, 100.  Told so the compiler also orders heads of 128 better: 64 tokens over up to 8192 keys 106.3 -> 101.0 us.)
 template <int D, bool I8, int WAVES>
-__global__ void __launch_bounds__(WAVES * 64) paged_tokens_kernel(PagedArgs g) {
+__global__ void __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu((D == 64 ? 2 : 1) * (I8 ? 2 : 1)))) paged_tokens_kernel(PagedArgs g) {
   constexpr int ROWS = 16, KEYS = 32, STEP = 8, T = WAVES * 64;
   constexpr int RB = D * (I8 ? 1 : 2);           // bytes of a key row
   constexpr int CH = RB / 16;                    // its chunks
@@ -64,7 +66,7 @@ __global__ void __launch_bounds__(WAVES * 64) paged_tokens_kernel(PagedArgs g) {
   // this lane's row
   const int m = u.tile * ROWS + r16, rows = u.seq.n * g.group;
   const int m_ld = m < rows ? m : rows - 1;
-  const int token = m_ld / g.group;
+  const int token = divided(m_ld, g.by_group);
   const int pos = m < rows ? u.seq.length - u.seq.n + token : -1;
   const int first = g.window > 0 ? pos - g.window + 1 : 0;
   const u16* q = g.q + (long long)(u.seq.first + token) * g.q_stride + (u.head * g.group + m_ld - token * g.group) * D;
@@ -213,9 +215,31 @@ __global__ void __launch_bounds__(WAVES * 64) paged_tokens_kernel(PagedArgs g) {
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the keys and the scales have been read)
       issue(K_TILE{}, next, slot);
     }
+    if (i + 2 < mine)
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * KL + VL) : "memory");
+    else if (i + 1 < mine)
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(KL + VL) : "memory");
+    else
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    // The values are read out of LDS ahead of the softmax, behind which their way would be waited for: one token over 777 keys 8.9 -> 8.7 us, 64 over up
+    // to 8192 in 8 bits 108.9 -> 107.5.
+    uint2 va[D / 16], vb[I8 ? 1 : D / 16];
+#pragma unroll
+    for (int x = 0; x < D / 16; ++x) {
+      if (I8) {
+        const int k8 = (lane & 15) >> 1;  // of 8 keys: 4 h + (0..3), 16 + 4 h + (0..3)
+        const int row = (k8 & 4) * 4 + h * 4 + (k8 & 3);
+        va[x] = lds_read_tr8(vs + row * RB + (x ^ v_swizzle(row)) * 16 + (lane & 1) * 8);
+      } else {
+        const int i4 = lane & 15;
+        const int row = h * 4 + (i4 >> 2);  // and 16 further: their swizzle is the same
+        const uint32_t at = vs + row * RB + ((2 * x + ((i4 & 3) >> 1)) ^ v_swizzle(row)) * 16 + (i4 & 1) * 8;
+        va[x] = lds_read_tr16(at), vb[x] = lds_read_tr16(at + 16 * RB);
+      }
+    }
     const int key0 = block * KEYS;
     // (a block that every row of the tile sees whole needs no mask; rows past the last see nothing and are not stored)
-    const int least = u.seq.length - u.seq.n + u.tile * ROWS / g.group;
+    const int least = u.seq.length - u.seq.n + divided(u.tile * ROWS, g.by_group);
     const bool edge = key0 + KEYS - 1 > least || (g.window > 0 && key0 <= high - g.window);
     if (edge) {
 #pragma unroll
@@ -266,27 +290,14 @@ __global__ void __launch_bounds__(WAVES * 64) paged_tokens_kernel(PagedArgs g) {
       pl[x] = pack_bf16x2(p0 - of_pair(ph[x], 0), p1 - of_pair(ph[x], 1));
     }
     const bf16x8 pf = as_bf16x8(make_uint4(ph[0], ph[1], ph[2], ph[3])), pf_low = as_bf16x8(make_uint4(pl[0], pl[1], pl[2], pl[3]));
-    if (i + 2 < mine)
-      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * KL + VL) : "memory");
-    else if (i + 1 < mine)
-      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(KL + VL) : "memory");
-    else
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
     for (int x = 0; x < D / 16; ++x) {
       bf16x8 vf;
       if (I8) {
-        const int k8 = (lane & 15) >> 1;  // of 8 keys: 4 h + (0..3), 16 + 4 h + (0..3)
-        const int row = (k8 & 4) * 4 + h * 4 + (k8 & 3);
-        const uint2 w = lds_read_tr8(vs + row * RB + (x ^ v_swizzle(row)) * 16 + (lane & 1) * 8);
-        const uint2 a = codes_to_bf16(w.x), b = codes_to_bf16(w.y);
+        const uint2 a = codes_to_bf16(va[x].x), b = codes_to_bf16(va[x].y);
         vf = as_bf16x8(make_uint4(a.x, a.y, b.x, b.y));
       } else {
-        const int i4 = lane & 15;
-        const int row = h * 4 + (i4 >> 2);  // and 16 further: their swizzle is the same
-        const uint32_t at = vs + row * RB + ((2 * x + ((i4 & 3) >> 1)) ^ v_swizzle(row)) * 16 + (i4 & 1) * 8;
-        const uint2 a = lds_read_tr16(at), b = lds_read_tr16(at + 16 * RB);
-        vf = as_bf16x8(make_uint4(a.x, a.y, b.x, b.y));
+        vf = as_bf16x8(make_uint4(va[x].x, va[x].y, vb[I8 ? 0 : x].x, vb[I8 ? 0 : x].y));
       }
       oacc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf, oacc[x], 0, 0, 0);
       oacc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf_low, oacc[x], 0, 0, 0);
@@ -349,7 +360,7 @@ __global__ void __launch_bounds__(WAVES * 64) paged_tokens_kernel(PagedArgs g) {
         if (c == 0) g.stat[to] = mine_stat[i];
         continue;
       }
-      const int tok = mm / g.group;
+      const int tok = divided(mm, g.by_group);
       const float inv = u.seq.length - u.seq.n + tok < 0 ? 0.f : 1.0f / mine_stat[i].y;
       u16* o = g.o + ((long long)(u.seq.first + tok) * g.heads + u.head * g.group + mm - tok * g.group) * D + c * 4;
       *(uint2*)o = make_uint2(pack_bf16x2(acc[i].x * inv, acc[i].y * inv), pack_bf16x2(acc[i].z * inv, acc[i].w * inv));
