@@ -1,7 +1,11 @@
 """Shape functions, refusals and the dispatch of rotary, cache_write, cache_read and paged_attention (no GPU needed)."""
 import ctypes
 import math
+import os
 import random
+import re
+import shutil
+import subprocess
 
 import pytest
 
@@ -280,3 +284,16 @@ def test_queries_without_elements_are_refused_by_their_shape():
     for shape in ((7, 4, 0), (7, 4, 32), (7, 3, 64), (7, 256)):
         with pytest.raises(nb.NimbleError):
             rt.paged_attention(torch.zeros(shape, dtype=torch.bfloat16), rt.PagedCache(k, k), batch)
+
+
+@pytest.mark.skipif(shutil.which("hipcc") is None, reason="hipcc not on PATH")
+def test_kernels_that_count_their_loads_have_no_others_under_way(tmp_path):
+    """They wait for loads to LDS by how many there are behind: registers that spill to memory would be counted too."""
+    from paper_2006_03031_amd import build
+    out = tmp_path / "paged.s"
+    subprocess.run(["hipcc", *build.FLAGS, "--cuda-device-only", "-S", os.path.join(build.CSRC, "paged_attention.hip"), "-o", str(out)], check=True,
+                   stdout=subprocess.PIPE, stderr=subprocess.STDOUT)
+    kernels = re.findall(r"\.amdhsa_kernel (\S+).*?\.amdhsa_private_segment_fixed_size (\d+)", out.read_text(), re.S)
+    counted = [(name, int(size)) for name, size in kernels if "paged_tokens_kernel" in name or "paged_chunks_kernel" in name]
+    assert len(counted) == 11
+    assert not [k for k in counted if k[1]]
