@@ -203,7 +203,7 @@ __device__ __forceinline__ void find_places(const CacheArgs& c, const SequencesA
 // f64, where a turned key is exact to 2^-50 or so: the code does not depend on how the quotient is computed, since one within 1e-12 of
 // the border of two is decided by the quotient itself.  Heads with an infinity or a NaN: codes 0, scale NaN.
 //   Bound by memory where there are many rows: 8448 of 16 + 16 + 16 heads of 64 in bf16 24.4 us, 104 MB at 4.3 TB/s.  61 rows of 32 + 8 + 8 heads of 128 in
-// 8 bits 6.0 us, four loads one behind the other (offsets, lengths, pages, table) and the f64 arithmetic of a head.
+// 8 bits 4.1 us (replayed in a graph), four loads one behind the other (offsets, lengths, pages, table) and the f64 arithmetic of a head.
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ int code_of(double x, double a, double inv) {
   const double t = x * inv;
@@ -222,11 +222,11 @@ __global__ void __launch_bounds__(256) cache_write_kernel(CacheWriteArgs g) {
   int a, b;
   chunks_of<INTERLEAVED>(l, INTERLEAVED ? 0 : g.R >> 3, a, b);
   const bool turned = g.table && l * 8 < g.R;
-  // Heads of all rows one after the other: this lane's, and the next 256 / LANES further.  A head is loaded ahead of its turn, the first ahead of
+  // Heads of all rows one after the other: this lane's, and the next 256 / LANES further (times the workgroups that share the rows).  A head is loaded ahead of its turn, the first ahead of
   // the places.
   constexpr int STEP = 256 / LANES;
-  const int step_r = STEP / heads, step_h = STEP - step_r * heads;
-  int next_h = threadIdx.x / LANES, next_r = next_h / heads;
+  const int step = STEP * gridDim.y, step_r = step / heads, step_h = step - step_r * heads;
+  int next_h = blockIdx.y * STEP + threadIdx.x / LANES, next_r = next_h / heads;
   next_h -= next_r * heads;
   Chunk next_a{}, next_b{};
   auto load = [&]() {
@@ -319,7 +319,7 @@ __global__ void __launch_bounds__(256) cache_read_kernel(CacheReadArgs g) {
   const int G = g.cache.kv_heads;
   const int beside = g.rows_each >= MOST ? MOST : 1;                    // rows of a wave; its other lanes have other heads
   const int c = threadIdx.x % LANES, x = threadIdx.x / LANES, r0 = x % beside, h0 = x / beside, step = 256 / LANES / beside;
-  for (int h = h0; h < 2 * G; h += step) {
+  for (int h = h0 + blockIdx.y * step; h < 2 * G; h += step * gridDim.y) {
     const int head = h < G ? h : h - G;
     const unsigned char* from = h < G ? g.cache.k : g.cache.v;
     const float* scales = h < G ? g.cache.k_scale : g.cache.v_scale;

@@ -160,6 +160,19 @@ def test_write(H, G, sizes, interleaved, D, rot, int8):
 
 
 @pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("H,G,D", [(33, 16, 128), (64, 64, 64), (300, 5, 128)])
+def test_few_rows_of_many_heads_are_written_by_several_workgroups(H, G, D, int8):
+    test_write(H, G, 0, False, D, D, int8)
+    test_write(H, G, len(SIZES) - 1, True, D, 16, int8)
+
+
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("D,G", [(128, 41), (64, 100)])
+def test_few_rows_of_many_heads_are_read_by_several_workgroups(D, G, int8):
+    test_read(D, G, 16, False, int8)
+
+
+@pytest.mark.parametrize("int8", [False, True])
 def test_write_without_queries_and_rows_without_a_place(int8):
     batch = Batch([(40, 3), (-2, 5), (20, 2), (30, 4)], 16, extra_columns=0)
     batch.pages[0, 2] = -1                   # dropped
