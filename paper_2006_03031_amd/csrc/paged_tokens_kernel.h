@@ -19,8 +19,8 @@ namespace nimble {
 //            page, whose number is a scalar.  Chunk c of row r sits at c ^ swizzle(r).  Keys outside of what the tile sees repeat the
 //            nearest one that it does.
 //   Bound by memory where the cache is large: one token over 131001 keys, 8 heads of 128 in bf16, 87.4 us, 537 MB at 6.1 TB/s, of which 5.1 are the second
-// launch (a kernel that only reads reaches 6.4 to 6.5); 64 tokens over up to 8192 keys in 8 bits 101 us, 563 MB at 5.6 TB/s: two tiles a workgroup, whose
-// beginnings and ends nothing hides.  One token over 777 keys, 16 heads of 64: 8.4 us, a launch, three loads one behind the other for the unit,
+// launch (a kernel that only reads reaches 6.4 to 6.5); 64 tokens over up to 8192 keys in 8 bits 99 us, 563 MB at 5.7 TB/s: two tiles a workgroup, whose
+// beginnings and ends nothing hides.  One token over 777 keys, 16 heads of 64: 7.5 us, a launch, three loads one behind the other for the unit,
 // the wave's three blocks and the meeting of eight waves.
 // ---------------------------------------------------------------------------
 // (As many waves a SIMD as the LDS holds: with fewer the spans, one for each, go in two rounds.  64 tokens over 4096 keys, 16 heads of 64 in 8 bits, with three
@@ -107,49 +107,60 @@ __global__ void __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu
     page = page < g.cache.pages ? page : g.cache.pages - 1;
     return (((long long)page * g.cache.kv_heads + u.head) << g.cache.page_shift) + (key & slot_mask);
   };
-  // Where a block's two times 16 keys are: rows of the cache, and which of each 16 are loaded as they are.
+  // Where a block's two times 16 keys are: rows of the cache, and whether all are loaded as they are.
   struct Place {
     long long row[2];
-    int lo[2], hi[2];
+    int key[2];
+    bool whole;
   };
   auto place_of = [&](int i) {  // of the wave's block i
     if (i && (i & 63) == 0) look_up(i);
+    const int key0 = (block0 + wave + i * WAVES) * KEYS;
     Place p;
+    p.whole = key0 >= low && key0 + KEYS - 1 <= high;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const int key = held_to((block0 + wave + i * WAVES) * KEYS + t * 16);
-      p.row[t] = group_row(i, t, key);
-      p.lo[t] = low - key > 0 ? low - key : 0;
-      p.hi[t] = high - key < 15 ? high - key : 15;
+      p.key[t] = held_to(key0 + t * 16);
+      p.row[t] = group_row(i, t, p.key[t]);
     }
     return p;
   };
+  // (One branch for all of a block's loads, and one for their kind: with one or two for each load they took half of the loop's instructions; one token
+  // over 777 keys 8.4 -> 7.5 us, 64 over up to 8192 in 8 bits 100.7 -> 98.8, chunks of 77 rows 13.4 -> 12.7.)
   auto issue = [&](auto is_v, const Place& p, int slot) {
     constexpr bool V = decltype(is_v)::value;
-    const uint32_t to = ring + slot * SLOT;
+    const uint32_t to = ring + slot * SLOT + V * TILE;
+    const unsigned char* from[2];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const unsigned char* from = uniform_pointer((V ? g.cache.v : g.cache.k) + p.row[t] * RB);
-      const bool whole = p.lo[t] == 0 && p.hi[t] == 15;
+    for (int t = 0; t < 2; ++t) from[t] = uniform_pointer((V ? g.cache.v : g.cache.k) + p.row[t] * RB);
+    auto nearest = [&](int t, int row) {  // the row that stands in for one of the 16
+      const int lo = low - p.key[t] > 0 ? low - p.key[t] : 0, hi = high - p.key[t] < 15 ? high - p.key[t] : 15;
+      return row < lo ? lo : row > hi ? hi : row;
+    };
+    if (!p.whole) {
 #pragma unroll
-      for (int n = 0; n < LOADS; ++n) {
-        uint32_t off = V ? v_off[n] : k_off[n];
-        if (!whole) {
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int n = 0; n < LOADS; ++n) {
           const int row = n * PER + load_row;
-          const int there = row < p.lo[t] ? p.lo[t] : row > p.hi[t] ? p.hi[t] : row;
-          off += (there - row) * RB;
+          dma16_so((V ? v_off[n] : k_off[n]) + (uint32_t)((nearest(t, row) - row) * RB), from[t], to + (t * LOADS + n) * 1024);
         }
-        const uint32_t at = to + V * TILE + (t * LOADS + n) * 1024;
-        if (g.once) dma16_so_once(off, from, at);
-        else dma16_so(off, from, at);
-      }
+    } else if (g.once) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int n = 0; n < LOADS; ++n) dma16_so_once(V ? v_off[n] : k_off[n], from[t], to + (t * LOADS + n) * 1024);
+    } else {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int n = 0; n < LOADS; ++n) dma16_so(V ? v_off[n] : k_off[n], from[t], to + (t * LOADS + n) * 1024);
     }
     if (I8 && !V) {  // lane -> scale of a key (0..31) or a value (32..63)
-      const int t = (lane >> 4) & 1, row = lane & 15;
-      const int l0 = t ? p.lo[1] : p.lo[0], h0 = t ? p.hi[1] : p.hi[0];
-      const int there = row < l0 ? l0 : row > h0 ? h0 : row;
-      const float* from = (lane < 32 ? g.cache.k_scale : g.cache.v_scale) + (t ? p.row[1] : p.row[0]) + there;
-      dma4(from, to + 2 * TILE);
+      const int t = (lane >> 4) & 1;
+      const int row0 = p.whole ? lane & 15 : nearest(0, lane & 15), row1 = p.whole ? lane & 15 : nearest(1, lane & 15);
+      const long long at0 = p.row[0] + row0, at1 = p.row[1] + row1;
+      dma4((lane < 32 ? g.cache.k_scale : g.cache.v_scale) + (t ? at1 : at0), to + 2 * TILE);
     }
   };
   using K_TILE = std::false_type;
