@@ -175,16 +175,9 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(I8 && 
   // chunk 2 dd + h of row 32 t + r: a row's first byte is a multiple of its length, so that the swizzle is one exclusive or
   typedef const __attribute__((address_space(3))) uint4* LdsPtr;
   const uint32_t k_at = ring + r32 * RB + (h ^ k_swizzle(r32)) * 16;
-  auto qk = [&](f32x16 (&s)[2], int slot, int dd) {
-    uint32_t at = k_at + slot * TILE;
-    asm volatile("" : "+v"(at));
-    const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const LdsPtr from = (LdsPtr)(uintptr_t)((at ^ (dd * 32)) + t * 32 * RB);
-      const bf16x8 kf = as_bf16x8(make_uint4(from->x, from->y, from->z, from->w));
-      s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[dd], dd == 0 ? zero : s[t], 0, 0, 0);
-    }
+  auto k_part = [&](int slot, int dd, int t) {
+    const LdsPtr from = (LdsPtr)(uintptr_t)(((k_at + slot * TILE) ^ (dd * 32)) + t * 32 * RB);
+    return as_bf16x8(make_uint4(from->x, from->y, from->z, from->w));
   };
   // Which of this lane's keys of a block its row sees: from `least` on `range` + 1, counted from the lane's first (one comparison each).
   struct Seen {
@@ -201,8 +194,22 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(I8 && 
     const int slot = i & 1, key0 = i * KEYS;
     const float* scales = (const float*)(lds + 4 * TILE) + slot * 2 * KEYS;
     f32x16 s[2];
+    // Read one step ahead of the matrix instructions, which the barrier keeps the compiler from undoing: 2048 tokens over 16384 keys, heads of 128 in bf16
+    // 505 -> 501 us, in 8 bits 609 -> 591; two ahead takes registers that heads of 64 need (21.2 -> 22.5, 32 prompts of up to 512).
+    const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    bf16x8 kf[2][2];
 #pragma unroll
-    for (int dd = 0; dd < D / 16; ++dd) qk(s, slot, dd);
+    for (int t = 0; t < 2; ++t) kf[0][t] = k_part(slot, 0, t);
+#pragma unroll
+    for (int dd = 0; dd < D / 16; ++dd) {
+      if (dd + 1 < D / 16) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) kf[(dd + 1) & 1][t] = k_part(slot, dd + 1, t);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int t = 0; t < 2; ++t) s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[dd & 1][t], qf[dd], dd == 0 ? zero : s[t], 0, 0, 0);
+    }
     const bool edge = key0 + KEYS - 1 > wave_least || (g.window > 0 && key0 <= wave_high - g.window);
     if (I8) {
 #pragma unroll
@@ -243,6 +250,22 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(I8 && 
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int z = 0; z < 4; ++z) {
+      // The values come out of LDS behind the exponentials, for which heads of 64 in bf16 have no registers (505 -> 498 us, with the keys' reads 496; in
+      // 8 bits, heads of 64, 434 -> 422).
+      constexpr bool AHEAD = D == 128 || I8;
+      uint2 values[NT][2];
+      auto read_values = [&]() {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          const uint32_t at = vs + v_off[t] + z * 16 * RB;
+          values[t][0] = lds_read_tr16(at);
+          values[t][1] = lds_read_tr16(at + 8 * RB);
+        }
+      };
+      if (AHEAD) {
+        read_values();
+        __builtin_amdgcn_sched_barrier(0);
+      }
       float p[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -265,10 +288,10 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(I8 && 
       }
       // (in bf16, which is as far off as the rounding of the result; in two, as few rows have it, the prompt took 679 us where this takes 510)
       const bf16x8 pf = as_bf16x8(make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7])));
+      if (!AHEAD) read_values();
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        const uint32_t at = vs + v_off[t] + z * 16 * RB;
-        const uint2 lo = lds_read_tr16(at), hi = lds_read_tr16(at + 8 * RB);
+        const uint2 lo = values[t][0], hi = values[t][1];
         oacc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(make_uint4(lo.x, lo.y, hi.x, hi.y)), pf, oacc[t], 0, 0, 0);
       }
     }
