@@ -15,12 +15,12 @@ namespace nimble {
 //   bf16:    direct global->LDS loads.  Chunk c of key row r sits at c ^ k_swizzle(r), of value row r at c ^ v_swizzle(r).
 //   8 bits:  codes go through registers, where they become bf16, which holds them exactly, once for the workgroup; a key's scale multiplies its
 //            scores, a value's its probability.
-//   Bound by the matrix products and by what the chip draws: 2048 tokens over 16384 keys, 32 heads of 128 over 8, 502 to 516 us, 1000 to 1026 TFLOP/s with random numbers;
+//   Bound by the matrix products and by what the chip draws: 2048 tokens over 16384 keys, 32 heads of 128 over 8, 494 to 525 us, 0.98 to 1.04 PFLOP/s with random numbers (by card);
 // with zeros, at a higher clock, 398 us, 1296 (the library's product of 8192^3 with random numbers 1307 to 1354).  Of LDS reads it needs as
 // much time as of matrix instructions (32 rows a wave).  Tried and slower: scores of block i + 1 ahead of the probabilities of block i (no gain, or spilled),
 // 64 rows a wave (868: accumulators move to and fro), eight waves over 256 rows in two phases (537 where this took 521),
 // the sum of the probabilities by a matrix instruction with ones (+ 5 %), a copy of the loop without masks (+ 9 %).  32 prompts of up to 512, 16 heads of 64:
-// 20.8 us, 69 MB at 3.3 TB/s: 1280 tiles of 1 to 8 blocks, of which 1024 are under way at once; a tile spends 1.3 us in finding itself and 1.7 to 2.9 until its
+// 21.3 us, 69 MB at 3.2 TB/s: 1280 tiles of 1 to 8 blocks, of which 1024 are under way at once; a tile spends 1.3 us in finding itself and 1.7 to 2.9 until its
 // first keys are there.
 // ---------------------------------------------------------------------------
 // (Heads of 64 in 8 bits: three waves a SIMD, with registers for what is converted; 2048 tokens over 16384 keys 439 us, two to four 466, four 684.  Of
