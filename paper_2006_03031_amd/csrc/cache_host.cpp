@@ -60,7 +60,10 @@ SequencesArgs sequences_args(const nimble_sequences& s) {
 
 // ------------------------------------------------------------------------------------------------ attention
 constexpr int kPagedRows[NIMBLE_PAGED_COUNT] = {16, 128};
-// Up to so many keys nothing is cut: the second launch costs more than a longer walk saves (one token over 777 keys of 64: 10.4 us cut, then 7.8).
+// Up to so many keys nothing is cut: the second launch costs more than a longer walk saves; half as many for few rows of bf16 heads of 128, which have four
+// waves for a walk and not eight.  One token, cut / not, us:  16 heads of 64 in bf16 over 800 keys 10.0 / 8.4, 1200 10.4 / 10.3, 2000 10.2 / 12.8; in 8 bits 1000
+// 10.0 / 10.2; 8 heads of 128 in 8 bits 800 11.3 / 11.2, 1000 11.4 / 12.6, in bf16 500 11.5 / 10.5, 800 11.6 / 13.7; of each of 64 sequences, 8 heads of 128
+// in 8 bits, 1000 27.0 / 25.5.
 constexpr int64_t kUncutKeys = 1024;
 constexpr int64_t kStepKeys = 256;   // of the tokens' spans
 // Waves of a workgroup, and workgroups that a compute unit holds at once, by their LDS (tokens) and registers: as many parts as fill the chip once
@@ -108,7 +111,8 @@ static int plan_paged(int64_t rows, int64_t count, int64_t width, int64_t heads,
   out.kernel = paged_kernel(rows * group, live, kv_heads, D, dtype, seen(kPagedRows[0]));
   out.rows = kPagedRows[out.kernel];
   const int64_t tiles = rows * group / out.rows + live, keys = seen(out.rows);   // a sequence adds at most one tile that is not full
-  out.parts = keys > kUncutKeys;
+  const bool four = four_waves_per_cu(D, dtype) == 1 && rows * group <= kPagedRows[0] * live;
+  out.parts = keys > (four ? kUncutKeys / 2 : kUncutKeys);
   const PagedWaves w = paged_waves(out.kernel, D, dtype, !out.parts && tiles * kv_heads <= kComputeUnits);
   const int64_t target = (int64_t)kComputeUnits * w.per_cu;
   out.block = 64u * (unsigned)w.waves;
