@@ -75,7 +75,7 @@ struct PagedWaves {
 };
 static int four_waves_per_cu(int64_t D, int dtype) { return (D == 128 ? 1 : 2) * (dtype == NIMBLE_I8 ? 2 : 1); }
 static PagedWaves paged_waves(int kernel, int64_t D, int dtype, bool lone) {
-  if (kernel == NIMBLE_PAGED_CHUNKS) return {4, 2};
+  if (kernel == NIMBLE_PAGED_CHUNKS) return {4, D == 64 ? 3 : 2};
   const int four = four_waves_per_cu(D, dtype);
   return lone && four > 1 ? PagedWaves{8, four / 2} : PagedWaves{4, four};
 }

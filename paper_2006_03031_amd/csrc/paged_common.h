@@ -20,7 +20,7 @@ struct PagedArgs {
   float* part;         // [slots][rows][D] sums of parts, not divided
   float2* stat;        // [slots][rows] their largest score (base 2) and sum of probabilities
   int* items;          // [0]: tiles that may have been cut, then kPagedItemWords each, from the second entry on
-  int slots, target_units;
+  int slots, target_units, fewer_units;  // (fewer_units: see part_blocks)
   int once;            // keys and values are loaded past the caches
 };
 
@@ -91,7 +91,9 @@ __device__ __forceinline__ void tile_work(const PagedArgs& g, const Sequence& q,
 }
 
 // The blocks of one part, give or take half as many: a tile is cut into as many parts as comes closest, since what is left of one that is a little too
-// long costs a part's prologue and a join.  The same in every lane of every wave of a call.
+// long costs a part's prologue and a join.  Fewer units where parts of as many as fit would be of less than 16 blocks (heads of 64, of which a compute unit holds
+// three and not two: 2048 rows over 16384 keys, 16 heads of 64 in bf16, 150 us with two to a compute unit, 136 with three, in 8 bits 231 and 196; 128 rows over
+// 30128 keys, 10 blocks a part, 36.9 and 40.2).  The same in every lane of every wave of a call.
 template <int ROWS, int KEYS, int LEAST>
 __device__ __forceinline__ int part_blocks(const PagedArgs& g) {
   const int lane = threadIdx.x & 63;
@@ -105,7 +107,10 @@ __device__ __forceinline__ int part_blocks(const PagedArgs& g) {
     }
   }
   total = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(wave_scan(total)), 63));
-  const float most = ceilf(total * (float)g.cache.kv_heads / (float)g.target_units) + 1.0f;
+  total *= (float)g.cache.kv_heads;
+  float most = total / (float)g.target_units;
+  if (most < 16.0f) most = total / (float)g.fewer_units;
+  most = ceilf(most) + 1.0f;
   return most < (float)LEAST ? LEAST : most > 1.0e9f ? 1000000000 : (int)most;
 }
 

@@ -85,6 +85,28 @@ def test_sequences_that_are_cut(H, G, D, sizes, int8):
     _check(_run(q, cache, batch), q, cache, batch)
 
 
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("D,window", [(64, 0), (128, 0), (64, 20000)])
+def test_many_rows_over_many_keys(D, window, int8):
+    """Parts of more than 16 blocks, of which heads of 64 have more: a sequence's 256 rows of each of 16 heads over 30056 keys."""
+    G, n, L = 16, 256, 30056
+    batch = Batch([(L - n, n)], 64)
+    cache, q = pu.random_cache(batch, G, D, int8), _q(batch, G, D)
+    got = _run(q, cache, batch, window=window).double()
+    page, slot = batch.slots(0, torch.arange(L))
+    positions, keys = torch.arange(L - n, L).cuda()[:, None], torch.arange(L).cuda()[None]
+    unseen = (keys > positions) | ((keys <= positions - window) if window else False)
+    for h in range(G):
+        k, v = (pu.values(cache, which)[page, h, slot].cuda() for which in range(2))
+        x = q[:, h].double().cuda()
+        w = torch.softmax((x @ k.t().contiguous() * D ** -0.5).masked_fill(unseen, -math.inf), 1)
+        want = w @ v
+        scores_off = (D + 4) * 2.0 ** -24 * D ** -0.5 * float((x.abs() @ k.abs().t().contiguous()).max())
+        step = pu.half_step(BF)
+        bound = step * want.abs() + (step + 2 * scores_off + 2.0 ** -18) * (w @ v.abs()) + 2.0 ** -124 * v.abs().sum(0)
+        assert bool(((got[:, h] - want).abs() <= bound).all()), h
+
+
 @pytest.mark.parametrize("count", [65, 300])
 def test_many_sequences(count):
     batch = Batch([(i * 7 % 90, i % 3) for i in range(count)], 16)

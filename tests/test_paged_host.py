@@ -217,7 +217,8 @@ def _check_parts(p, sizes, group, kv_heads, window, width_keys, target):
     total = 0.0
     for tiles, blocks in work:
         total = _f32(total + _f32(tiles * blocks))
-    most = min(max(4, math.ceil(_f32(_f32(total * kv_heads) / target)) + 1), 1 << 30) if p.parts else 1 << 30
+    per = [_f32(_f32(total * kv_heads) / units) for units in (target, min(target, 512))] if p.parts else None
+    most = min(max(4, math.ceil(per[per[0] < 16]) + 1), 1 << 30) if p.parts else 1 << 30
     units = slots = cut = 0
     for tiles, blocks in work:
         parts = max(1, (blocks + most // 2) // most)
