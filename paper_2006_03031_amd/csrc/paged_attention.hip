@@ -22,11 +22,16 @@ static void launch_paged(const PagedArgs& g, const nimble_paged_plan& p, bool in
     join(paged_join_kernel<128, D>);
   } else {
     constexpr int kWide = D == 128 ? 4 : 8;  // (of bf16: what the LDS holds)
-    const bool wide = p.block == 512;
-    if (int8 && wide) launch(paged_tokens_kernel<D, true, 8>);
-    else if (int8) launch(paged_tokens_kernel<D, true, 4>);
-    else if (wide) launch(paged_tokens_kernel<D, false, kWide>);
-    else launch(paged_tokens_kernel<D, false, 4>);
+    if (p.block == 512) {  // (nothing is cut)
+      if (int8) launch(paged_tokens_kernel<D, true, 8, false>);
+      else launch(paged_tokens_kernel<D, false, kWide, false>);
+    } else if (p.parts) {
+      if (int8) launch(paged_tokens_kernel<D, true, 4, true>);
+      else launch(paged_tokens_kernel<D, false, 4, true>);
+    } else {
+      if (int8) launch(paged_tokens_kernel<D, true, 4, false>);
+      else launch(paged_tokens_kernel<D, false, 4, false>);
+    }
     join(paged_join_kernel<16, D>);
   }
 }

@@ -229,7 +229,7 @@ __device__ __forceinline__ void unit_keys(const PagedArgs& g, const PagedUnit& u
 // the tile has.  (64 sequences of up to 8192 keys, uneven, as tiles cut into equal parts of at most a 512th of all: 144 us, 1.5 rounds
 // of workgroups; in spans 121.)
 // ---------------------------------------------------------------------------
-template <int ROWS, int KEYS, int STEP>
+template <int ROWS, int KEYS, int STEP, bool CUT>
 struct SpanWalk {
   const PagedArgs& g;
   int base;                // this lane's sequence is base + lane
@@ -248,7 +248,7 @@ struct SpanWalk {
     int blocks;
     tile_work<ROWS, KEYS>(g, q, tiles, blocks);
     steps = (blocks + STEP - 1) / STEP;
-    if (steps == 0 || !g.slots) steps = tiles > 0;  // rows that see nothing; without a workspace a tile is a step and so is a span
+    if (steps == 0 || !CUT) steps = tiles > 0;  // rows that see nothing; without a workspace a tile is a step and so is a span
     return (unsigned)tiles * (unsigned)steps * (unsigned)g.cache.kv_heads;  // (all of them fewer than 2^31: checked by the host)
   }
   __device__ __forceinline__ void load(int b) {
@@ -266,7 +266,7 @@ struct SpanWalk {
       load(0);
       total = lane_value(upto, 63);
     }
-    per = g.slots ? (total + (unsigned)g.target_units - 1) / (unsigned)g.target_units : 1;
+    per = CUT ? (total + (unsigned)g.target_units - 1) / (unsigned)g.target_units : 1;
     if (per == 0) per = 1;
     const unsigned long long from = (unsigned long long)w * per;
     none = from >= total;
@@ -286,7 +286,7 @@ struct SpanWalk {
     u.seq.n = of(q.n);
     u.seq.length = of(q.length);
     u.tiles = of(tiles);
-    u.parts = of(steps);
+    u.parts = CUT ? of(steps) : 1;
     const unsigned G = (unsigned)g.cache.kv_heads;
     const unsigned first = lane_value(upto, l) - (unsigned)u.tiles * (unsigned)u.parts * G;
     const unsigned which = u.parts == 1 ? at - first : (at - first) / (unsigned)u.parts;

@@ -14,18 +14,19 @@ namespace nimble {
 //   8 bits:  codes become bf16, which holds them exactly, behind the LDS reads; a key's scale multiplies its scores, a value's its
 //            probability.  A lane reads 16 codes of a key row where it reads 8 elements of bf16, so that the elements of a
 //            matrix instruction's k are taken from the row in another order, and those of q in the same.
-//   Work:    a workgroup walks its span of all tiles' blocks (SpanWalk).
+//   Work:    a workgroup walks its span of all tiles' blocks (SpanWalk); without CUT it has one tile (what is left out ahead of the loop and behind it: one token
+//            over 777 keys 7.55 -> 6.9 us, chunks of 77 rows 12.6 -> 12.0).
 //   Loads:   direct global->LDS loads into the wave's own ring of two blocks, waited for by count: no barrier in the loop.  16 keys lie in one
 //            page, whose number is a scalar.  Chunk c of row r sits at c ^ swizzle(r).  Keys outside of what the tile sees repeat the
 //            nearest one that it does.
 //   Bound by memory where the cache is large: one token over 131001 keys, 8 heads of 128 in bf16, 87.4 us, 537 MB at 6.1 TB/s, of which 5.1 are the second
 // launch (a kernel that only reads reaches 6.4 to 6.5); 64 tokens over up to 8192 keys in 8 bits 99 us, 563 MB at 5.7 TB/s: two tiles a workgroup, whose
-// beginnings and ends nothing hides.  One token over 777 keys, 16 heads of 64: 7.5 us, a launch, three loads one behind the other for the unit,
+// beginnings and ends nothing hides.  One token over 777 keys, 16 heads of 64: 6.9 us, a launch, three loads one behind the other for the unit,
 // the wave's three blocks and the meeting of eight waves.
 // ---------------------------------------------------------------------------
 // (As many waves a SIMD as the LDS holds: with fewer the spans, one for each, go in two rounds.  64 tokens over 4096 keys, 16 heads of 64 in 8 bits, with three
 // of four 121 us, 100.  Told so the compiler also orders heads of 128 better: 64 tokens over up to 8192 keys 106.3 -> 101.0 us.)
-template <int D, bool I8, int WAVES>
+template <int D, bool I8, int WAVES, bool CUT>
 __global__ void __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu((D == 64 ? 2 : 1) * (I8 ? 2 : 1)))) paged_tokens_kernel(PagedArgs g) {
   constexpr int ROWS = 16, KEYS = 32, STEP = 8, T = WAVES * 64;
   constexpr int RB = D * (I8 ? 1 : 2);           // bytes of a key row
@@ -45,20 +46,25 @@ __global__ void __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r16 = lane & 15, h = lane >> 4;
-  SpanWalk<ROWS, KEYS, STEP> walk(g, blockIdx.x);
-  if (g.slots && tid == 0) {
+  SpanWalk<ROWS, KEYS, STEP, CUT> walk(g, blockIdx.x);
+  if (CUT && tid == 0) {
     if (blockIdx.x == 0) g.items[0] = (int)gridDim.x;
     g.items[(1 + blockIdx.x) * kPagedItemWords] = 0;
   }
   if (walk.none) return;
-  for (bool again = true; again; again = walk.at < walk.end) {
+  for (bool again = true; again; again = CUT && walk.at < walk.end) {
   PagedUnit u;
   int low, high, block0, block1;
   unsigned x0, x1, tile_at;
   walk.next(u, x0, x1, tile_at);
-  u.slot = x0 == 0 && x1 == (unsigned)u.parts ? -1 : 2 * (int)blockIdx.x + (x0 == 0);
-  share_keys<ROWS, KEYS>(g, u, x0, x1, low, high, block0, block1);
-  if (x0 == 0 && x1 < (unsigned)u.parts && tid == 0) {
+  u.slot = !CUT || (x0 == 0 && x1 == (unsigned)u.parts) ? -1 : 2 * (int)blockIdx.x + (x0 == 0);
+  if (CUT) {
+    share_keys<ROWS, KEYS>(g, u, x0, x1, low, high, block0, block1);
+  } else {
+    u.part = 0;
+    unit_keys<ROWS, KEYS>(g, u, low, high, block0, block1);
+  }
+  if (CUT && x0 == 0 && x1 < (unsigned)u.parts && tid == 0) {
     const int last = (int)walk.owner(tile_at + u.parts - 1);
     put_item(g, u, (int)blockIdx.x, last - (int)blockIdx.x + 1, u.slot, 2 * ((int)blockIdx.x + 1), 2);
   }
