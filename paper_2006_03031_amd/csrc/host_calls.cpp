@@ -437,7 +437,7 @@ PyObject* cache_read(PyObject*, PyObject* const* args, Py_ssize_t n) {
 }
 
 // paged_attention(q, cache, sequences, alpha, window, out or None) -> o or None, with a workspace of its own.  One token of one sequence of 777:
-// 23.3 us a call through the steps, 7.4 here (the kernel's time).
+// 23.3 us a call through the steps, 6.9 here (the kernel's time).
 PyObject* paged_attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   if (n != 6 || !g_paged_attention || modes_active() || !PyFloat_CheckExact(args[3]) || !PyLong_CheckExact(args[4])) Py_RETURN_NONE;
