@@ -517,6 +517,7 @@ typedef struct nimble_paged_plan {
   int32_t rows;             /* rows of a tile                                                          */
   int32_t parts;            /* 1: sequences may be cut into parts, and a second launch joins them      */
   uint32_t grid, join_grid[2], block;
+  int32_t step;             /* of the first kernel, where parts: keys in which it counts what it shares */
   int64_t slots;            /* parts that the workspace holds                                          */
   uint64_t workspace_bytes;
 } nimble_paged_plan;

@@ -58,8 +58,8 @@ class _CCache(ctypes.Structure):
 
 class _CPagedPlan(ctypes.Structure):
     _fields_ = [("kernel", ctypes.c_int32), ("rows", ctypes.c_int32), ("parts", ctypes.c_int32),
-                ("grid", ctypes.c_uint32), ("join_grid", ctypes.c_uint32 * 2), ("block", ctypes.c_uint32), ("slots", ctypes.c_int64),
-                ("workspace_bytes", ctypes.c_uint64)]
+                ("grid", ctypes.c_uint32), ("join_grid", ctypes.c_uint32 * 2), ("block", ctypes.c_uint32), ("step", ctypes.c_int32),
+                ("slots", ctypes.c_int64), ("workspace_bytes", ctypes.c_uint64)]
 
 
 @dataclass
@@ -70,6 +70,7 @@ class PagedPlan:
     grid: int
     join_grid: Tuple[int, int]
     block: int
+    step: int
     slots: int
     workspace_bytes: int
 
@@ -470,7 +471,7 @@ def paged_attention_plan(rows: int, count: int, width: int, heads: int, kv_heads
                          window: int = 0) -> PagedPlan:
     c = _CPagedPlan()
     _check(load().nimble_paged_attention_plan_of(rows, count, width, heads, kv_heads, page, D, dtype, window, ctypes.byref(c)))
-    return PagedPlan(c.kernel, c.rows, c.parts, c.grid, (c.join_grid[0], c.join_grid[1]), c.block, c.slots, c.workspace_bytes)
+    return PagedPlan(c.kernel, c.rows, c.parts, c.grid, (c.join_grid[0], c.join_grid[1]), c.block, c.step, c.slots, c.workspace_bytes)
 
 
 # ---------------------------------------------------------------- device side

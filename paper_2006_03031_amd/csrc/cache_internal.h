@@ -37,6 +37,7 @@ constexpr int64_t kMostPagedGrid = 1 << 23;
 // Sequences are looked for 64 by 64 (SpanWalk, find_unit), positions and rows are 32-bit numbers.
 constexpr int64_t kMostSequences = 1 << 16, kMostPositions = 1ll << 30, kMostRows = 1ll << 24;
 constexpr int kPagedItemWords = 12;
+constexpr int kPagedBlockKeys = 32;  // of the kernel of few rows
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 

@@ -81,6 +81,7 @@ int nimble_paged_attention_dyn(const void* q, int64_t q_stride, const nimble_cac
   if (p.parts) {
     g.slots = (int)p.slots;
     g.target_units = (int)(p.slots - 8) / 2;  // (see plan_paged)
+    while ((kPagedBlockKeys << g.step_shift) < p.step) ++g.step_shift;
     g.fewer_units = g.target_units < 2 * kComputeUnits ? g.target_units : 2 * kComputeUnits;
     g.part = (float*)workspace;
     g.stat = (float2*)(g.part + p.slots * p.rows * cache->D);

@@ -21,6 +21,7 @@ struct PagedArgs {
   float2* stat;        // [slots][rows] their largest score (base 2) and sum of probabilities
   int* items;          // [0]: tiles that may have been cut, then kPagedItemWords each, from the second entry on
   int slots, target_units, fewer_units;  // (fewer_units: see part_blocks)
+  int step_shift;      // of the blocks of a step (SpanWalk)
   int once;            // keys and values are loaded past the caches
 };
 
@@ -225,11 +226,11 @@ __device__ __forceinline__ void unit_keys(const PagedArgs& g, const PagedUnit& u
 // number of them: the blocks of all tiles in a row, one sequence after the other, cut into spans of equal length, one a workgroup.  A span may
 // end one tile, hold several and begin another.  A workgroup leaves at most two parts: of the tile that another one began (slot 2 w) and of
 // the one that it begins (slot 2 w + 1); the second launch finds a cut tile by the workgroup that began it.
-//   Lengths are counted in steps of STEP blocks, a tile as many as the longest of its sequence; a share of them is that share of the blocks that
+//   Lengths are counted in steps of 2^step_shift blocks, a tile as many as the longest of its sequence; a share of them is that share of the blocks that
 // the tile has.  (64 sequences of up to 8192 keys, uneven, as tiles cut into equal parts of at most a 512th of all: 144 us, 1.5 rounds
 // of workgroups; in spans 121.)
 // ---------------------------------------------------------------------------
-template <int ROWS, int KEYS, int STEP, bool CUT>
+template <int ROWS, int KEYS, bool CUT>
 struct SpanWalk {
   const PagedArgs& g;
   int base;                // this lane's sequence is base + lane
@@ -247,8 +248,8 @@ struct SpanWalk {
     q = sequence_of(g.seqs, s, g.cache.page_shift);
     int blocks;
     tile_work<ROWS, KEYS>(g, q, tiles, blocks);
-    steps = (blocks + STEP - 1) / STEP;
-    if (steps == 0 || !CUT) steps = tiles > 0;  // rows that see nothing; without a workspace a tile is a step and so is a span
+    steps = CUT ? (blocks + (1 << g.step_shift) - 1) >> g.step_shift : 0;
+    if (steps == 0) steps = tiles > 0;  // rows that see nothing; without a workspace a tile is a step and so is a span
     return (unsigned)tiles * (unsigned)steps * (unsigned)g.cache.kv_heads;  // (all of them fewer than 2^31: checked by the host)
   }
   __device__ __forceinline__ void load(int b) {

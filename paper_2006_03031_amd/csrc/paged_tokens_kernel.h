@@ -28,7 +28,7 @@ namespace nimble {
 // of four 121 us, 100.  Told so the compiler also orders heads of 128 better: 64 tokens over up to 8192 keys 106.3 -> 101.0 us.)
 template <int D, bool I8, int WAVES, bool CUT>
 __global__ void __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu((D == 64 ? 2 : 1) * (I8 ? 2 : 1)))) paged_tokens_kernel(PagedArgs g) {
-  constexpr int ROWS = 16, KEYS = 32, STEP = 8, T = WAVES * 64;
+  constexpr int ROWS = 16, KEYS = kPagedBlockKeys, T = WAVES * 64;
   constexpr int RB = D * (I8 ? 1 : 2);           // bytes of a key row
   constexpr int CH = RB / 16;                    // its chunks
   constexpr int PER = 1024 / RB;                 // rows of one load
@@ -46,7 +46,7 @@ __global__ void __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r16 = lane & 15, h = lane >> 4;
-  SpanWalk<ROWS, KEYS, STEP, CUT> walk(g, blockIdx.x);
+  SpanWalk<ROWS, KEYS, CUT> walk(g, blockIdx.x);
   if (CUT && tid == 0) {
     if (blockIdx.x == 0) g.items[0] = (int)gridDim.x;
     g.items[(1 + blockIdx.x) * kPagedItemWords] = 0;

@@ -233,7 +233,7 @@ def _check_spans(p, sizes, group, kv_heads, window, width_keys, target):
     """The spans of the tokens' kernel: every step has a workgroup, every part a slot, and every cut tile is found by its first."""
     ends, at = [], 0
     for tiles, blocks in _tiles(p, sizes, group, window, width_keys, 32):
-        steps = (max(1, -(-blocks // 8)) if p.parts else 1) if tiles else 0
+        steps = (max(1, -(-blocks // (p.step // 32))) if p.parts else 1) if tiles else 0
         for _ in range(tiles * kv_heads):
             ends.append((at, at + steps))
             at += steps
