@@ -105,6 +105,11 @@ static int plan_paged(int64_t rows, int64_t count, int64_t width, int64_t heads,
   if (heads < 1 || heads > 65536 || heads % kv_heads) return fail(heads < 1 || heads > 65536 ? NIMBLE_ERR_ARG : NIMBLE_ERR_SHAPE, "%lld query heads over %lld of the cache", (long long)heads, (long long)kv_heads);
   if (window < 0) return fail(NIMBLE_ERR_ARG, "negative window");
   nimble_paged_plan out{};
+  if (rows == 0 || count == 0) {  // nothing is launched
+    out.rows = kPagedRows[0];
+    *p = out;
+    return NIMBLE_OK;
+  }
   const int64_t group = heads / kv_heads, live = count < rows ? count : rows;
   auto seen = [&](int64_t tile_rows) {  // the most keys that a tile can see
     const int64_t all = width * page;
