@@ -1,4 +1,4 @@
-// Device entry point of attention over a paged cache (kernels: paged_tokens_kernel.h, paged_chunks_kernel.h; the parts of long sequences: paged_common.h).
+// Device entry point of attention over a paged cache (kernels: paged_tokens_kernel.h, paged_chunks_kernel.h; the division of the work: paged_work.h).
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -60,17 +60,11 @@ int nimble_paged_attention_dyn(const void* q, int64_t q_stride, const nimble_cac
   if (p.workspace_bytes && (!workspace || workspace_bytes < p.workspace_bytes))
     return fail(NIMBLE_ERR_WORKSPACE, "paged_attention: workspace of %llu bytes needed", (unsigned long long)p.workspace_bytes);
   PagedArgs g{};
-  g.cache = cache_args(*cache);
-  g.seqs = sequences_args(*seqs);
-  if (cache->pages == 0) g.seqs.width = 0;  // nothing is cached
+  set_extents(g, *cache, *seqs, heads, window);
+  set_parts(g, p, cache->D, workspace);
   g.q = (const uint16_t*)q;
   g.o = (uint16_t*)o;
   g.q_stride = q_stride;
-  g.heads = (int)heads;
-  g.group = (int)(heads / cache->kv_heads);
-  g.by_group = divisor_of(g.group);
-  g.by_heads = divisor_of(cache->kv_heads);
-  g.window = (int)(window < kMostPositions ? window : 0);  // (2^30 and beyond: all)
   g.a2 = alpha * 1.4426950408889634f;
   if (!std::isfinite(g.a2)) return fail(NIMBLE_ERR_ARG, "paged_attention: alpha = %g is too large", (double)alpha);
   // Past the caches where each key is read by one workgroup and the page table has room for more than 8 MB: what a layer finds in memory, other
@@ -78,15 +72,6 @@ int nimble_paged_attention_dyn(const void* q, int64_t q_stride, const nimble_cac
   // cache, alone over and over, later (128 MB 33.6 -> 33.0, 34.3 -> 37.3, 256 MB 50.3 -> 53); a short sequence of one token 7.8 -> 8.6.
   g.once = p.kernel == NIMBLE_PAGED_TOKENS && seqs->rows * g.group <= p.rows * seqs->count &&
            (double)seqs->count * seqs->width * cache->page * cache->kv_heads * cache->D * (cache->dtype == NIMBLE_I8 ? 2 : 4) > 8e6;
-  if (p.parts) {
-    g.slots = (int)p.slots;
-    g.target_units = (int)(p.slots - 8) / 2;  // (see plan_paged)
-    while ((kPagedBlockKeys << g.step_shift) < p.step) ++g.step_shift;
-    g.fewer_units = g.target_units < 2 * kComputeUnits ? g.target_units : 2 * kComputeUnits;
-    g.part = (float*)workspace;
-    g.stat = (float2*)(g.part + p.slots * p.rows * cache->D);
-    g.items = (int*)(g.stat + p.slots * p.rows);
-  }
   if (cache->D == 64)
     launch_paged<64>(g, p, cache->dtype == NIMBLE_I8, (hipStream_t)stream);
   else

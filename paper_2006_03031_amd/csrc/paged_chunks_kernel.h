@@ -46,10 +46,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(I8 && 
   if (wave == 0) find_unit<ROWS, KEYS, LEAST>(g, blockIdx.x, unit);
   __syncthreads();
   PagedUnit u;
-  const bool found = take_unit(unit, u);
-  if (g.slots && blockIdx.x == 0 && tid == 0) g.items[0] = unit[11];
-  if (!found) return;
-  if (u.parts > 1 && (u.slot >= g.slots || u.item >= g.target_units)) return;  // (not with offsets that keep to their description)
+  if (!take_unit(g, unit, u)) return;
   int low, high, block0, block1;
   unit_keys<ROWS, KEYS>(g, u, low, high, block0, block1);
   const int rows = u.seq.n * g.group, before = u.seq.length - u.seq.n;
@@ -332,7 +329,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(I8 && 
       if (i >= wave0 && i < wave1) block(i);
     }
   }
-  if (u.parts > 1 && u.part == 0 && tid == 0) put_item(g, u, u.item, u.parts, u.slot, u.slot + g.cache.kv_heads, g.cache.kv_heads);
+  put_unit_item(g, u);
   if (m0 >= rows) return;
   if (!I8) {
     bool odd = false;

@@ -47,27 +47,12 @@ __global__ void __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r16 = lane & 15, h = lane >> 4;
   SpanWalk<ROWS, KEYS, CUT> walk(g, blockIdx.x);
-  if (CUT && tid == 0) {
-    if (blockIdx.x == 0) g.items[0] = (int)gridDim.x;
-    g.items[(1 + blockIdx.x) * kPagedItemWords] = 0;
-  }
+  walk.clear_item();
   if (walk.none) return;
   for (bool again = true; again; again = CUT && walk.at < walk.end) {
   PagedUnit u;
   int low, high, block0, block1;
-  unsigned x0, x1, tile_at;
-  walk.next(u, x0, x1, tile_at);
-  u.slot = !CUT || (x0 == 0 && x1 == (unsigned)u.parts) ? -1 : 2 * (int)blockIdx.x + (x0 == 0);
-  if (CUT) {
-    share_keys<ROWS, KEYS>(g, u, x0, x1, low, high, block0, block1);
-  } else {
-    u.part = 0;
-    unit_keys<ROWS, KEYS>(g, u, low, high, block0, block1);
-  }
-  if (CUT && x0 == 0 && x1 < (unsigned)u.parts && tid == 0) {
-    const int last = (int)walk.owner(tile_at + u.parts - 1);
-    put_item(g, u, (int)blockIdx.x, last - (int)blockIdx.x + 1, u.slot, 2 * ((int)blockIdx.x + 1), 2);
-  }
+  walk.take(u, low, high, block0, block1);
 
   // this lane's row
   const int m = u.tile * ROWS + r16, rows = u.seq.n * g.group;
