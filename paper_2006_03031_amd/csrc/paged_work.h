@@ -138,7 +138,9 @@ __device__ __forceinline__ void find_unit(const PagedArgs& g, unsigned unit, int
   const int head = (int)(unit - want * G);
   unsigned units = 0, cut_units = 0, cut_tiles = 0;  // of the sequences ahead
   bool found = false;
-  for (int base = 0; base < g.seqs.count && (!found || unit == 0); base += 64) {
+  // Offsets that fall give more units than the grid has workgroups.  Then there is nothing to join: parts of some tiles are computed by nobody.
+  const unsigned fit = (unsigned)divided((int)gridDim.x, g.by_heads);
+  for (int base = 0; base < g.seqs.count && (!found || (unit == 0 && units <= fit)); base += 64) {
     const int s = base + lane;
     Sequence q{0, 0, 0};
     int tiles = 0, blocks = 0;
@@ -189,7 +191,7 @@ __device__ __forceinline__ void find_unit(const PagedArgs& g, unsigned unit, int
   }
   if (lane == 0) {
     if (!found) shared[0] = 0;
-    shared[11] = (int)cut_tiles * G;
+    shared[11] = units <= fit ? (int)cut_tiles * G : 0;
   }
 }
 __device__ __forceinline__ bool take_unit(const PagedArgs& g, const int* shared, PagedUnit& u) {

@@ -32,7 +32,7 @@ def work(tmp_path_factory):
         S = len(lengths)
         plan = nb.paged_attention_plan(rows, S, width, heads, kv_heads, page, D, dtype, window)
         off, lens = (ctypes.c_int64 * len(offsets))(*offsets), (ctypes.c_int64 * max(S, 1))(*lengths)
-        room = 4 * plan.grid + 70000
+        room = 4 * plan.grid + 400000
         out = (ctypes.c_int64 * (len(FIELDS) * room))()
         items = (ctypes.c_int * (12 * (2 + plan.join_grid[0] + plan.grid)))(*[UNWRITTEN] * (12 * (2 + plan.join_grid[0] + plan.grid)))
         n = lib.paged_work(rows, S, width, heads, kv_heads, page, D, dtype, window, off, lens, stride, out, room, items)
@@ -121,3 +121,40 @@ def test_every_block_of_every_tile_has_one_workgroup(work):
         seen.add((got[0].kernel, got[0].parts, cut > 0, window > 0))
     assert {s[:3] for s in seen} >= {(0, 1, True), (0, 1, False), (0, 0, False), (1, 1, True), (1, 1, False), (1, 0, False)}
     assert (0, 1, True, True) in seen and (1, 1, True, True) in seen
+
+
+def falling(rng, rows, S):
+    """Offsets that do not keep to their description."""
+    kind = rng.randrange(4)
+    if kind == 0:
+        return [(s & 1) * rows for s in range(S + 1)]
+    if kind == 1:
+        return [rng.randint(0, rows) for _ in range(S + 1)]
+    if kind == 2:
+        return [rng.choice((0, rows, -5, rows + 7, -2 ** 63, 2 ** 63 - 1, rng.randint(0, rows))) for _ in range(S + 1)]
+    return sorted((rng.randint(0, rows) for _ in range(S + 1)), reverse=True)
+
+
+def test_cut_tiles_beyond_the_grid_are_not_joined(work):
+    """Sequences that share rows: more tiles than the grid was made for, so that parts of some are computed by nobody."""
+    rows, S = 2048, 129
+    offsets = [(s & 1) * rows for s in range(S)] + [16]
+    plan, records, items = work(offsets, [1] * (S - 1) + [16384], rows, 1024, 32, 8, 16, 64, nb.BF16)
+    assert plan.kernel == 1 and plan.parts
+    check_bounds(plan, records, items, rows, 4, 8)
+
+
+def test_falling_offsets_stay_inside(work):
+    rng = random.Random(5)
+    seen = set()
+    for _ in range(90):
+        S, rows = rng.choice((1, 2, 7, 64, 65, 300)), rng.choice((1, 16, 70, 500, 2048))
+        kv_heads, group, page = rng.choice((1, 2, 8)), rng.choice((1, 4, 7)), rng.choice((16, 256))
+        width = rng.choice((1, 100, 1000))
+        offsets = falling(rng, rows, S)
+        few = rng.random() < 0.5  # (a long sequence behind many short ones)
+        lengths = [1 if few and s < S - 2 else rng.choice((0, 1, width * page, rng.randint(0, width * page), -3, 2 ** 62)) for s in range(S)]
+        window = rng.choice((0, 0, 100, 3000))
+        got = work(offsets, lengths, rows, width, group * kv_heads, kv_heads, page, rng.choice((64, 128)), rng.choice((nb.BF16, nb.I8)), window)
+        seen.add((got[0].kernel, got[0].parts, check_bounds(*got, rows, group, kv_heads) > 0))
+    assert seen >= {(0, 1, True), (1, 1, True), (0, 0, False), (1, 0, False)}
