@@ -46,8 +46,11 @@ struct PagedUnit {
   int slot, item;  // in the workspace; slot -1: the tile was not cut
 };
 
-// Inclusive sums over the 64 lanes, in registers.
-template <typename T>
+// A sum that stays at the largest number where it would pass it.
+__device__ __forceinline__ unsigned held_sum(unsigned a, unsigned b) { return __builtin_elementwise_add_sat(a, b); }
+
+// Inclusive sums over the 64 lanes, in registers.  HELD: as held_sum, an instruction more a step.
+template <bool HELD = false, typename T>
 __device__ __forceinline__ T wave_scan(T x) {
   auto step = [&](auto ctrl, auto rows) {
     constexpr int C = decltype(ctrl)::value, R = decltype(rows)::value;
@@ -57,7 +60,8 @@ __device__ __forceinline__ T wave_scan(T x) {
     for (unsigned& y : w) y = (unsigned)__builtin_amdgcn_update_dpp(0, (int)y, C, R, 0xf, false);
     T y;
     __builtin_memcpy(&y, w, sizeof y);
-    x += y;
+    if constexpr (HELD) x = held_sum(x, y);
+    else x += y;
   };
   using std::integral_constant;
   step(integral_constant<int, 0x111>{}, integral_constant<int, 0xf>{});  // from 1, 2, 4 and 8 lanes below in a row of 16
@@ -281,23 +285,25 @@ struct SpanWalk {
     tile_work<ROWS, KEYS>(g, q, tiles, blocks);
     steps = CUT ? (blocks + (1 << g.step_shift) - 1) >> g.step_shift : 0;
     if (steps == 0) steps = tiles > 0;  // rows that see nothing; without a workspace a tile is a step and so is a span
-    return (unsigned)tiles * (unsigned)steps * (unsigned)g.cache.kv_heads;  // (all of them fewer than 2^31: checked by the host)
+    return (unsigned)tiles * (unsigned)steps * (unsigned)g.cache.kv_heads;  // (fewer than 2^31, of one sequence or of all: checked by the host)
   }
   __device__ __forceinline__ void load(int b) {
     base = b;
-    upto = ahead + wave_scan(look(b + (threadIdx.x & 63)));
+    upto = held_sum(ahead, wave_scan<true>(look(b + (threadIdx.x & 63))));
   }
   __device__ __forceinline__ SpanWalk(const PagedArgs& args, unsigned w) : g(args) {
     unsigned total = 0;
     ahead = 0;
     if (g.seqs.count > 64) {
-      for (int b = 0; b < g.seqs.count; b += 64) total += look(b + (threadIdx.x & 63));
-      total = lane_value(wave_scan(total), 63);
+      for (int b = 0; b < g.seqs.count; b += 64) total = held_sum(total, look(b + (threadIdx.x & 63)));
+      total = lane_value(wave_scan<true>(total), 63);
       load(0);
     } else {
       load(0);
       total = lane_value(upto, 63);
     }
+    // Sequences that share rows (offsets that fall) may have more steps than the host allows for: nobody has work then.
+    if (total > 0x7fffffffu) total = 0;
     per = CUT ? (total + (unsigned)g.target_units - 1) / (unsigned)g.target_units : 1;
     if (per == 0) per = 1;
     const unsigned long long from = (unsigned long long)w * per;

@@ -158,3 +158,14 @@ def test_falling_offsets_stay_inside(work):
         got = work(offsets, lengths, rows, width, group * kv_heads, kv_heads, page, rng.choice((64, 128)), rng.choice((nb.BF16, nb.I8)), window)
         seen.add((got[0].kernel, got[0].parts, check_bounds(*got, rows, group, kv_heads) > 0))
     assert seen >= {(0, 1, True), (1, 1, True), (0, 0, False), (1, 0, False)}
+
+
+@pytest.mark.parametrize("window", [0, 3000])
+@pytest.mark.parametrize("S,rows,keys", [(17, 256, 1 << 30), (65, 1024, 1 << 28), (129, 2048, 1 << 26)])
+def test_steps_past_32_bits_are_not_joined(work, S, rows, keys, window):
+    """Sequences that share rows, each over so many keys that the steps of all together pass 32 bits, by so little or so much."""
+    for last in (51200, 256, keys):
+        lengths = [keys] * (S - 1) + [last]
+        got = work([(s & 1) * rows for s in range(S + 1)], lengths, rows, keys // 1024, 8, 8, 1024, 128, nb.BF16, window)
+        assert got[0].kernel == 0 and got[0].parts
+        check_bounds(*got, rows, 1, 8)
