@@ -104,6 +104,7 @@ static int plan_paged(int64_t rows, int64_t count, int64_t width, int64_t heads,
   if (rc != NIMBLE_OK) return rc;
   if (heads < 1 || heads > 65536 || heads % kv_heads) return fail(heads < 1 || heads > 65536 ? NIMBLE_ERR_ARG : NIMBLE_ERR_SHAPE, "%lld query heads over %lld of the cache", (long long)heads, (long long)kv_heads);
   if (window < 0) return fail(NIMBLE_ERR_ARG, "negative window");
+  if (window >= kMostPositions) window = 0;  // all
   nimble_paged_plan out{};
   if (rows == 0 || count == 0) {  // nothing is launched
     out.rows = kPagedRows[0];

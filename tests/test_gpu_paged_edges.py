@@ -28,3 +28,16 @@ def test_an_idle_step_with_a_table_of_full_width(rows):
         graph.replay()
     torch.cuda.synchronize()
     assert bool((out == 8).all())
+
+
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("sizes", [[(300, 1), (20, 3)], [(5000, 1), (100, 2)], [(1500, 200)]])
+def test_a_window_beyond_all_positions_is_none(sizes, int8):
+    from paper_2006_03031_amd import runtime as rt
+    batch = Batch(sizes, 32)
+    cache = pu.to_gpu(pu.random_cache(batch, 2, 64, int8))
+    q = torch.randn(batch.rows, 4, 64, generator=torch.Generator().manual_seed(3)).to(BF).cuda()
+    seqs = batch.on_gpu()
+    want = rt.paged_attention(q, cache, seqs)
+    for window in (1 << 30, 1 << 62, 2 ** 63 - 1):
+        assert torch.equal(rt.paged_attention(q, cache, seqs, window=window), want)

@@ -28,3 +28,11 @@ def test_batches_without_sequences_are_checked_all_the_same():
         with pytest.raises(nb.NimbleError) as e:
             call()
         assert e.value.code == code
+
+
+@pytest.mark.parametrize("rows,count,width", [(7, 2, 5), (7, 2, 1000), (4000, 3, 1 << 26), (64, 64, 20000)])
+@pytest.mark.parametrize("window", [1 << 30, (1 << 30) + 1, 1 << 62, 2 ** 63 - 16, 2 ** 63 - 1])
+def test_a_window_beyond_all_positions_is_none(window, rows, count, width):
+    for D, dtype in ((64, nb.BF16), (128, nb.I8)):
+        args = (rows, count, width, 4, 2, 16, D, dtype)
+        assert nb.paged_attention_plan(*args, window) == nb.paged_attention_plan(*args, 0)
