@@ -201,7 +201,7 @@ __device__ __forceinline__ void find_places(const CacheArgs& c, const SequencesA
 // New rows into the cache.  A workgroup takes `rows_each` neighbouring rows of the batch; D / 16 lanes a head, of queries, keys and values alike, each
 // with two chunks as above.  8 bits: scale = a / 127, code = 127 x / a to the nearest integer, ties to even, with a = max |x| of the head, all of it in
 // f64, where a turned key is exact to 2^-50 or so: the code does not depend on how the quotient is computed, since one within 1e-12 of
-// the border of two is decided by the quotient itself.  Heads with an infinity or a NaN: codes 0, scale NaN.
+// the border of two is decided by the quotient itself.  Heads with an infinity or a NaN, or a scale beyond f32: codes 0, scale NaN.
 //   Bound by memory where there are many rows: 8448 of 16 + 16 + 16 heads of 64 in bf16 24.4 us, 104 MB at 4.3 TB/s.  61 rows of 32 + 8 + 8 heads of 128 in
 // 8 bits 4.1 us (replayed in a graph), four loads one behind the other (offsets, lengths, pages, table) and the f64 arithmetic of a head.
 // ---------------------------------------------------------------------------
@@ -286,7 +286,9 @@ __global__ void __launch_bounds__(256) cache_write_kernel(CacheWriteArgs g) {
     if (odd) top = INFINITY;
 #pragma unroll
     for (int o = LANES / 2; o > 0; o >>= 1) top = fmax(top, __shfl_xor(top, o, 64));  // (the lanes of a head take the same branches)
-    const bool finite = top < INFINITY;
+    // (a turned key may pass f32 where its scale does not: the quotient in f64 then; a scale that passes it too is no scale)
+    const float scale = top > (double)3.40282347e38f ? (float)(top / 127.0) : (float)top / 127.0f;
+    const bool finite = scale < INFINITY;
     const double inv = finite && top > 0 ? 127.0 / top : 0.0;
     uint32_t code[4] = {0, 0, 0, 0};
     if (inv > 0) {
@@ -300,7 +302,7 @@ __global__ void __launch_bounds__(256) cache_write_kernel(CacheWriteArgs g) {
     unsigned char* y = (kind == 1 ? g.cache.k : g.cache.v) + to * D;
     *(uint2*)(y + a * 8) = make_uint2(code[0], code[1]);
     *(uint2*)(y + b * 8) = make_uint2(code[2], code[3]);
-    if (l == 0) (kind == 1 ? g.cache.k_scale : g.cache.v_scale)[to] = finite ? (float)top / 127.0f : __uint_as_float(0x7fc00000u);
+    if (l == 0) (kind == 1 ? g.cache.k_scale : g.cache.v_scale)[to] = finite ? scale : __uint_as_float(0x7fc00000u);
   }
 }
 

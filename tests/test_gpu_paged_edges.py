@@ -41,3 +41,40 @@ def test_a_window_beyond_all_positions_is_none(sizes, int8):
     want = rt.paged_attention(q, cache, seqs)
     for window in (1 << 30, 1 << 62, 2 ** 63 - 1):
         assert torch.equal(rt.paged_attention(q, cache, seqs, window=window), want)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_scales_of_turned_keys_beyond_the_largest_number(interleaved, D):
+    """Pairs of the largest bf16 turned by an eighth of a circle are 1.41 times it, more than f32 holds; their scale, a 127th of that, is not."""
+    from paper_2006_03031_amd import runtime as rt
+    batch = Batch([(0, 3)], 16)
+    cache = pu.to_gpu(pu.random_cache(batch, 1, D, True))
+    g = torch.Generator().manual_seed(1)
+    most = torch.finfo(BF).max
+    k = (torch.randint(-4, 5, (3, 1, D), generator=g) / 4 * most).to(BF)
+    k[:, :, 0], k[:, :, 1], k[:, :, D // 2] = most, -most, -most
+    table = torch.full((3, D // 2, 2), 0.5 ** 0.5)
+    rt.cache_write(cache, k.cuda(), k.cuda(), batch.on_gpu(), table=table.cuda(), interleaved=interleaved)
+    page, slot = batch.slots(0, torch.arange(3))
+    for which, rows in ((0, pu.turned(k, table, interleaved)[0]), (1, k.double())):
+        codes, scales = cache[which].cpu()[page, :, slot], cache[2 + which].cpu()[page, :, slot]
+        top = rows.abs().amax(-1)
+        assert bool(((scales.double() - top / 127).abs() <= 2 * 2.0 ** -24 * top / 127).all())   # (two roundings to f32 at most)
+        assert bool(((codes.double() - 127 * rows / top[..., None]).abs() <= 0.5 + 1e-9).all())
+    assert bool((pu.turned(k, table, interleaved)[0].abs().amax(-1) > torch.finfo(torch.float32).max).all())
+    back = rt.cache_read(cache, batch.on_gpu(), 3, 1)[1]
+    assert bool(back.isfinite().all())
+
+
+def test_scales_that_no_number_holds():
+    """A table whose magnitude takes a 127th of the keys beyond f32: as keys that are infinite, codes 0 and a scale that is NaN."""
+    from paper_2006_03031_amd import runtime as rt
+    batch = Batch([(0, 2)], 16)
+    cache = pu.to_gpu(pu.random_cache(batch, 1, 64, True))
+    k = torch.full((2, 1, 64), 1e30, dtype=BF)
+    table = torch.tensor([1e12, 0.0]).expand(2, 32, 2).contiguous()
+    rt.cache_write(cache, k.cuda(), k.cuda(), batch.on_gpu(), table=table.cuda())
+    page, slot = batch.slots(0, torch.arange(2))
+    assert bool((cache.k.cpu()[page, :, slot] == 0).all()) and bool(cache.k_scale.cpu()[page, :, slot].isnan().all())
+    assert bool((cache.v.cpu()[page, :, slot] == 127).all()) and bool(cache.v_scale.cpu()[page, :, slot].isfinite().all())
