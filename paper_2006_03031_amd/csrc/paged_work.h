@@ -46,11 +46,8 @@ struct PagedUnit {
   int slot, item;  // in the workspace; slot -1: the tile was not cut
 };
 
-// A sum that stays at the largest number where it would pass it.
-__device__ __forceinline__ unsigned held_sum(unsigned a, unsigned b) { return __builtin_elementwise_add_sat(a, b); }
-
-// Inclusive sums over the 64 lanes, in registers.  HELD: as held_sum, an instruction more a step.
-template <bool HELD = false, typename T>
+// Inclusive sums over the 64 lanes, in registers.
+template <typename T>
 __device__ __forceinline__ T wave_scan(T x) {
   auto step = [&](auto ctrl, auto rows) {
     constexpr int C = decltype(ctrl)::value, R = decltype(rows)::value;
@@ -60,8 +57,7 @@ __device__ __forceinline__ T wave_scan(T x) {
     for (unsigned& y : w) y = (unsigned)__builtin_amdgcn_update_dpp(0, (int)y, C, R, 0xf, false);
     T y;
     __builtin_memcpy(&y, w, sizeof y);
-    if constexpr (HELD) x = held_sum(x, y);
-    else x += y;
+    x += y;
   };
   using std::integral_constant;
   step(integral_constant<int, 0x111>{}, integral_constant<int, 0xf>{});  // from 1, 2, 4 and 8 lanes below in a row of 16
@@ -142,9 +138,7 @@ __device__ __forceinline__ void find_unit(const PagedArgs& g, unsigned unit, int
   const int head = (int)(unit - want * G);
   unsigned units = 0, cut_units = 0, cut_tiles = 0;  // of the sequences ahead
   bool found = false;
-  // Offsets that fall give more units than the grid has workgroups.  Then there is nothing to join: parts of some tiles are computed by nobody.
-  const unsigned fit = (unsigned)divided((int)gridDim.x, g.by_heads);
-  for (int base = 0; base < g.seqs.count && (!found || (unit == 0 && units <= fit)); base += 64) {
+  for (int base = 0; base < g.seqs.count && (!found || unit == 0); base += 64) {
     const int s = base + lane;
     Sequence q{0, 0, 0};
     int tiles = 0, blocks = 0;
@@ -191,11 +185,14 @@ __device__ __forceinline__ void find_unit(const PagedArgs& g, unsigned unit, int
     if (g.slots) {
       cut_units += (unsigned)__builtin_amdgcn_readlane((int)b, 63);
       cut_tiles += (unsigned)__builtin_amdgcn_readlane((int)c, 63);
+      if (units > 1u << 30) units = 1u << 30;  // (only with offsets that fall; 64 sequences have fewer than 2^30)
     }
   }
+  // Offsets that fall give more units than the grid has workgroups.  Then there is nothing to join: parts of some tiles are computed by nobody.
+  if (g.slots && unit == 0 && units > (unsigned)divided((int)gridDim.x, g.by_heads)) cut_tiles = 0;
   if (lane == 0) {
     if (!found) shared[0] = 0;
-    shared[11] = units <= fit ? (int)cut_tiles * G : 0;
+    shared[11] = (int)cut_tiles * G;
   }
 }
 __device__ __forceinline__ bool take_unit(const PagedArgs& g, const int* shared, PagedUnit& u) {
@@ -261,6 +258,9 @@ __device__ __forceinline__ void share_keys(const PagedArgs& g, const PagedUnit& 
 // number of them: the blocks of all tiles in a row, one sequence after the other, cut into spans of equal length, one a workgroup.  A span may
 // end one tile, hold several and begin another.  A workgroup leaves at most two parts: of the tile that another one began (slot 2 w) and of
 // the one that it begins (slot 2 w + 1); the second launch finds a cut tile by the workgroup that began it.
+//   Sequences that share rows (offsets that fall) may have steps that pass 32 bits together.  A tile that the walk takes is one of its sequence all the same: the
+// sums ahead of it are not past `at`, the sum with it is, and one sequence has fewer than 2^31 steps, so that its own did not wrap.  But it may end behind
+// the last span, whose parts nobody has; then it is not joined.
 //   Lengths are counted in steps of 2^step_shift blocks, a tile as many as the longest of its sequence; a share of them is that share of the blocks that
 // the tile has.  (64 sequences of up to 8192 keys, uneven, as tiles cut into equal parts of at most a 512th of all: 144 us, 1.5 rounds
 // of workgroups; in spans 121.)
@@ -289,21 +289,19 @@ struct SpanWalk {
   }
   __device__ __forceinline__ void load(int b) {
     base = b;
-    upto = held_sum(ahead, wave_scan<true>(look(b + (threadIdx.x & 63))));
+    upto = ahead + wave_scan(look(b + (threadIdx.x & 63)));
   }
   __device__ __forceinline__ SpanWalk(const PagedArgs& args, unsigned w) : g(args) {
     unsigned total = 0;
     ahead = 0;
     if (g.seqs.count > 64) {
-      for (int b = 0; b < g.seqs.count; b += 64) total = held_sum(total, look(b + (threadIdx.x & 63)));
-      total = lane_value(wave_scan<true>(total), 63);
+      for (int b = 0; b < g.seqs.count; b += 64) total += look(b + (threadIdx.x & 63));
+      total = lane_value(wave_scan(total), 63);
       load(0);
     } else {
       load(0);
       total = lane_value(upto, 63);
     }
-    // Sequences that share rows (offsets that fall) may have more steps than the host allows for: nobody has work then.
-    if (total > 0x7fffffffu) total = 0;
     per = CUT ? (total + (unsigned)g.target_units - 1) / (unsigned)g.target_units : 1;
     if (per == 0) per = 1;
     const unsigned long long from = (unsigned long long)w * per;
@@ -355,8 +353,8 @@ struct SpanWalk {
       unit_keys<ROWS, KEYS>(g, u, low, high, block0, block1);
     }
     if (CUT && x0 == 0 && x1 < (unsigned)u.parts && threadIdx.x == 0) {
-      const int last = (int)owner(tile_at + u.parts - 1);
-      put_item(g, u, (int)blockIdx.x, last - (int)blockIdx.x + 1, u.slot, 2 * ((int)blockIdx.x + 1), 2);
+      const unsigned last = owner(tile_at + u.parts - 1);
+      if (last < gridDim.x) put_item(g, u, (int)blockIdx.x, (int)last - (int)blockIdx.x + 1, u.slot, 2 * ((int)blockIdx.x + 1), 2);
     }
   }
 };

@@ -104,7 +104,6 @@ static bool __any(bool x) { return __ballot(x) != 0; }
 static int __popcll(uint64_t x) { return __builtin_popcountll(x); }
 static int __ffsll(uint64_t x) { return __builtin_ffsll((long long)x); }
 static unsigned __umulhi(unsigned a, unsigned b) { return (unsigned)(((uint64_t)a * b) >> 32); }
-static unsigned __builtin_elementwise_add_sat(unsigned a, unsigned b) { return a + b < a ? ~0u : a + b; }
 static int __float_as_int(float x) {
   int i;
   memcpy(&i, &x, 4);
