@@ -434,7 +434,8 @@ int nimble_product_plan_of(int64_t R, int64_t E, int64_t N, int64_t K, int in_dt
  * unspecified content, but no access outside the tensors.  Pages may be shared by sequences that only read them; slots that two rows
  * of one call write hold either, or a mixture.
  * Rows of queries, keys and values may lie `stride` elements apart (a multiple of 8, not less than a row's heads * D), so that the parts of
- * one product's output are taken as they are.  Outputs must not overlap operands, but for what is said below. */
+ * one product's output are taken as they are.  Outputs must not overlap operands or each other,
+ * but for what is said below: refused (NIMBLE_ERR_ARG).  Rows that lie in each other's gaps, the same stride apart, do not overlap. */
 typedef struct nimble_sequences {
   const void* offsets;
   const void* lengths;

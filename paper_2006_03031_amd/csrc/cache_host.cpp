@@ -48,6 +48,41 @@ int check_sequences(const nimble_sequences* s, int64_t page) {
   return NIMBLE_OK;
 }
 
+// Rows that lie in each other's gaps share nothing; those of two strides are only taken for it where one lot lies behind the other.
+static bool share(const Extent& a, const Extent& b) {
+  if (!a.at || !b.at || a.rows <= 0 || b.rows <= 0 || a.bytes <= 0 || b.bytes <= 0) return false;
+  typedef __int128 Wide;
+  const Wide d = (Wide)(uintptr_t)b.at - (Wide)(uintptr_t)a.at;                        // of the first rows
+  if (d >= (Wide)(a.rows - 1) * a.stride + a.bytes || -d >= (Wide)(b.rows - 1) * b.stride + b.bytes) return false;
+  if (a.rows > 1 && b.rows > 1 && a.stride != b.stride) return true;
+  const Wide stride = a.rows > 1 ? a.stride : b.stride;
+  // rows i of a and j of b share bytes where d - a.bytes < (i - j) stride < d + b.bytes, -(b.rows - 1) <= i - j <= a.rows - 1
+  Wide k = d - a.bytes;
+  k = k >= 0 ? k / stride + 1 : -((-k - 1) / stride);                                  // the least i - j with more
+  if (k < -(b.rows - 1)) k = -(b.rows - 1);
+  return k <= a.rows - 1 && k * stride < d + b.bytes;
+}
+
+int check_apart(const char* what, std::initializer_list<Extent> outputs, std::initializer_list<Extent> operands) {
+  for (const Extent* o = outputs.begin(); o != outputs.end(); ++o) {
+    for (const Extent* x = o + 1; x != outputs.end(); ++x)
+      if (share(*o, *x)) return fail(NIMBLE_ERR_ARG, "%s: %s and %s overlap", what, o->name, x->name);
+    for (const Extent& x : operands)
+      if (share(*o, x)) return fail(NIMBLE_ERR_ARG, "%s: %s and %s overlap", what, o->name, x.name);
+  }
+  return NIMBLE_OK;
+}
+
+// One after the other: keys, values and, in 8 bits, their scales; the batch's offsets, lengths and pages.
+std::array<Extent, 4> cache_extents(const nimble_cache& c) {
+  const int64_t slots = c.pages * c.kv_heads * c.page, element = c.dtype == NIMBLE_I8 ? 1 : 2, scale = c.dtype == NIMBLE_I8 ? 4 : 0;
+  return {extent("the cache's keys", c.k, slots * c.D * element), extent("the cache's values", c.v, slots * c.D * element),
+          extent("the keys' scales", c.k_scale, slots * scale), extent("the values' scales", c.v_scale, slots * scale)};
+}
+std::array<Extent, 3> sequences_extents(const nimble_sequences& s) {
+  return {extent("offsets", s.offsets, (s.count + 1) * 8), extent("lengths", s.lengths, s.count * 8), extent("pages", s.pages, s.count * s.width * 4)};
+}
+
 CacheArgs cache_args(const nimble_cache& c) {
   CacheArgs a{(unsigned char*)c.k, (unsigned char*)c.v, (float*)c.k_scale, (float*)c.v_scale, (unsigned)c.pages, (int)c.kv_heads, 0};
   while ((1ll << a.page_shift) < c.page) ++a.page_shift;

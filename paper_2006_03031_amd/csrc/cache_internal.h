@@ -1,6 +1,9 @@
 // What the paged cache's operators share between host and device: arguments, limits.
 #ifndef NIMBLE_CACHE_INTERNAL_H_
 #define NIMBLE_CACHE_INTERNAL_H_
+#include <array>
+#include <initializer_list>
+
 #include "nimble_internal.h"
 
 namespace nimble {
@@ -40,6 +43,22 @@ constexpr int kPagedItemWords = 12;
 constexpr int kPagedBlockKeys = 32;  // of the kernel of few rows
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// `rows` rows of `bytes` bytes, `stride` bytes apart; nothing where `at` is null.
+struct Extent {
+  const char* name;
+  const void* at;
+  int64_t rows, bytes, stride;
+};
+inline Extent extent(const char* name, const void* at, int64_t bytes) { return Extent{name, at, 1, bytes, bytes}; }
+// Rows of bf16, in elements.  (Beyond 2^40 of them apart the second lies behind all memory as well.)
+inline Extent extent(const char* name, const void* at, int64_t rows, int64_t row, int64_t stride) {
+  return rows == 1 || stride == row ? extent(name, at, rows * row * 2) : Extent{name, at, rows, row * 2, (stride < 1ll << 40 ? stride : 1ll << 40) * 2};
+}
+// Outputs that share memory with an operand or with each other are refused.
+int check_apart(const char* what, std::initializer_list<Extent> outputs, std::initializer_list<Extent> operands);
+std::array<Extent, 4> cache_extents(const nimble_cache& c);
+std::array<Extent, 3> sequences_extents(const nimble_sequences& s);
 
 int check_hip_launch(const char* what);
 

@@ -99,6 +99,10 @@ int nimble_rotary_dyn(const void* x, int64_t x_stride, const void* positions, co
   if (misaligned(x, 2) || misaligned(y, 2) || misaligned(positions, 8) || misaligned(table, 8))
     return fail(NIMBLE_ERR_ALIGN, "x and y must be 2-byte aligned, positions and table 8-byte");
   if (x == y && T > 1 && x_stride != y_stride) return fail(NIMBLE_ERR_ARG, "rotary: in place with two strides");
+  const int rc = check_apart("rotary", {extent("y", y, T, H * D, y_stride)},
+                             {extent("x", x == y ? nullptr : x, T, H * D, x_stride), extent("positions", R ? positions : nullptr, T * 8),
+                              extent("the table", table, table_rows * R * 8)});
+  if (rc != NIMBLE_OK) return rc;
   const RotaryArgs g{(const uint16_t*)x, (const long long*)positions, (const float2*)table, (uint16_t*)y, (long long)x_stride, (long long)y_stride,
                      (long long)table_rows, (long long)T, (int)H, (int)D, (int)R};
   const bool whole = D % 16 == 0 && R % 8 == 0 && !misaligned(x) && !misaligned(y) && !misaligned(table) && (T == 1 || (x_stride % 8 == 0 && y_stride % 8 == 0));
@@ -135,6 +139,15 @@ int nimble_cache_write_dyn(const nimble_cache* cache, const nimble_sequences* se
   if (q && q == q_out && q_stride != heads * D) return fail(NIMBLE_ERR_ARG, "cache_write: queries in place have to be contiguous");
   if (misaligned(q_out) || misaligned(table)) return fail(NIMBLE_ERR_ALIGN, "device pointers must be 16-byte aligned");
   if (table && R > 0 && table_rows == 0) return fail(NIMBLE_ERR_SHAPE, "cache_write: a table without positions");
+  const auto [ck, cv, cks, cvs] = cache_extents(*cache);
+  const auto [offsets, lengths, pages] = sequences_extents(*seqs);
+  const int64_t T = seqs->rows, wide = heads * D, narrow = cache->kv_heads * D;
+  rc = check_apart("cache_write", {extent("out", q ? q_out : nullptr, T, wide, wide), ck, cv, cks, cvs},
+                   {extent("q", q == q_out ? nullptr : q, T, wide, q_stride), extent("k", k, T, narrow, k_stride),
+                    extent("v", v, T, narrow, v_stride), extent("the table", table, (table_rows < 1ll << 40 ? table_rows : 1ll << 40) * R * 8), offsets, lengths, pages});
+  if (rc == NIMBLE_OK && q == q_out)  // in place
+    rc = check_apart("cache_write", {ck, cv, cks, cvs}, {extent("q", q, T, wide, q_stride)});
+  if (rc != NIMBLE_OK) return rc;
   CacheWriteArgs g{};
   g.cache = cache_args(*cache);
   g.seqs = sequences_args(*seqs);
@@ -170,6 +183,11 @@ int nimble_cache_read_dyn(const nimble_cache* cache, const nimble_sequences* seq
   if (seqs->rows == 0 || seqs->count == 0) return NIMBLE_OK;
   if (!k_out || !v_out) return fail(NIMBLE_ERR_NULL, "null tensor pointer");
   if (misaligned(k_out) || misaligned(v_out)) return fail(NIMBLE_ERR_ALIGN, "device pointers must be 16-byte aligned");
+  const auto [ck, cv, cks, cvs] = cache_extents(*cache);
+  const auto [offsets, lengths, pages] = sequences_extents(*seqs);
+  const int64_t bytes = seqs->rows * cache->kv_heads * cache->D * (out_dtype == NIMBLE_F32 ? 4 : 2);
+  rc = check_apart("cache_read", {extent("k_out", k_out, bytes), extent("v_out", v_out, bytes)}, {ck, cv, cks, cvs, offsets, lengths, pages});
+  if (rc != NIMBLE_OK) return rc;
   const CacheReadArgs g{cache_args(*cache), sequences_args(*seqs), k_out, v_out, rows_each(seqs->rows, 16)};
   if (cache->D == 64)
     launch_read<64>(g, cache->dtype == NIMBLE_I8, out_dtype == NIMBLE_F32, (hipStream_t)stream);

@@ -59,6 +59,12 @@ int nimble_paged_attention_dyn(const void* q, int64_t q_stride, const nimble_cac
   if (((uintptr_t)o | (uintptr_t)workspace) & 15) return fail(NIMBLE_ERR_ALIGN, "device pointers must be 16-byte aligned");
   if (p.workspace_bytes && (!workspace || workspace_bytes < p.workspace_bytes))
     return fail(NIMBLE_ERR_WORKSPACE, "paged_attention: workspace of %llu bytes needed", (unsigned long long)p.workspace_bytes);
+  const auto [ck, cv, cks, cvs] = cache_extents(*cache);
+  const auto [offsets, lengths, pages] = sequences_extents(*seqs);
+  const int64_t row = heads * cache->D;
+  rc = check_apart("paged_attention", {extent("out", o, seqs->rows, row, row), extent("the workspace", workspace, (int64_t)p.workspace_bytes)},
+                   {extent("q", q, seqs->rows, row, q_stride), ck, cv, cks, cvs, offsets, lengths, pages});
+  if (rc != NIMBLE_OK) return rc;
   PagedArgs g{};
   set_extents(g, *cache, *seqs, heads, window);
   set_parts(g, p, cache->D, workspace);

@@ -448,7 +448,7 @@ def rotary(x: torch.Tensor, positions: torch.Tensor, table: torch.Tensor, interl
 def cache_write(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, sequences: Sequences, q: Optional[torch.Tensor] = None,
                 table: Optional[torch.Tensor] = None, interleaved: bool = False, out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
     """Keys and values k, v [T, kv_heads, D] of a batch's rows into their places of the cache; with a table (rotary_table) the keys are
-    turned by their positions first, and the queries q [T, heads, D] with them: returns these, contiguous (`out` may be q), or None without q.
+    turned by their positions first, and the queries q [T, heads, D] with them: returns these, contiguous (`out` may be q where that is), or None without q.
     An 8-bit cache holds each token and head as quantize_rows does.  k, v and q may be parts of wider rows."""
     r = _host_calls.cache_write(cache, k, v, sequences, q, table, interleaved, out)
     if r is not None:
@@ -499,7 +499,8 @@ def paged_attention(q: torch.Tensor, cache: PagedCache, sequences: Sequences, al
     """Attention of a batch's rows q [T, heads, D] over their sequences in the cache, what cache_write has just put there included: row i of a
     sequence, at position p, sees the keys max(0, p - window + 1) .. p (window = 0: all up to p); heads is a multiple of the cache's, whose
     heads / kv_heads query heads share keys.  alpha: 1 / sqrt(D) unless given.  A token of each sequence and chunks of many are served alike.
-    workspace: of nb.paged_attention_plan's size, for one call at a time; by default a new one, so that calls may overlap."""
+    out shares no memory with q or the cache.  workspace: of nb.paged_attention_plan's size, for one call at a time; by default a new one, so that calls
+    may overlap."""
     if workspace is None:
         o = _host_calls.paged_attention(q, cache, sequences, alpha if alpha is not None else q.shape[2] ** -0.5 if q.dim() == 3 and q.shape[2] else None, window, out)
         if o is not None:

@@ -166,6 +166,11 @@ static void chunks_body() {  // as paged_chunks_kernel takes its unit
   put_record(u, low, high, block0, block1);
 }
 
+// check_apart of two tensors: 0, or what a refusal returns.
+extern "C" int apart(int64_t a, int64_t a_rows, int64_t a_bytes, int64_t a_stride, int64_t b, int64_t b_rows, int64_t b_bytes, int64_t b_stride) {
+  return check_apart("", {Extent{"a", (void*)a, a_rows, a_bytes, a_stride}}, {Extent{"b", (void*)b, b_rows, b_bytes, b_stride}});
+}
+
 // Workgroups of one call, every `stride`-th from the first on (and all where stride is 1).  out: records of 14 numbers; items: the table that the second
 // launch reads, 1 + its workgroups (or more) entries of 12 words, filled by the caller with what an unwritten workspace holds.  Returns the number of records, or
 // a negative status.

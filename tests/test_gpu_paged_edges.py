@@ -78,3 +78,35 @@ def test_scales_that_no_number_holds():
     page, slot = batch.slots(0, torch.arange(2))
     assert bool((cache.k.cpu()[page, :, slot] == 0).all()) and bool(cache.k_scale.cpu()[page, :, slot].isnan().all())
     assert bool((cache.v.cpu()[page, :, slot] == 127).all()) and bool(cache.v_scale.cpu()[page, :, slot].isfinite().all())
+
+
+def test_parts_of_one_buffer_that_do_not_overlap():
+    """Outputs beside operands: heads of the same wider rows, in place, behind each other in one allocation."""
+    import paper_2006_03031_amd as nb
+    from paper_2006_03031_amd import runtime as rt
+    batch = Batch([(40, 3), (0, 9)], 16)
+    T, H, G, D = batch.rows, 4, 2, 64
+    rows = torch.randn(T, 2 * H + 2 * G, D, generator=torch.Generator().manual_seed(1)).to(BF).cuda()
+    q, k, v, y = rows.split([H, G, G, H], 1)
+    table, positions = pu.angles(60, D).float().cuda(), torch.arange(T, device="cuda")
+    for _ in range(2):  # (through the steps, then natively)
+        want = rt.rotary(q.contiguous(), positions, table)
+        assert rt.rotary(q, positions, table, out=y) is y and torch.equal(y, want)
+        x = q.contiguous()
+        assert rt.rotary(x, positions, table, out=x) is x and torch.equal(x, want)
+        cache, seqs = pu.to_gpu(pu.random_cache(batch, G, D, False)), batch.on_gpu()
+        turned = rt.cache_write(cache, k, v, seqs, q=q, table=table)
+        one = torch.empty(2, T, H, D, dtype=BF, device="cuda")
+        one[0] = q
+        assert torch.equal(rt.cache_write(cache, k, v, seqs, q=one[0], table=table, out=one[0]), turned)
+        one[0] = q
+        assert torch.equal(rt.cache_write(cache, k, v, seqs, q=one[0], table=table, out=one[1]), turned)
+        assert torch.equal(rt.paged_attention(one[1], cache, seqs, out=one[0]), rt.paged_attention(turned, cache, seqs))
+        shared = rt.PagedCache(cache.k, cache.k)  # keys that are the values
+        assert torch.equal(rt.paged_attention(turned, shared, seqs), rt.paged_attention(turned, rt.PagedCache(cache.k, cache.k.clone()), seqs))
+        for call in (lambda: rt.paged_attention(turned, cache, seqs, out=turned), lambda: rt.cache_write(shared, k, v, seqs),
+                     lambda: rt.cache_write(cache, k, v, seqs, q=one[0], out=one.view(-1, H, D)[1:T + 1]),
+                     lambda: rt.cache_read(cache, seqs, T, out=(one[0, :, :G].contiguous(),) * 2)):
+            with pytest.raises(nb.NimbleError) as e:
+                call()
+            assert e.value.code == -8 and "overlap" in str(e.value)

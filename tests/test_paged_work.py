@@ -17,16 +17,21 @@ FIELDS = "workgroup s first n length tile head slot parts part low high block0 b
 
 
 @pytest.fixture(scope="module")
-def work(tmp_path_factory):
+def lib(tmp_path_factory):
     out = str(tmp_path_factory.mktemp("work") / "paged_work.so")
     here = os.path.dirname(os.path.abspath(__file__))
     subprocess.run(["g++", "-O1", "-U_FORTIFY_SOURCE", "-std=c++17", "-fPIC", "-shared", "-I" + os.path.join(build.ROOT, "include"), "-I" + build.CSRC,
                     os.path.join(here, "paged_work_cpu.cpp"), os.path.join(build.CSRC, "cache_host.cpp"), "-o", out], check=True)
     lib = ctypes.CDLL(out)
+    lib.apart.argtypes = [ctypes.c_int64] * 8
     i64, p = ctypes.c_int64, ctypes.c_void_p
     lib.paged_work.argtypes = [i64] * 7 + [ctypes.c_int, i64, p, p, i64, p, i64, p]
     lib.paged_work.restype = i64
+    return lib
 
+
+@pytest.fixture(scope="module")
+def work(lib):
     def run(offsets, lengths, rows, width, heads, kv_heads, page, D, dtype, window=0, stride=1):
         """(plan, records of all workgroups, table of the second launch)"""
         S = len(lengths)
@@ -169,3 +174,29 @@ def test_steps_past_32_bits_are_not_joined(work, S, rows, keys, window):
         got = work([(s & 1) * rows for s in range(S + 1)], lengths, rows, keys // 1024, 8, 8, 1024, 128, nb.BF16, window)
         assert got[0].kernel == 0 and got[0].parts
         check_bounds(*got, rows, 1, 8)
+
+
+def test_tensors_that_share_memory(lib):
+    """Whether rows of bytes share one, against the sets of their addresses."""
+    rng = random.Random(3)
+    seen = set()
+    for _ in range(20000):
+        a_rows, b_rows = rng.choice((1, 1, 2, 3, 7)), rng.choice((1, 2, 5))
+        a_bytes, b_bytes = rng.randint(1, 9), rng.randint(1, 9)
+        stride = rng.randint(max(a_bytes, b_bytes), 40)
+        a, b = 1000, 1000 + rng.randint(-150, 150)
+        sets = [{at + i * stride + x for i in range(rows) for x in range(n)} for at, rows, n in ((a, a_rows, a_bytes), (b, b_rows, b_bytes))]
+        refused = lib.apart(a, a_rows, a_bytes, stride, b, b_rows, b_bytes, stride) != 0
+        assert refused == bool(sets[0] & sets[1])
+        inside = max(sets[0]) >= min(sets[1]) and max(sets[1]) >= min(sets[0])
+        seen.add((refused, inside))
+        # of two strides: refused where one does not lie behind the other
+        other = stride + rng.randint(1, 5)
+        sets[1] = {b + j * other + x for j in range(b_rows) for x in range(b_bytes)}
+        inside = max(sets[0]) >= min(sets[1]) and max(sets[1]) >= min(sets[0])
+        refused = lib.apart(a, a_rows, a_bytes, stride, b, b_rows, b_bytes, other) != 0
+        assert refused == (inside if a_rows > 1 and b_rows > 1 else bool(sets[0] & sets[1]))
+    assert seen == {(True, True), (False, True), (False, False)}
+    assert lib.apart(0, 1, 10, 10, 0, 1, 10, 10) == 0 and lib.apart(4096, 0, 10, 10, 4096, 1, 10, 10) == 0
+    far = 2 ** 62
+    assert lib.apart(4096, 2 ** 31, 2, 2 ** 41, 8192, 2 ** 31, 2, 2 ** 41) == 0 and lib.apart(far, 2 ** 31, 2 ** 40, 2 ** 41, 4096, 2 ** 31, 2 ** 40, 2 ** 41) != 0
