@@ -477,15 +477,16 @@ int nimble_rotary_table_dyn(void* table, int64_t positions, int64_t rot, double 
 /* Rotary positions: y[t,h] is x[t,h] with its first 2R elements turned in pairs, the rest copied.  With (c,s) = table[positions[t], i]:
  *   y_a = x_a c - x_b s,  y_b = x_b c + x_a s,   (a,b) = (i, i+R), or (2i, 2i+1) where interleaved != 0;   i = 0 .. R-1.
  * x, y [T,H,D] bf16 (y may be x), rows x_stride and y_stride elements apart, any D and R with 2R <= D; positions [T] int64 (held to
- * 0..table_rows-1), table [table_rows, R, 2] f32.  f32, rounded once.  Aligned heads of whole 32 bytes with R a
- * multiple of 8 are the fast ones; other widths, alignments and strides are taken too: x and y need 2 bytes, table and positions 8. */
+ * 0..table_rows-1), table [table_rows, R, 2] f32.  f32, off by 2^-23 (|x_a c| + |x_b s|) at most, then rounded to bf16.  Aligned heads of
+ * whole 32 bytes with R a multiple of 8 are the fast ones; other widths, alignments and strides are taken too: x and y need 2 bytes, table
+ * and positions 8. */
 int nimble_rotary_dyn(const void* x, int64_t x_stride, const void* positions, const void* table, int64_t table_rows, void* y,
                       int64_t y_stride, int64_t T, int64_t H, int64_t D, int64_t R, int interleaved, void* stream);
 
 /* Keys and values of new rows into the cache, k turned by its position first where table is given (R a multiple of 8; 2R <= D), and the
  * queries with them: q_out = rotary(q) where q is given (q_out [rows, heads, D] contiguous, may be q itself; with no table a copy).
  * bf16: rotary's rounding.  int8: the codes and scales of nimble_quantize_rows_dyn for each token and head, of the turned keys before any
- * rounding.  Rows at positions below 0, or that the page table does not reach, or whose page is not one of the cache's, are not written. */
+ * rounding (a head whose scale no f32 holds is as one with an infinity: codes 0, scale NaN).  Rows at positions below 0, or that the page table does not reach, or whose page is not one of the cache's, are not written. */
 int nimble_cache_write_dyn(const nimble_cache* cache, const nimble_sequences* seqs, const void* k, int64_t k_stride, const void* v,
                            int64_t v_stride, const void* q, int64_t q_stride, void* q_out, int64_t heads, const void* table,
                            int64_t table_rows, int64_t R, int interleaved, void* stream);

@@ -100,8 +100,11 @@ constexpr int kPagedRows[NIMBLE_PAGED_COUNT] = {16, 128};
 // 10.0 / 10.2; 8 heads of 128 in 8 bits 800 11.3 / 11.2, 1000 11.4 / 12.6, in bf16 500 11.5 / 10.5, 800 11.6 / 13.7; of each of 64 sequences, 8 heads of 128
 // in 8 bits, 1000 27.0 / 25.5.
 constexpr int64_t kUncutKeys = 1024;
-// Spans of few rows are counted in so many keys; in half as many where not even all keys that there is room for give every workgroup a span (one token
-// over 2000 keys, 8 heads of 128 in bf16 12.0 -> 11.6 us, over 4000 13.4 -> 12.0, in 8 bits 12.5 -> 11.5; 64 over up to 8192 98.8, with half 100.1: more is cut).
+// Spans of few rows are counted in so many keys; in half as many where a tile has up to 4 rows, whose parts are joined by a workgroup a row, and even then no more
+// spans than compute units, of up to 4096 keys, so that no row has more than 32 parts.  Microseconds, 256 / 128 keys a step: one token over 2000 keys, 32 heads of 128
+// over 8, 12.3 / 11.6, over 4000 13.2 / 12.2, in 8 bits 11.1 / 10.8 and 12.2 / 11.7; 16 heads of 64 over 2000 in 8 bits 10.4 / 9.8.  Beyond: over 8000 keys 14.5 / 15.7, in
+// 8 bits 13.2 / 14.2; of two sequences over 4000 in 8 bits 13.0 / 15.6; tiles of 8 rows, 16 heads of 64 in 8 bits, over 2000 11.1 / 11.5, over 4000 12.7 / 17.1, of 16
+// rows 13.5 / 19.9; 64 tokens over up to 8192 98.9 / 100.2.
 constexpr int64_t kStepKeys = 256;
 // Waves of a workgroup, and workgroups that a compute unit holds at once, by their LDS (tokens) and registers: as many parts as fill the chip once
 // are aimed at.  Tokens: four waves where workgroups share a compute unit, so that one loads while another joins its waves' sums and goes over to
@@ -165,7 +168,8 @@ static int plan_paged(int64_t rows, int64_t count, int64_t width, int64_t heads,
   if (out.parts) {
     // tokens: a span a workgroup, with two parts; chunks: a unit a workgroup, tiles and as many more as the cuts make
     const bool spans = out.kernel == NIMBLE_PAGED_TOKENS;
-    out.step = (int32_t)(spans ? tiles * kv_heads * ceil_div(keys, kStepKeys) <= target ? kStepKeys / 2 : kStepKeys : 0);
+    const bool halves = rows * group <= 4 * live && keys <= 4096 && tiles * kv_heads * ceil_div(keys, kStepKeys / 2) <= kComputeUnits;
+    out.step = (int32_t)(spans ? halves ? kStepKeys / 2 : kStepKeys : 0);
     out.grid = (uint32_t)(spans ? target : tiles * kv_heads + target);
     out.slots = 2 * target + 8;
     const int64_t most = rows * group < out.rows ? rows * group : out.rows;

@@ -92,3 +92,13 @@ def test_rows_that_lie_over_each_other_are_refused(call, change, kw):
     with pytest.raises(nb.NimbleError) as e:
         call({**AT, **change}, **kw)
     assert e.value.code == -8 and "overlap" in str(e.value)
+
+
+@pytest.mark.parametrize("rows,count,keys,heads,kv_heads,D,dtype,step", [
+    (1, 1, 2000, 32, 8, 128, nb.BF16, 128), (1, 1, 4000, 32, 8, 128, nb.I8, 128), (1, 1, 2000, 16, 16, 64, nb.I8, 128), (4, 4, 2000, 8, 2, 64, nb.I8, 128),
+    (1, 1, 8000, 32, 8, 128, nb.BF16, 256), (2, 2, 4000, 32, 8, 128, nb.I8, 256), (2, 1, 2000, 32, 8, 128, nb.I8, 256), (8, 1, 4000, 16, 16, 64, nb.I8, 256),
+    (64, 64, 2000, 32, 8, 128, nb.I8, 256), (16, 1, 4000, 16, 16, 64, nb.BF16, 256)])
+def test_steps_of_few_rows(rows, count, keys, heads, kv_heads, D, dtype, step):
+    """Short ones where tiles have up to 4 rows, and spans are few."""
+    p = nb.paged_attention_plan(rows, count, -(-keys // 16), heads, kv_heads, 16, D, dtype)
+    assert (p.kernel, p.parts, p.step) == (0, 1, step)
