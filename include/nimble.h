@@ -486,7 +486,8 @@ int nimble_rotary_dyn(const void* x, int64_t x_stride, const void* positions, co
 /* Keys and values of new rows into the cache, k turned by its position first where table is given (R a multiple of 8; 2R <= D), and the
  * queries with them: q_out = rotary(q) where q is given (q_out [rows, heads, D] contiguous, may be q itself; with no table a copy).
  * bf16: rotary's rounding.  int8: the codes and scales of nimble_quantize_rows_dyn for each token and head, of the turned keys before any
- * rounding (a head whose scale no f32 holds is as one with an infinity: codes 0, scale NaN).  Rows at positions below 0, or that the page table does not reach, or whose page is not one of the cache's, are not written. */
+ * rounding (a head whose scale no f32 holds is as one with an infinity: codes 0, scale NaN).  Rows at positions below 0, or that the page
+ * table does not reach, or whose page is not one of the cache's, are not written. */
 int nimble_cache_write_dyn(const nimble_cache* cache, const nimble_sequences* seqs, const void* k, int64_t k_stride, const void* v,
                            int64_t v_stride, const void* q, int64_t q_stride, void* q_out, int64_t heads, const void* table,
                            int64_t table_rows, int64_t R, int interleaved, void* stream);

@@ -122,13 +122,14 @@ static PagedWaves paged_waves(int kernel, int64_t D, int dtype, bool lone) {
 
 // Which kernel.  16 rows a workgroup for up to 16 rows a sequence (32 of heads of 64 in 8 bits, where sequences and heads are many), and for more where nothing
 // is cut and its tiles are about as many as the chip holds; else 128.  Microseconds, 16 / 128 rows a workgroup (graph replays; rows: of a sequence and a head of the cache):
-//   bf16, heads of 64, 16 of the cache:  1 sequence, 128 rows over 628 keys 7.9 / 14.1, 512 over 1012 13 / 19; 16, 64 over 564 20 / 15, 128 over 628 35 / 17,
-//     1 sequence, 32 rows over 4032 17 / 13, 128 over 4128 25 / 17, over 30128 148 / 37
-//   bf16, 128, 8:  1, 128 over 532 12 / 17; 4, 13 / 17; 16, 45 / 19; 1, 32 over 4008 17 / 14, over 30008 50 / 31
-//   int8, 64, 16:  16, 128 over 628 28 / 21; 4, 32 over 4032 25 / 24, over 30032 91 / 98, 128 over 4128 58 / 36; 64, 32 over 532 27 / 34, over 4032 160 / 191;
-//     1, 32 over 4032 17 / 14
-//   int8, 128, 8:  16, 128 over 532 26 / 25; 4, 32 over 4008 24 / 23, over 30008 85 / 79, 128 over 30032 224 / 102
-// (On 560 shapes of 32 to 512 rows, 1 to 64 sequences and up to 30512 keys the rule's choice takes 0.2 % longer than the better one, 1.16 times at most.)
+//   bf16, heads of 64, 16 of the cache:  1 sequence, 128 rows over 628 keys 7.6 / 14.1, 512 over 1012 13 / 20; 16, 64 over 564 19 / 15, 128 over 628 34 / 17,
+//     1 sequence, 32 rows over 4032 17 / 13, 128 over 4128 25 / 17, over 30128 153 / 38
+//   bf16, 128, 8:  1, 128 over 532 11 / 17; 4, 12 / 17; 16, 41 / 19; 1, 32 over 4008 17 / 14, over 30008 51 / 31
+//   int8, 64, 16:  16, 128 over 628 27 / 21; 4, 32 over 4032 25 / 25, over 30032 90 / 80, 128 over 4128 58 / 36; 64, 32 over 532 27 / 34, over 4032 159 / 190;
+//     1, 32 over 4032 18 / 14
+//   int8, 128, 8:  16, 128 over 532 25 / 25; 4, 32 over 4008 24 / 23, over 30008 85 / 79, 128 over 30032 226 / 102
+// (On 560 shapes of 32 to 512 rows, 1 to 64 sequences of equal kind and up to 30512 keys the rule's choice takes 0.2 % longer than the better one; 1.5 times for 16 sequences of
+// 32 rows over 30008 keys of 8 heads of 64 in 8 bits, 199 / 135, 1.14 times at most elsewhere.)
 static int paged_kernel(int64_t rows, int64_t live, int64_t kv_heads, int64_t D, int dtype, int64_t keys) {
   if (keys <= kUncutKeys && (rows / kPagedRows[0] + live) * kv_heads <= kComputeUnits * 3 / 2 * four_waves_per_cu(D, dtype)) return NIMBLE_PAGED_TOKENS;
   const bool small = dtype == NIMBLE_I8 && D == 64 && live * kv_heads >= kComputeUnits / 4;
