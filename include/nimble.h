@@ -484,7 +484,8 @@ int nimble_rotary_dyn(const void* x, int64_t x_stride, const void* positions, co
                       int64_t y_stride, int64_t T, int64_t H, int64_t D, int64_t R, int interleaved, void* stream);
 
 /* Keys and values of new rows into the cache, k turned by its position first where table is given (R a multiple of 8; 2R <= D), and the
- * queries with them: q_out = rotary(q) where q is given (q_out [rows, heads, D] contiguous, may be q itself; with no table a copy).
+ * queries with them: q_out = rotary(q) where q is given (q_out [rows, heads, D] contiguous, may be q itself; with no table a copy).  Positions
+ * are held to 0..table_rows-1 for that, as in rotary.
  * bf16: rotary's rounding.  int8: the codes and scales of nimble_quantize_rows_dyn for each token and head, of the turned keys before any
  * rounding (a head whose scale no f32 holds is as one with an infinity: codes 0, scale NaN).  Rows at positions below 0, or that the page
  * table does not reach, or whose page is not one of the cache's, are not written. */
@@ -509,7 +510,8 @@ int nimble_cache_read_dyn(const nimble_cache* cache, const nimble_sequences* seq
 int nimble_paged_attention_dyn(const void* q, int64_t q_stride, const nimble_cache* cache, const nimble_sequences* seqs, void* o,
                                int64_t heads, float alpha, int64_t window, void* workspace, size_t workspace_bytes, void* stream);
 
-/* What the dispatch function decides for a call of nimble_paged_attention_dyn (host only; it looks at numbers, not at pointers). */
+/* What the dispatch function decides for a call of nimble_paged_attention_dyn (host only; it looks at numbers, not at pointers).  Without rows
+ * or sequences: nothing is launched, grid and workspace are 0. */
 typedef enum nimble_paged_kernel {
   NIMBLE_PAGED_TOKENS = 0, /* 16 rows (query heads that share keys, tokens) per workgroup, its waves share the keys among them */
   NIMBLE_PAGED_CHUNKS = 1, /* 128 rows per workgroup, 32 a wave                                                              */
